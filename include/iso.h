@@ -49,7 +49,17 @@ enum iso_status {
 
 enum iso_op {
     ISO_OP_ALLTOALL  = 0,        /* individual block per neighbour (Section 2)  */
-    ISO_OP_ALLGATHER = 1         /* same block to every neighbour (Section 2)   */
+    ISO_OP_ALLGATHER = 1,        /* same block to every neighbour (Section 2)   */
+    /* in iso_request_info only: the operators on the ranks' tokens, which have no plan */
+    ISO_OP_ATTENTION          = 2,
+    ISO_OP_ATTENTION_BACKWARD = 3,
+    ISO_OP_ROTARY             = 4
+};
+
+enum iso_dtype {                 /* element type of the operators' tensors      */
+    ISO_DTYPE_F32  = 0,
+    ISO_DTYPE_BF16 = 1,
+    ISO_DTYPE_F16  = 2
 };
 
 enum iso_algorithm {
@@ -447,6 +457,87 @@ int iso_request_free(iso_request_t *req);
 #define ISO_NOALLOC_TABLE_BYTES   (256u << 10)
 int iso_neighbor_alltoall_noalloc(const void *sendbuf, void *recvbuf, size_t m, iso_comm_t comm,
                                   int algorithm, void *hip_stream);
+
+/* ---- operators on the ranks' tokens ---------------------------------------------
+ * Every rank holds one token: a row of head_dim elements for every head.  A tensor of such rows is iso_heads_t: the device
+ * address of rank 0's first head and the distances, in elements, between consecutive ranks and consecutive heads (both >= 0,
+ * 0 repeats a row of an input); the elements of a row are consecutive.  [p][heads][head_dim], [heads][p][head_dim] and slices
+ * of one buffer of all projections are all of this form.  Addresses are aligned to the element size; rows on 16-byte
+ * boundaries that hold whole groups of 16 bytes are read and written fastest.
+ *
+ * The calls return requests as the collectives' do: buffers are bound once, iso_start enqueues the kernels on a stream (on
+ * one that is being captured as well) and returns, iso_wait and iso_request_free work as everywhere.  iso_start_range counts
+ * the operator's kernels, iso_request_set_graph makes a chain of them in both forms, and iso_request_plan is ISO_ERR_ARG.
+ * The same inputs give the same bits in every start.  Sums, softmax statistics and angles are held in 32 bits or more; what
+ * is written is rounded to the tensors' type once.
+ * Errors: ISO_ERR_ARG (null or misaligned pointer, bad count, type, scale or cap), ISO_ERR_TOO_LARGE (head_dim > 256, heads >
+ * 65536, 2^31 rows or more), ISO_ERR_OVERLAP (a written tensor shares bytes with another one, or two of its own rows do; rows
+ * of tensors with the same strides are told apart, other tensors by the ranges that they span), ISO_ERR_POINTER and
+ * ISO_ERR_WORKSPACE as in the collectives' init calls. */
+typedef struct {
+    void *data;
+    int64_t rank_stride, head_stride;
+} iso_heads_t;
+
+/* Attention of every rank R over its neighbourhood: neighbour i is the rank R (-) C^i whose block the allgather would deliver
+ * in place i, repeats and the rank itself (offset 0) as they are listed.
+ *     x_i = t_i + bias[h][i]     t_i = cap tanh(scale q . k_i / cap), or scale q . k_i where cap is 0
+ *     lse = log sum_i exp x_i    out = sum_i exp(x_i - lse) v_i
+ * A neighbour does not count where it has no source (mesh), or where segments are given and its segment is not the rank's; a
+ * negative segment holds no token.  Keys, values and biases of neighbours that do not count may hold anything, infinities and
+ * NaN included.  A row without neighbours gets out = 0 and lse = -inf, and no gradient.  A bias of -inf takes its neighbour
+ * out; where every bias of a row is -inf, the row is one without neighbours. */
+typedef struct {
+    int32_t dtype;               /* enum iso_dtype: of q, k, v, out, bias and the gradients */
+    int32_t q_heads, kv_heads;   /* kv_heads divides q_heads: head h reads key head h / (q_heads / kv_heads) */
+    int32_t head_dim;            /* 1 to 256 */
+    float scale;
+    float cap;                   /* 0: scores are not capped */
+    iso_heads_t q, out;          /* [p] rows, or [n_rows] where `rows` is given */
+    iso_heads_t k, v;            /* [p] rows */
+    float *lse;                  /* device [p or n_rows][q_heads]; may be NULL in the forward pass */
+    const void *bias;            /* device [q_heads][s], or NULL */
+    const int32_t *segments;     /* device [p], or NULL: all ranks in one */
+    /* Single tokens: the ranks whose rows q and out hold, device [n_rows], read when the request is started; NULL: all ranks
+     * in their order.  A rank outside [0, p) has no neighbours.  Forward pass only. */
+    const int64_t *rows;
+    int64_t n_rows;
+} iso_attention_t;
+
+/* Gradients of a sum over out with the weights grad_out.  grad_k and grad_v add up the q heads that share a key; grad_bias
+ * is [q_heads][s] of the tensors' type, or NULL.  All are overwritten. */
+typedef struct {
+    iso_heads_t grad_out;        /* [p] rows of q_heads */
+    iso_heads_t grad_q;          /* [p] rows of q_heads */
+    iso_heads_t grad_k, grad_v;  /* [p] rows of kv_heads */
+    void *grad_bias;
+} iso_attention_grads_t;
+
+int iso_neighbor_attention_init(const iso_attention_t *attention, iso_comm_t comm, iso_request_t *req);
+/* attention->out and ->lse are what the forward pass wrote. */
+int iso_neighbor_attention_backward_init(const iso_attention_t *attention, const iso_attention_grads_t *grads,
+                                         void *workspace, size_t workspace_bytes, iso_comm_t comm, iso_request_t *req);
+/* with_bias: grad_bias will be asked for. */
+int iso_neighbor_attention_backward_workspace_bytes(iso_comm_t comm, int dtype, int q_heads, int kv_heads, int head_dim,
+                                                    int with_bias, size_t *bytes);
+
+/* Rotary positions with several axes: pair j of a row's channels, (j, j + pairs) or (2j, 2j + 1) where `interleaved`, is
+ * turned by the angle w = position[axes[j]] * freqs[j], the same for all heads:
+ *     (a, b) -> (a cos w - b sin w, a sin w + b cos w)
+ * Channels from 2 * pairs on are copied.  `inverse` turns back, which is also the gradient.  out may be x (same strides). */
+typedef struct {
+    int32_t dtype, heads, head_dim;
+    int32_t pairs;               /* 0 to head_dim / 2 */
+    int32_t interleaved, inverse;
+    iso_heads_t x, out;          /* [n] rows */
+    int64_t n;                   /* tokens; p where the positions are the ranks' coordinates */
+    const double *freqs;         /* host, [pairs] */
+    const int32_t *axes;         /* host, [pairs] */
+    const int32_t *positions;    /* device [n][n_axes], read when the request is started; NULL: row R is at the coordinates of
+                                    rank R on comm's torus, axis j its dimension j */
+    int32_t n_axes;              /* of positions */
+} iso_rotary_t;
+int iso_rotary_init(const iso_rotary_t *rotary, iso_comm_t comm, iso_request_t *req);      /* comm: NULL with positions */
 
 /* ---- diagnostics ----------------------------------------------------------- */
 const char *iso_error_string(int status);

@@ -15,6 +15,8 @@ ISO_MAX_DIMS = 16
  ISO_ERR_TOO_LARGE, ISO_ERR_POINTER, ISO_ERR_SCRATCH) = range(9)
 ISO_NOALLOC_SCRATCH_BYTES, ISO_NOALLOC_TABLE_BYTES = 32 << 20, 256 << 10
 ISO_OP_ALLTOALL, ISO_OP_ALLGATHER = 0, 1
+ISO_OP_ATTENTION, ISO_OP_ATTENTION_BACKWARD, ISO_OP_ROTARY = 2, 3, 4
+ISO_DTYPE_F32, ISO_DTYPE_BF16, ISO_DTYPE_F16 = 0, 1, 2
 ISO_ALG_COMBINED, ISO_ALG_COMBINED_BYDIM, ISO_ALG_SX_ROUNDS, ISO_ALG_SX_FUSED, ISO_ALG_ONEHOP = 0, 1, 2, 3, 4
 ISO_ALG_COMBINED_STAGED = 5
 ISO_BUF_SEND, ISO_BUF_RECV, ISO_BUF_WORK = 0, 1, 2
@@ -75,6 +77,30 @@ class iso_start_info_t(ctypes.Structure):
                 ("bytes_read", ctypes.c_uint64), ("bytes_written", ctypes.c_uint64)]
 
 
+class iso_heads_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rank_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class iso_attention_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("q", iso_heads_t), ("out", iso_heads_t), ("k", iso_heads_t), ("v", iso_heads_t),
+                ("lse", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("segments", ctypes.c_void_p),
+                ("rows", ctypes.c_void_p), ("n_rows", ctypes.c_int64)]
+
+
+class iso_attention_grads_t(ctypes.Structure):
+    _fields_ = [("grad_out", iso_heads_t), ("grad_q", iso_heads_t), ("grad_k", iso_heads_t), ("grad_v", iso_heads_t),
+                ("grad_bias", ctypes.c_void_p)]
+
+
+class iso_rotary_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("x", iso_heads_t), ("out", iso_heads_t), ("n", ctypes.c_int64), ("freqs", ctypes.c_void_p),
+                ("axes", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n_axes", ctypes.c_int32)]
+
+
 def _struct_dict(st):
     out = {}
     for name, _ in st._fields_:
@@ -121,6 +147,11 @@ _PROTOTYPES = {
     "iso_neighbor_allgatherw_init": ([_VP, _SZ, _SZ, _VP, _VP, _VP, _SZ, _VP, _SZ, _VP, _I,
                                       ctypes.POINTER(_VP)], _I),
     "iso_neighbor_alltoall_noalloc": ([_VP, _VP, _SZ, _VP, _I, _VP], _I),
+    "iso_neighbor_attention_init": ([ctypes.POINTER(iso_attention_t), _VP, ctypes.POINTER(_VP)], _I),
+    "iso_neighbor_attention_backward_init": ([ctypes.POINTER(iso_attention_t), ctypes.POINTER(iso_attention_grads_t),
+                                              _VP, _SZ, _VP, ctypes.POINTER(_VP)], _I),
+    "iso_neighbor_attention_backward_workspace_bytes": ([_VP, _I, _I, _I, _I, _I, ctypes.POINTER(_SZ)], _I),
+    "iso_rotary_init": ([ctypes.POINTER(iso_rotary_t), _VP, ctypes.POINTER(_VP)], _I),
     "iso_start": ([_VP, _VP], _I),
     "iso_start_range": ([_VP, _I, _I, _VP], _I),
     "iso_request_set_graph": ([_VP, _I], _I),
@@ -488,6 +519,111 @@ def iso_neighbor_alltoall_noalloc(sendbuf, recvbuf, m, comm, algorithm=ISO_ALG_C
     """One all-to-all enqueued on `stream` with no device allocation (see iso.h)."""
     _check(load_library().iso_neighbor_alltoall_noalloc(_ptr(sendbuf), _ptr(recvbuf), m, comm.handle, algorithm,
                                                         _stream_handle(stream)), "iso_neighbor_alltoall_noalloc")
+
+
+def _dtype(dtype):
+    import torch
+    known = {torch.float32: ISO_DTYPE_F32, torch.bfloat16: ISO_DTYPE_BF16, torch.float16: ISO_DTYPE_F16}
+    if dtype not in known:
+        raise TypeError("tensors must be float32, bfloat16 or float16")
+    return known[dtype]
+
+
+def _heads(x, shape, dtype, name):
+    """A [ranks][heads][head_dim] tensor with any strides but of its rows, as iso_heads_t."""
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}, not {tuple(x.shape)} of {x.dtype}")
+    if x.numel() and x.shape[2] > 1 and x.stride(2) != 1:
+        raise ValueError(f"{name}: the elements of a row must be consecutive")
+    return iso_heads_t(x.data_ptr() or None, x.stride(0), x.stride(1))
+
+
+def _array(x, shape, dtype, name):
+    if x is None:
+        return None
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}, not {tuple(x.shape)} of {x.dtype}")
+    return _ptr(x)
+
+
+def _attention(q, k, v, out, lse, bias, segments, scale, cap, rows, comm):
+    import torch
+    info = iso_neighborhood_info(comm)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [ranks][heads][head_dim]")
+    n, q_heads, head_dim = q.shape
+    kv_heads, p, s = k.shape[1], info["p"], info["s"]
+    if rows is None and n != p:
+        raise ValueError(f"q must hold the rows of all {p} ranks, or `rows` say whose rows it holds")
+    t = iso_attention_t(dtype=_dtype(q.dtype), q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, cap=cap,
+                        scale=head_dim ** -0.5 if scale is None else scale,
+                        n_rows=0 if rows is None else n)
+    t.q, t.out = _heads(q, q.shape, q.dtype, "q"), _heads(out, q.shape, q.dtype, "out")
+    t.k, t.v = (_heads(x, (p, kv_heads, head_dim), q.dtype, name) for x, name in ((k, "k"), (v, "v")))
+    t.lse = _array(lse, (n, q_heads), torch.float32, "lse")
+    t.bias = _array(bias, (q_heads, s), q.dtype, "bias")
+    t.segments = _array(segments, (p,), torch.int32, "segments")
+    t.rows = _array(rows, (n,), torch.int64, "rows")
+    if rows is not None and not n:
+        t.rows = 8                       # an empty list has no address, and NULL would stand for all ranks; never read
+    return t
+
+
+def iso_neighbor_attention_init(q, k, v, out, comm, *, lse=None, bias=None, segments=None, scale=None, cap=0.0, rows=None):
+    """q, out: [p][q_heads][head_dim], or [len(rows)][...] for single tokens; k, v: [p][kv_heads][head_dim]; any strides with
+    consecutive elements in a row.  scale: head_dim ** -0.5 unless given.  The rest as in iso.h."""
+    t = _attention(q, k, v, out, lse, bias, segments, scale, cap, rows, comm)
+    h = ctypes.c_void_p()
+    _check(load_library().iso_neighbor_attention_init(ctypes.byref(t), comm.handle, ctypes.byref(h)), "iso_neighbor_attention_init")
+    return Request(h.value, (q, k, v, out, lse, bias, segments, rows))
+
+
+def iso_neighbor_attention_backward_workspace_bytes(comm, q_heads, kv_heads, head_dim, dtype, bias=False):
+    """dtype: of the tensors (torch); bias: whether grad_bias will be asked for."""
+    out = ctypes.c_size_t()
+    _check(load_library().iso_neighbor_attention_backward_workspace_bytes(
+        comm.handle, _dtype(dtype), q_heads, kv_heads, head_dim, int(bool(bias)), ctypes.byref(out)),
+        "iso_neighbor_attention_backward_workspace_bytes")
+    return out.value
+
+
+def iso_neighbor_attention_backward_init(q, k, v, out, lse, grad_out, grad_q, grad_k, grad_v, workspace, comm, *, bias=None,
+                                         grad_bias=None, segments=None, scale=None, cap=0.0, workspace_bytes=None):
+    """out, lse: as the forward pass left them; grad_*: shaped as what they belong to, any strides."""
+    t = _attention(q, k, v, out, lse, bias, segments, scale, cap, None, comm)
+    g = iso_attention_grads_t()
+    g.grad_out, g.grad_q = _heads(grad_out, q.shape, q.dtype, "grad_out"), _heads(grad_q, q.shape, q.dtype, "grad_q")
+    g.grad_k, g.grad_v = _heads(grad_k, k.shape, q.dtype, "grad_k"), _heads(grad_v, k.shape, q.dtype, "grad_v")
+    g.grad_bias = _array(grad_bias, (q.shape[1], iso_neighborhood_info(comm)["s"]), q.dtype, "grad_bias")
+    h = ctypes.c_void_p()
+    _check(load_library().iso_neighbor_attention_backward_init(
+        ctypes.byref(t), ctypes.byref(g), _ptr(workspace), _nbytes(workspace, workspace_bytes), comm.handle, ctypes.byref(h)),
+        "iso_neighbor_attention_backward_init")
+    return Request(h.value, (q, k, v, out, lse, grad_out, grad_q, grad_k, grad_v, workspace, bias, grad_bias, segments))
+
+
+def iso_rotary_init(x, out, freqs, axes, comm=None, *, positions=None, interleaved=False, inverse=False):
+    """x, out: [n][heads][head_dim]; freqs, axes: one value for each pair of channels; positions: [n][axes] int32, or None for
+    the coordinates of comm's ranks."""
+    import torch
+    if x.dim() != 3:
+        raise ValueError("x must be [tokens][heads][head_dim]")
+    freqs = np.ascontiguousarray(freqs, dtype=np.float64).reshape(-1)
+    axes = np.ascontiguousarray(axes, dtype=np.int32).reshape(-1)
+    if freqs.size != axes.size:
+        raise ValueError("freqs and axes must have one value for each pair")
+    t = iso_rotary_t(dtype=_dtype(x.dtype), heads=x.shape[1], head_dim=x.shape[2], pairs=freqs.size,
+                     interleaved=int(bool(interleaved)), inverse=int(bool(inverse)), n=x.shape[0],
+                     freqs=freqs.ctypes.data, axes=axes.ctypes.data)
+    t.x, t.out = _heads(x, x.shape, x.dtype, "x"), _heads(out, x.shape, x.dtype, "out")
+    if positions is not None:
+        if positions.dim() != 2:
+            raise ValueError("positions must be [tokens][axes]")
+        t.positions, t.n_axes = _array(positions, (x.shape[0], positions.shape[1]), torch.int32, "positions"), positions.shape[1]
+    h = ctypes.c_void_p()
+    _check(load_library().iso_rotary_init(ctypes.byref(t), comm.handle if comm is not None else None, ctypes.byref(h)),
+           "iso_rotary_init")
+    return Request(h.value, (x, out, positions))
 
 
 def iso_start(req, stream=None):

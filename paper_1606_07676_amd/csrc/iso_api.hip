@@ -8,11 +8,13 @@
 #include <memory>
 #include <mutex>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "iso.h"
 #include "iso_bind.hpp"
 #include "iso_kernels.hpp"
+#include "iso_operators.hpp"
 #include "iso_plan.hpp"
 
 namespace iso {
@@ -40,6 +42,7 @@ struct iso_plan_s {
 
 struct iso_request_s {
     iso::BoundRequest b;
+    std::unique_ptr<iso::BoundOperator> op;    // an operator's launches in place of a bound plan; its table is b.dev_table
     iso_plan_s plan_view;                // what iso_request_plan hands out
     hipStream_t last_stream = nullptr;
     bool started = false;
@@ -47,6 +50,11 @@ struct iso_request_s {
     hipGraphExec_t graph_exec = nullptr;
     int graph_form = 0;                  // ISO_GRAPH_CHAIN or ISO_GRAPH_BRANCHES: what `graph` was built as
     bool use_graph = false;
+
+    size_t launch_count() const { return op ? op->launches.size() : b.launches.size(); }
+    int enqueue_launch(size_t q, hipStream_t stream) const {
+        return op ? iso::enqueue_operator(op->launches[q], stream) : iso::enqueue(b.info.vector_bytes, b.launches[q], stream);
+    }
 };
 
 namespace {
@@ -137,6 +145,34 @@ int make_request(int op, const iso::Layout &lay, const void *sendbuf, void *recv
     if (st != ISO_SUCCESS) return st;
     guard.r = nullptr;
     *out = rq;
+    return ISO_SUCCESS;
+}
+
+// A request of an operator on the ranks' tokens: bind fills its launches and its device table.
+template <typename Bind>
+int make_operator_request(int op, const iso::Comm *comm, size_t workspace_bytes, iso_request_t *out, Bind &&bind) {
+    if (!out) return ISO_ERR_ARG;
+    struct Free {
+        void operator()(iso_request_s *r) const {
+            if (r->op->dev_table) (void)hipFree(r->op->dev_table);
+            delete r;
+        }
+    };
+    std::unique_ptr<iso::BoundOperator> bound = std::make_unique<iso::BoundOperator>();
+    std::unique_ptr<iso_request_s> fresh = std::make_unique<iso_request_s>();
+    fresh->op = std::move(bound);
+    std::unique_ptr<iso_request_s, Free> rq(fresh.release());
+    const int st = bind(*rq->op);
+    if (st != ISO_SUCCESS) return st;
+    iso_request_info_t &info = rq->b.info;
+    info.op = op;
+    info.algorithm = -1;
+    info.launches = (int32_t)rq->op->launches.size();
+    info.p = comm ? comm->p : 0;
+    info.s = comm ? comm->s : 0;
+    info.workspace_bytes = workspace_bytes;
+    rq->b.dev_table = std::exchange(rq->op->dev_table, nullptr);
+    *out = rq.release();
     return ISO_SUCCESS;
 }
 
@@ -547,9 +583,53 @@ int iso_neighbor_alltoall_noalloc(const void *sendbuf, void *recvbuf, size_t m, 
     });
 }
 
+int iso_neighbor_attention_init(const iso_attention_t *attention, iso_comm_t comm, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!attention || !comm) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_ATTENTION, &comm->c, 0, req, [&](iso::BoundOperator &op) {
+            return iso::AttentionBinder(op, comm->c, *attention, nullptr).bind(nullptr, 0);
+        });
+    });
+}
+
+int iso_neighbor_attention_backward_init(const iso_attention_t *attention, const iso_attention_grads_t *grads,
+                                         void *workspace, size_t workspace_bytes, iso_comm_t comm, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!attention || !grads || !comm) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_ATTENTION_BACKWARD, &comm->c, workspace_bytes, req, [&](iso::BoundOperator &op) {
+            return iso::AttentionBinder(op, comm->c, *attention, grads).bind(workspace, workspace_bytes);
+        });
+    });
+}
+
+int iso_neighbor_attention_backward_workspace_bytes(iso_comm_t comm, int dtype, int q_heads, int kv_heads, int head_dim,
+                                                    int with_bias, size_t *bytes) {
+    return guarded([&]() -> int {
+        if (!comm || !bytes) return ISO_ERR_ARG;
+        int st = iso::check_shape(dtype, q_heads, kv_heads, head_dim);
+        if (st != ISO_SUCCESS) return st;
+        iso::BackwardWorkspace w;
+        if ((st = iso::backward_workspace(comm->c, q_heads, with_bias != 0, w)) != ISO_SUCCESS) return st;
+        *bytes = (size_t)w.bytes;
+        return ISO_SUCCESS;
+    });
+}
+
+int iso_rotary_init(const iso_rotary_t *rotary, iso_comm_t comm, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!rotary) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_ROTARY, comm ? &comm->c : nullptr, 0, req, [&](iso::BoundOperator &op) {
+            return iso::bind_rotary(op, comm ? &comm->c : nullptr, *rotary);
+        });
+    });
+}
+
 int iso_request_set_graph(iso_request_t req, int enable) {
     if (!req || enable < 0 || enable > ISO_GRAPH_BRANCHES) return ISO_ERR_ARG;
-    if (!enable || req->b.launches.empty()) {
+    if (!enable || !req->launch_count()) {
         req->use_graph = false;
         return ISO_SUCCESS;
     }
@@ -580,26 +660,35 @@ int iso_request_set_graph(iso_request_t req, int enable) {
         };
         hipGraph_t g = nullptr;
         ISO_HIP_TRY(hipGraphCreate(&g, 0));
-        std::vector<hipGraphNode_t> nodes(req->b.launches.size());
+        std::vector<hipGraphNode_t> nodes(req->launch_count());
         hipError_t e = hipSuccess;
-        for (size_t i = 0; i < req->b.launches.size() && e == hipSuccess; ++i) {
-            const iso::Launch &l = req->b.launches[i];
+        for (size_t i = 0; i < nodes.size() && e == hipSuccess; ++i) {
             std::vector<hipGraphNode_t> deps;
-            if (enable == ISO_GRAPH_CHAIN) {
+            if (enable == ISO_GRAPH_CHAIN || req->op) {
                 if (i) deps.push_back(nodes[i - 1]);
             } else {
                 for (size_t j = 0; j < i; ++j) {
-                    const int rj = req->b.launches[j].round;
-                    if (rj != l.round && conflict(rj, l.round)) deps.push_back(nodes[j]);
+                    const int ri = req->b.launches[i].round, rj = req->b.launches[j].round;
+                    if (rj != ri && conflict(rj, ri)) deps.push_back(nodes[j]);
                 }
             }
-            const iso::KernelRef k = iso::select_kernel(req->b.info.vector_bytes, l);
-            void *args[1] = {const_cast<void *>(k.arg)};
+            void *args[1] = {nullptr};
             hipKernelNodeParams np{};
-            np.func = const_cast<void *>(k.func);
-            np.gridDim = dim3(l.grid);
-            np.blockDim = dim3(iso::kThreads);
-            np.sharedMemBytes = l.dyn_lds;
+            if (req->op) {
+                const iso::OperatorLaunch &l = req->op->launches[i];
+                args[0] = l.args.get();
+                np.func = const_cast<void *>(l.func);
+                np.gridDim = dim3(l.grid);
+                np.blockDim = dim3(l.threads);
+            } else {
+                const iso::Launch &l = req->b.launches[i];
+                const iso::KernelRef k = iso::select_kernel(req->b.info.vector_bytes, l);
+                args[0] = const_cast<void *>(k.arg);
+                np.func = const_cast<void *>(k.func);
+                np.gridDim = dim3(l.grid);
+                np.blockDim = dim3(iso::kThreads);
+                np.sharedMemBytes = l.dyn_lds;
+            }
             np.kernelParams = args;
             np.extra = nullptr;
             e = hipGraphAddKernelNode(&nodes[i], g, deps.empty() ? nullptr : deps.data(), deps.size(), &np);
@@ -624,6 +713,11 @@ int iso_start(iso_request_t req, void *hip_stream) {
     hipStream_t stream = (hipStream_t)hip_stream;
     if (req->use_graph) {
         ISO_HIP_TRY(hipGraphLaunch(req->graph_exec, stream));
+    } else if (req->op) {
+        for (const iso::OperatorLaunch &l : req->op->launches) {
+            int st = iso::enqueue_operator(l, stream);
+            if (st != ISO_SUCCESS) return st;
+        }
     } else {
         for (const iso::Launch &l : req->b.start_list()) {
             int st = iso::enqueue(req->b.info.vector_bytes, l, stream);
@@ -636,11 +730,11 @@ int iso_start(iso_request_t req, void *hip_stream) {
 }
 
 int iso_start_range(iso_request_t req, int first, int count, void *hip_stream) {
-    if (!req || first < 0 || count < 0 || (size_t)first + (size_t)count > req->b.launches.size())
+    if (!req || first < 0 || count < 0 || (size_t)first + (size_t)count > req->launch_count())
         return ISO_ERR_ARG;
     hipStream_t stream = (hipStream_t)hip_stream;
     for (int q = first; q < first + count; ++q) {
-        int st = iso::enqueue(req->b.info.vector_bytes, req->b.launches[(size_t)q], stream);
+        int st = req->enqueue_launch((size_t)q, stream);
         if (st != ISO_SUCCESS) return st;
     }
     req->last_stream = stream;
@@ -650,7 +744,7 @@ int iso_start_range(iso_request_t req, int first, int count, void *hip_stream) {
 
 int iso_wait(iso_request_t req) {
     if (!req) return ISO_ERR_ARG;
-    if (!req->started || req->b.launches.empty()) return ISO_SUCCESS;
+    if (!req->started || !req->launch_count()) return ISO_SUCCESS;
     ISO_HIP_TRY(hipStreamSynchronize(req->last_stream));
     return ISO_SUCCESS;
 }
@@ -663,6 +757,11 @@ int iso_request_info(iso_request_t req, iso_request_info_t *info) {
 
 int iso_request_start_info(iso_request_t req, iso_start_info_t *info) {
     if (!req || !info) return ISO_ERR_ARG;
+    if (req->op) {
+        *info = iso_start_info_t{};
+        info->kernels = (int32_t)req->op->launches.size();
+        return ISO_SUCCESS;
+    }
     const std::vector<iso::Launch> &list = req->use_graph ? req->b.launches : req->b.start_list();
     *info = iso_start_info_t{};
     info->kernels = (int32_t)list.size();
@@ -675,7 +774,7 @@ int iso_request_start_info(iso_request_t req, iso_start_info_t *info) {
 
 int iso_request_plan(iso_request_t req, iso_plan_t *plan) {
     return guarded([&]() -> int {
-        if (!req || !plan) return ISO_ERR_ARG;
+        if (!req || !plan || req->op) return ISO_ERR_ARG;
         if (req->plan_view.p.rounds.empty()) req->plan_view.p = req->b.plan;
         *plan = &req->plan_view;
         return ISO_SUCCESS;
@@ -687,7 +786,7 @@ int iso_request_free(iso_request_t *req) {
     int st = ISO_SUCCESS;
     if (*req) {
         // the last collective may still be running: its kernels read the device table
-        if ((*req)->started && !(*req)->b.launches.empty()) {
+        if ((*req)->started && (*req)->launch_count()) {
             hipError_t e = hipStreamSynchronize((*req)->last_stream);
             if (e != hipSuccess) {
                 g_last_hip_error = (int)e;

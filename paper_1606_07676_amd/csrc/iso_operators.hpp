@@ -1,0 +1,390 @@
+// Host side of the operators on the ranks' tokens (attention over the neighbourhood, rotary positions): argument checks,
+// the choice of kernels and the launches of a request.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <memory>
+#include <vector>
+
+#include "iso_attention_kernels.hpp"
+#include "iso_bind.hpp"
+#include "iso_rotary_kernels.hpp"
+
+namespace iso {
+
+// One kernel launch of an operator: its arguments are one struct, kept with it.
+struct OperatorLaunch {
+    const void *func = nullptr;
+    uint32_t grid = 0, threads = 0;
+    std::shared_ptr<void> args;
+};
+
+struct BoundOperator {
+    std::vector<OperatorLaunch> launches;
+    void *dev_table = nullptr;             // owned by the request
+};
+
+template <typename Args>
+int add_launch(BoundOperator &b, const void *func, uint64_t grid, uint32_t threads, const Args &args) {
+    if (!grid) return ISO_SUCCESS;
+    if (grid > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
+    b.launches.push_back({func, (uint32_t)grid, threads, std::make_shared<Args>(args)});
+    return ISO_SUCCESS;
+}
+
+inline int enqueue_operator(const OperatorLaunch &l, hipStream_t stream) {
+    void *args[1] = {l.args.get()};
+    ISO_HIP_TRY(hipLaunchKernel(l.func, dim3(l.grid), dim3(l.threads), args, 0, stream));
+    return ISO_SUCCESS;
+}
+
+inline size_t dtype_size(int dtype) { return dtype == ISO_DTYPE_F32 ? 4 : 2; }
+
+// ---- buffers -------------------------------------------------------------------
+
+// n ranks with `heads` rows of `bytes` each, strides in bytes; a plain array is one head.
+struct Region {
+    uintptr_t at;
+    uint64_t n, heads, rank_stride, head_stride, bytes;
+    bool written;
+
+    bool empty() const { return !n || !heads || !bytes; }
+    uint64_t footprint() const { return (heads - 1) * head_stride + bytes; }     // of one rank
+    uint64_t span() const { return (n - 1) * rank_stride + footprint(); }
+};
+
+constexpr uint64_t kMaxSpan = uint64_t(1) << 60;
+
+// Rows of tensors that share their strides (slices of one [p][heads][head_dim] buffer) are told apart rank by rank, or head
+// by head; anything else by the ranges that they span.
+inline bool regions_meet(const Region &a, const Region &b) {
+    if (a.empty() || b.empty()) return false;
+    if (a.at + a.span() <= b.at || b.at + b.span() <= a.at) return false;
+    if (a.rank_stride != b.rank_stride || !a.rank_stride) return true;
+    const uint64_t rank = a.rank_stride;
+    if (a.footprint() > rank || b.footprint() > rank) return true;
+    const uint64_t delta = b.at >= a.at ? (b.at - a.at) % rank : (rank - (a.at - b.at) % rank) % rank;
+    if (delta >= a.footprint() && delta + b.footprint() <= rank) return false;
+    const uint64_t head = a.head_stride;
+    if (!head || head != b.head_stride || rank % head) return true;
+    return !(delta % head >= a.bytes && delta % head + b.bytes <= head);
+}
+
+// Two rows of one written tensor must not share bytes.
+inline bool region_meets_itself(const Region &r) {
+    if (r.empty()) return false;
+    const bool by_rank = (r.heads == 1 || r.head_stride >= r.bytes) && (r.n == 1 || r.rank_stride >= r.footprint());
+    const bool by_head = (r.n == 1 || r.rank_stride >= r.bytes) &&
+                         (r.heads == 1 || r.head_stride >= (r.n - 1) * r.rank_stride + r.bytes);
+    return !by_rank && !by_head;
+}
+
+// The buffers of one request.
+class Regions {
+  public:
+    int heads(const iso_heads_t &t, uint64_t n, int heads, int head_dim, int dtype, bool written) {
+        const uint64_t size = dtype_size(dtype);
+        if (!n || !heads || !head_dim) return ISO_SUCCESS;
+        if (!t.data || t.rank_stride < 0 || t.head_stride < 0 || (uintptr_t)t.data % size) return ISO_ERR_ARG;
+        if ((uint64_t)t.rank_stride > kMaxSpan / size / n || (uint64_t)t.head_stride > kMaxSpan / size / (uint64_t)heads)
+            return ISO_ERR_TOO_LARGE;
+        return add({(uintptr_t)t.data, n, (uint64_t)heads, (uint64_t)t.rank_stride * size, (uint64_t)t.head_stride * size,
+                    (uint64_t)head_dim * size, written});
+    }
+    int array(const void *data, uint64_t bytes, uint64_t alignment, bool written) {
+        if (!bytes) return ISO_SUCCESS;
+        if (!data || (uintptr_t)data % alignment) return ISO_ERR_ARG;
+        return add({(uintptr_t)data, 1, 1, 0, 0, bytes, written});
+    }
+    // except: this pair of regions may be the same rows (an operator in place)
+    int disjoint(int except_a = -1, int except_b = -1) const {
+        for (size_t i = 0; i < list.size(); ++i) {
+            if (list[i].written && region_meets_itself(list[i])) return ISO_ERR_OVERLAP;
+            for (size_t j = 0; j < i; ++j) {
+                if ((int)j == except_a && (int)i == except_b) continue;
+                if ((list[i].written || list[j].written) && regions_meet(list[i], list[j])) return ISO_ERR_OVERLAP;
+            }
+        }
+        return ISO_SUCCESS;
+    }
+
+  private:
+    int add(const Region &r) {
+        list.push_back(r);
+        return check_device_range((const void *)r.at, r.span());
+    }
+    std::vector<Region> list;
+};
+
+inline Heads device_heads(const iso_heads_t &t) { return Heads{t.data, t.rank_stride, t.head_stride}; }
+
+// Rows start on 16-byte boundaries and hold whole groups of 16 bytes.
+inline bool wide(const iso_heads_t &t, int head_dim, int dtype) {
+    const uint64_t size = dtype_size(dtype);
+    return (((uintptr_t)t.data | (uint64_t)t.rank_stride * size | (uint64_t)t.head_stride * size | (uint64_t)head_dim * size) & 15) == 0;
+}
+
+// Offsets as the kernels add them: residues where the dimension wraps; where it does not, a coordinate beyond the mesh's
+// size has no source from anywhere, as the size itself has none, and sums stay inside 32 bits.
+inline std::vector<int32_t> kernel_offsets(const Comm &c) {
+    std::vector<int32_t> out((size_t)c.s * c.d);
+    for (int i = 0; i < c.s; ++i)
+        for (int j = 0; j < c.d; ++j) {
+            const int32_t n = c.dims[j], x = c.c(i, j);
+            out[(size_t)i * c.d + j] = c.periodic[j] ? x : std::clamp(x, -n, n);
+        }
+    return out;
+}
+
+inline NeighbourTorus neighbour_torus(const Comm &c, const void *offsets) {
+    NeighbourTorus t{};
+    t.d = c.d;
+    t.s = c.s;
+    t.p = (uint32_t)c.p;
+    for (int j = 0; j < c.d; ++j) {
+        t.dims[j] = c.dims[j];
+        t.inner[j] = (int32_t)c.inner[j];
+        if (!c.periodic[j]) t.open |= 1u << j;
+    }
+    t.offsets = (const int32_t *)offsets;
+    return t;
+}
+
+inline int upload_table(BoundOperator &b, const void *host, size_t bytes) {
+    if (!bytes) return ISO_SUCCESS;
+    ISO_HIP_TRY(hipMalloc(&b.dev_table, bytes));
+    ISO_HIP_TRY(hipMemcpy(b.dev_table, host, bytes, hipMemcpyHostToDevice));
+    return ISO_SUCCESS;
+}
+
+#define ISO_TRY(expr)                              \
+    do {                                           \
+        const int st_ = (expr);                    \
+        if (st_ != ISO_SUCCESS) return st_;        \
+    } while (0)
+
+// ---- attention --------------------------------------------------------------------
+
+template <template <typename, bool> class Kernel>
+const void *by_type(int dtype, bool wide) {
+    switch (dtype) {
+        case ISO_DTYPE_F32: return wide ? Kernel<float, true>::func() : Kernel<float, false>::func();
+        case ISO_DTYPE_BF16: return wide ? Kernel<__bf16, true>::func() : Kernel<__bf16, false>::func();
+        default: return wide ? Kernel<_Float16, true>::func() : Kernel<_Float16, false>::func();
+    }
+}
+#define ISO_KERNEL_BY_TYPE(name, kernel)                                            \
+    template <typename T, bool WIDE> struct name {                                  \
+        static const void *func() { return (const void *)(kernel<T, WIDE>); }       \
+    };
+ISO_KERNEL_BY_TYPE(RowKernel, attention_row_kernel)
+ISO_KERNEL_BY_TYPE(SplitRowKernel, attention_split_row_kernel)
+ISO_KERNEL_BY_TYPE(GradQRowKernel, attention_grad_q_row_kernel)
+ISO_KERNEL_BY_TYPE(GradKVRowKernel, attention_grad_kv_row_kernel)
+ISO_KERNEL_BY_TYPE(GradBiasRowKernel, attention_grad_bias_row_kernel)
+ISO_KERNEL_BY_TYPE(RotaryKernel, rotary_kernel)
+#undef ISO_KERNEL_BY_TYPE
+
+inline const void *sum_parts_by_type(int dtype) {
+    switch (dtype) {
+        case ISO_DTYPE_F32: return (const void *)(sum_parts_kernel<float>);
+        case ISO_DTYPE_BF16: return (const void *)(sum_parts_kernel<__bf16>);
+        default: return (const void *)(sum_parts_kernel<_Float16>);
+    }
+}
+
+// Parts of the ranks that the bias's gradient is summed over: enough wavefronts for the GPU, 64 ranks or more in each.
+inline uint64_t bias_parts(const Comm &c, int q_heads) {
+    const uint64_t slots = std::max<uint64_t>(1, (uint64_t)q_heads * c.s);
+    return std::clamp<uint64_t>(8192 / slots, 1, ((uint64_t)c.p + 63) / 64);
+}
+
+struct BackwardWorkspace {
+    uint64_t delta = 0, partials = 0, bytes = 0;                 // offsets
+};
+inline int backward_workspace(const Comm &c, int q_heads, bool bias, BackwardWorkspace &w) {
+    const uint64_t rows = (uint64_t)c.p * q_heads;               // below 2^47
+    w.partials = (rows * 4 + 255) / 256 * 256;
+    w.bytes = w.partials;
+    if (bias) {
+        if ((uint64_t)q_heads * c.s > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
+        w.bytes += bias_parts(c, q_heads) * q_heads * c.s * 4;
+    }
+    return ISO_SUCCESS;
+}
+
+inline int check_shape(int dtype, int q_heads, int kv_heads, int head_dim) {
+    if (dtype != ISO_DTYPE_F32 && dtype != ISO_DTYPE_BF16 && dtype != ISO_DTYPE_F16) return ISO_ERR_ARG;
+    if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || head_dim < 1) return ISO_ERR_ARG;
+    if (q_heads > 65536 || head_dim > kAttentionMaxHeadDim) return ISO_ERR_TOO_LARGE;
+    return ISO_SUCCESS;
+}
+
+class AttentionBinder {
+  public:
+    AttentionBinder(BoundOperator &out, const Comm &comm, const iso_attention_t &attention, const iso_attention_grads_t *grads)
+        : b(out), c(comm), t(attention), g(grads) {}
+
+    int bind(void *workspace, size_t workspace_bytes) {
+        ISO_TRY(check_shape(t.dtype, t.q_heads, t.kv_heads, t.head_dim));
+        if (!(t.cap >= 0.f) || std::isinf(t.cap) || !std::isfinite(t.scale)) return ISO_ERR_ARG;
+        if (t.n_rows < 0 || (t.n_rows && !t.rows) || (g && t.rows)) return ISO_ERR_ARG;
+        if (t.n_rows > 0x7FFFFFFF) return ISO_ERR_TOO_LARGE;
+        n = t.rows ? (uint64_t)t.n_rows : (uint64_t)c.p;
+        ISO_TRY(check_buffers(workspace, workspace_bytes));
+        if (!n) return ISO_SUCCESS;
+        const std::vector<int32_t> offsets = kernel_offsets(c);
+        ISO_TRY(upload_table(b, offsets.data(), offsets.size() * sizeof(int32_t)));
+        fill_args(workspace);
+        return g ? backward() : forward();
+    }
+
+  private:
+    int check_buffers(void *workspace, size_t workspace_bytes) {
+        Regions r;
+        const int nq = t.q_heads, nk = t.kv_heads, D = t.head_dim, dt = t.dtype;
+        const uint64_t p = (uint64_t)c.p, slots = (uint64_t)nq * c.s, size = dtype_size(dt);
+        ISO_TRY(r.heads(t.q, n, nq, D, dt, false));
+        ISO_TRY(r.heads(t.k, n ? p : 0, nk, D, dt, false));
+        ISO_TRY(r.heads(t.v, n ? p : 0, nk, D, dt, false));
+        ISO_TRY(r.heads(t.out, n, nq, D, dt, !g));
+        if (g && !t.lse) return ISO_ERR_ARG;
+        if (t.lse) ISO_TRY(r.array(t.lse, n * nq * 4, 4, !g));
+        if (t.bias && n) ISO_TRY(r.array(t.bias, slots * size, size, false));
+        if (t.segments && n) ISO_TRY(r.array(t.segments, p * 4, 4, false));
+        if (t.rows) ISO_TRY(r.array(t.rows, n * 8, 8, false));
+        if (g) {
+            ISO_TRY(r.heads(g->grad_out, n, nq, D, dt, false));
+            ISO_TRY(r.heads(g->grad_q, n, nq, D, dt, true));
+            ISO_TRY(r.heads(g->grad_k, n, nk, D, dt, true));
+            ISO_TRY(r.heads(g->grad_v, n, nk, D, dt, true));
+            if (g->grad_bias && !t.bias && c.s) return ISO_ERR_ARG;
+            if (g->grad_bias) ISO_TRY(r.array(g->grad_bias, slots * size, size, true));
+            ISO_TRY(backward_workspace(c, nq, g->grad_bias != nullptr, work));
+            if (!workspace || workspace_bytes < work.bytes) return ISO_ERR_WORKSPACE;
+            ISO_TRY(r.array(workspace, work.bytes, 4, true));
+        }
+        return r.disjoint();
+    }
+
+    void fill_args(void *workspace) {
+        a = AttentionArgs{};
+        a.torus = neighbour_torus(c, b.dev_table);
+        a.q = device_heads(t.q);
+        a.k = device_heads(t.k);
+        a.v = device_heads(t.v);
+        a.out = device_heads(t.out);
+        a.lse = t.lse;
+        a.bias = c.s ? t.bias : nullptr;
+        a.segments = t.segments;
+        a.rows = t.rows;
+        a.n = (uint32_t)n;
+        a.q_heads = t.q_heads;
+        a.kv_heads = t.kv_heads;
+        a.group = t.q_heads / t.kv_heads;
+        a.head_dim = t.head_dim;
+        a.scale = t.scale;
+        a.cap = t.cap;
+        const int per_lane = t.dtype == ISO_DTYPE_F32 ? 4 : 8;
+        while ((per_lane << a.lanes_log2) < t.head_dim) ++a.lanes_log2;
+        is_wide = wide(t.q, t.head_dim, t.dtype) && wide(t.k, t.head_dim, t.dtype) && wide(t.v, t.head_dim, t.dtype) &&
+                  wide(t.out, t.head_dim, t.dtype);
+        if (g) {
+            a.grad_out = device_heads(g->grad_out);
+            a.grad_q = device_heads(g->grad_q);
+            a.grad_k = device_heads(g->grad_k);
+            a.grad_v = device_heads(g->grad_v);
+            a.delta = (float *)((char *)workspace + work.delta);
+            a.partials = (float *)((char *)workspace + work.partials);
+            for (const iso_heads_t *x : {&g->grad_out, &g->grad_q, &g->grad_k, &g->grad_v})
+                is_wide = is_wide && wide(*x, t.head_dim, t.dtype);
+        }
+    }
+
+    int forward() {
+        const uint64_t items = n * t.q_heads;
+        // Few rows: the wavefronts of a workgroup share the neighbours of one, so that the GPU has work.
+        const uint64_t sets = 64 >> a.lanes_log2, takes = ((uint64_t)c.s + sets - 1) / sets;
+        a.waves = items < 2048 ? (int)std::clamp<uint64_t>(takes, 1, 16) : 1;
+        if (a.waves > 1) return add_launch(b, by_type<SplitRowKernel>(t.dtype, is_wide), items, 64u * a.waves, a);
+        return add_launch(b, by_type<RowKernel>(t.dtype, is_wide), (items + 3) / 4, 256, a);
+    }
+
+    int backward() {
+        ISO_TRY(add_launch(b, by_type<GradQRowKernel>(t.dtype, is_wide), (n * t.q_heads + 3) / 4, 256, a));
+        ISO_TRY(add_launch(b, by_type<GradKVRowKernel>(t.dtype, is_wide), (n * t.kv_heads + 3) / 4, 256, a));
+        if (!g->grad_bias || !c.s) return ISO_SUCCESS;
+        const uint64_t slots = (uint64_t)t.q_heads * c.s;
+        a.parts = (int)bias_parts(c, t.q_heads);
+        ISO_TRY(add_launch(b, by_type<GradBiasRowKernel>(t.dtype, is_wide), (slots * a.parts + 3) / 4, 256, a));
+        return add_launch(b, sum_parts_by_type(t.dtype), (slots + 15) / 16, 256,
+                          SumPartsArgs{a.partials, g->grad_bias, (uint32_t)slots, (uint32_t)a.parts});
+    }
+
+    BoundOperator &b;
+    const Comm &c;
+    const iso_attention_t &t;
+    const iso_attention_grads_t *g;
+    uint64_t n = 0;
+    BackwardWorkspace work;
+    AttentionArgs a{};
+    bool is_wide = false;
+};
+
+// ---- rotary positions --------------------------------------------------------------
+
+inline int bind_rotary(BoundOperator &b, const Comm *c, const iso_rotary_t &t) {
+    ISO_TRY(check_shape(t.dtype, t.heads, t.heads, t.head_dim));
+    if (t.pairs < 0 || 2 * (int64_t)t.pairs > t.head_dim || (t.pairs && (!t.freqs || !t.axes)) || t.n < 0) return ISO_ERR_ARG;
+    if (t.n > 0x7FFFFFFF) return ISO_ERR_TOO_LARGE;
+    if (!t.n) return ISO_SUCCESS;
+    if (!t.positions && (!c || t.n != c->p)) return ISO_ERR_ARG;
+    const int n_axes = t.positions ? t.n_axes : c->d;
+    for (int j = 0; j < t.pairs; ++j)
+        if (t.axes[j] < 0 || t.axes[j] >= n_axes || !std::isfinite(t.freqs[j])) return ISO_ERR_ARG;
+    Regions r;
+    const bool in_place = t.x.data == t.out.data && t.x.rank_stride == t.out.rank_stride && t.x.head_stride == t.out.head_stride;
+    ISO_TRY(r.heads(t.x, (uint64_t)t.n, t.heads, t.head_dim, t.dtype, false));
+    ISO_TRY(r.heads(t.out, (uint64_t)t.n, t.heads, t.head_dim, t.dtype, true));
+    if (t.positions) ISO_TRY(r.array(t.positions, (uint64_t)t.n * n_axes * 4, 4, false));
+    ISO_TRY(in_place ? r.disjoint(0, 1) : r.disjoint());
+
+    std::vector<unsigned char> table((size_t)t.pairs * 12);
+    for (int j = 0; j < t.pairs; ++j) {
+        const double turns = t.freqs[j] / 6.283185307179586476925286766559;
+        std::memcpy(table.data() + (size_t)j * 8, &turns, 8);
+        std::memcpy(table.data() + (size_t)t.pairs * 8 + (size_t)j * 4, &t.axes[j], 4);
+    }
+    ISO_TRY(upload_table(b, table.data(), table.size()));
+    RotaryArgs a{};
+    a.x = device_heads(t.x);
+    a.out = device_heads(t.out);
+    a.positions = t.positions;
+    a.turns = (const double *)b.dev_table;
+    a.axes = (const int32_t *)((const char *)b.dev_table + (size_t)t.pairs * 8);
+    a.n = (uint32_t)t.n;
+    a.n_axes = n_axes;
+    a.head_dim = t.head_dim;
+    a.pairs = t.pairs;
+    a.interleaved = t.interleaved != 0;
+    a.sign = t.inverse ? -1.f : 1.f;
+    for (int j = 0; c && j < c->d; ++j) {
+        a.dims[j] = c->dims[j];
+        a.inner[j] = (int32_t)c->inner[j];
+    }
+    // a workgroup makes about one angle per lane
+    a.ranks = std::clamp(256 / std::max(1, t.pairs), 1, 8);
+    const int per_lane = t.dtype == ISO_DTYPE_F32 ? 4 : 8;
+    const bool whole = (t.interleaved ? 2 * t.pairs : t.pairs) % per_lane == 0;      // no unit of 16 bytes mixes both kinds
+    const bool is_wide = whole && wide(t.x, t.head_dim, t.dtype) && wide(t.out, t.head_dim, t.dtype);
+    const int E = is_wide ? per_lane : 1;
+    const int units = t.interleaved && is_wide ? t.head_dim / E : (t.head_dim - t.pairs) / E;
+    a.by_pairs = make_fastdiv((uint32_t)std::max(1, t.pairs));
+    a.by_units = make_fastdiv((uint32_t)units);
+    a.by_heads = make_fastdiv((uint32_t)t.heads);
+    return add_launch(b, by_type<RotaryKernel>(t.dtype, is_wide), ((uint64_t)t.n + a.ranks - 1) / a.ranks, 256, a);
+}
+
+}  // namespace iso

@@ -8,7 +8,7 @@ ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libiso.so")
 SOURCES = [os.path.join(HERE, "csrc", "iso_api.hip"), os.path.join(HERE, "csrc", "iso_plan.cpp")]
 HEADERS = [os.path.join(HERE, "csrc", h) for h in ("iso_kernels.hpp", "iso_plan.hpp", "iso_fastdiv.hpp", "iso_bind.hpp",
-                                                      "iso_attention_kernels.hpp", "iso_rotary_kernels.hpp", "iso_operators.hpp")]
+                                                      "iso_attention_kernels.hpp", "iso_attention_tiles.hpp", "iso_tiles.hpp", "iso_rotary_kernels.hpp", "iso_operators.hpp")]
 HEADERS.append(os.path.join(ROOT, "include", "iso.h"))
 
 

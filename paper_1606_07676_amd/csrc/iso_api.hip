@@ -680,6 +680,7 @@ int iso_request_set_graph(iso_request_t req, int enable) {
                 np.func = const_cast<void *>(l.func);
                 np.gridDim = dim3(l.grid);
                 np.blockDim = dim3(l.threads);
+                np.sharedMemBytes = l.lds;
             } else {
                 const iso::Launch &l = req->b.launches[i];
                 const iso::KernelRef k = iso::select_kernel(req->b.info.vector_bytes, l);

@@ -9,15 +9,17 @@
 #include <vector>
 
 #include "iso_attention_kernels.hpp"
+#include "iso_attention_tiles.hpp"
 #include "iso_bind.hpp"
 #include "iso_rotary_kernels.hpp"
+#include "iso_tiles.hpp"
 
 namespace iso {
 
 // One kernel launch of an operator: its arguments are one struct, kept with it.
 struct OperatorLaunch {
     const void *func = nullptr;
-    uint32_t grid = 0, threads = 0;
+    uint32_t grid = 0, threads = 0, lds = 0;
     std::shared_ptr<void> args;
 };
 
@@ -27,16 +29,16 @@ struct BoundOperator {
 };
 
 template <typename Args>
-int add_launch(BoundOperator &b, const void *func, uint64_t grid, uint32_t threads, const Args &args) {
+int add_launch(BoundOperator &b, const void *func, uint64_t grid, uint32_t threads, const Args &args, size_t lds = 0) {
     if (!grid) return ISO_SUCCESS;
     if (grid > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
-    b.launches.push_back({func, (uint32_t)grid, threads, std::make_shared<Args>(args)});
+    b.launches.push_back({func, (uint32_t)grid, threads, (uint32_t)lds, std::make_shared<Args>(args)});
     return ISO_SUCCESS;
 }
 
 inline int enqueue_operator(const OperatorLaunch &l, hipStream_t stream) {
     void *args[1] = {l.args.get()};
-    ISO_HIP_TRY(hipLaunchKernel(l.func, dim3(l.grid), dim3(l.threads), args, 0, stream));
+    ISO_HIP_TRY(hipLaunchKernel(l.func, dim3(l.grid), dim3(l.threads), args, l.lds, stream));
     return ISO_SUCCESS;
 }
 
@@ -152,6 +154,18 @@ inline NeighbourTorus neighbour_torus(const Comm &c, const void *offsets) {
     return t;
 }
 
+// The parts of a request's device table, each on a 16-byte boundary.
+class Table {
+  public:
+    template <typename V> size_t add(const std::vector<V> &part) {
+        const size_t at = (bytes.size() + 15) / 16 * 16;
+        bytes.resize(at + part.size() * sizeof(V));
+        if (!part.empty()) std::memcpy(bytes.data() + at, part.data(), part.size() * sizeof(V));
+        return at;
+    }
+    std::vector<unsigned char> bytes;
+};
+
 inline int upload_table(BoundOperator &b, const void *host, size_t bytes) {
     if (!bytes) return ISO_SUCCESS;
     ISO_HIP_TRY(hipMalloc(&b.dev_table, bytes));
@@ -186,6 +200,36 @@ ISO_KERNEL_BY_TYPE(GradKVRowKernel, attention_grad_kv_row_kernel)
 ISO_KERNEL_BY_TYPE(GradBiasRowKernel, attention_grad_bias_row_kernel)
 ISO_KERNEL_BY_TYPE(RotaryKernel, rotary_kernel)
 #undef ISO_KERNEL_BY_TYPE
+
+template <template <typename, int, bool> class Kernel, typename T>
+const void *tile_by_size(int head_dim, bool segments) {
+    if (head_dim <= 32) return segments ? Kernel<T, 32, true>::func() : Kernel<T, 32, false>::func();
+    if (head_dim <= 64) return segments ? Kernel<T, 64, true>::func() : Kernel<T, 64, false>::func();
+    if (head_dim <= 96) return segments ? Kernel<T, 96, true>::func() : Kernel<T, 96, false>::func();
+    return segments ? Kernel<T, 128, true>::func() : Kernel<T, 128, false>::func();
+}
+template <template <typename, int, bool> class Kernel>
+const void *tile_by_type(int dtype, int head_dim, bool segments) {
+    return dtype == ISO_DTYPE_BF16 ? tile_by_size<Kernel, __bf16>(head_dim, segments) : tile_by_size<Kernel, _Float16>(head_dim, segments);
+}
+#define ISO_TILE_KERNEL(name, kernel)                                                           \
+    template <typename T, int DP, bool SEGMENTS> struct name {                                  \
+        static const void *func() { return (const void *)(kernel<T, DP, SEGMENTS>); }           \
+    };
+ISO_TILE_KERNEL(TileKernel, attention_tile_kernel)
+#undef ISO_TILE_KERNEL
+
+constexpr int kTileMaxHeadDim = 128;
+constexpr size_t kTileMaxLds = 64 << 10;
+inline int tile_head_dim(int head_dim) { return (head_dim + 31) / 32 * 32; }
+inline size_t tile_lds_bytes(int head_dim, int chunks, size_t biases) {
+    switch (tile_head_dim(head_dim)) {
+        case 32: return TileLds<__bf16, 32>::bytes(chunks, biases);
+        case 64: return TileLds<__bf16, 64>::bytes(chunks, biases);
+        case 96: return TileLds<__bf16, 96>::bytes(chunks, biases);
+        default: return TileLds<__bf16, 128>::bytes(chunks, biases);
+    }
+}
 
 inline const void *sum_parts_by_type(int dtype) {
     switch (dtype) {
@@ -235,9 +279,13 @@ class AttentionBinder {
         n = t.rows ? (uint64_t)t.n_rows : (uint64_t)c.p;
         ISO_TRY(check_buffers(workspace, workspace_bytes));
         if (!n) return ISO_SUCCESS;
-        const std::vector<int32_t> offsets = kernel_offsets(c);
-        ISO_TRY(upload_table(b, offsets.data(), offsets.size() * sizeof(int32_t)));
+        Table table;
+        table.add(kernel_offsets(c));
+        choose_width();
+        const bool tiles = !g && takes_tiles(table);
+        ISO_TRY(upload_table(b, table.bytes.data(), table.bytes.size()));
         fill_args(workspace);
+        if (tiles) return forward_tiles();
         return g ? backward() : forward();
     }
 
@@ -289,8 +337,6 @@ class AttentionBinder {
         a.cap = t.cap;
         const int per_lane = t.dtype == ISO_DTYPE_F32 ? 4 : 8;
         while ((per_lane << a.lanes_log2) < t.head_dim) ++a.lanes_log2;
-        is_wide = wide(t.q, t.head_dim, t.dtype) && wide(t.k, t.head_dim, t.dtype) && wide(t.v, t.head_dim, t.dtype) &&
-                  wide(t.out, t.head_dim, t.dtype);
         if (g) {
             a.grad_out = device_heads(g->grad_out);
             a.grad_q = device_heads(g->grad_q);
@@ -298,9 +344,51 @@ class AttentionBinder {
             a.grad_v = device_heads(g->grad_v);
             a.delta = (float *)((char *)workspace + work.delta);
             a.partials = (float *)((char *)workspace + work.partials);
-            for (const iso_heads_t *x : {&g->grad_out, &g->grad_q, &g->grad_k, &g->grad_v})
-                is_wide = is_wide && wide(*x, t.head_dim, t.dtype);
         }
+    }
+
+    void choose_width() {
+        is_wide = true;
+        for (const iso_heads_t *x : {&t.q, &t.k, &t.v, &t.out}) is_wide = is_wide && wide(*x, t.head_dim, t.dtype);
+        if (!g) return;
+        for (const iso_heads_t *x : {&g->grad_out, &g->grad_q, &g->grad_k, &g->grad_v})
+            is_wide = is_wide && wide(*x, t.head_dim, t.dtype);
+    }
+
+    bool takes_tiles(Table &table) {
+        if (t.rows || t.dtype == ISO_DTYPE_F32 || !is_wide || t.head_dim > kTileMaxHeadDim) return false;
+        const int group = t.q_heads / t.kv_heads;
+        int heads = 1;
+        while (heads < 8 && group % (2 * heads) == 0) heads *= 2;
+        TilePlan p;
+        if (!build_tile_plan(c, heads, false, p)) return false;
+        lds = tile_lds_bytes(t.head_dim, p.chunks, t.bias ? (size_t)heads * (c.s + 1) : 0);
+        if (lds > kTileMaxLds || p.blocks * 256.0 > 12.0 * kTileColumns * c.s) return false;
+        at_columns = table.add(p.column_at);
+        at_rows = table.add(p.row_at);
+        at_active = table.add(p.active);
+        at_index = table.add(p.index);
+        plan = std::move(p);
+        return true;
+    }
+
+    int forward_tiles() {
+        TileArgs ta{};
+        ta.a = a;
+        for (int j = 0; j < c.d; ++j) ta.tile[j] = plan.tile[j], ta.tiles[j] = plan.tiles[j];
+        ta.n_tiles = (uint32_t)plan.n_tiles;
+        ta.heads = plan.heads;
+        ta.parts = a.group / plan.heads;
+        ta.chunks = plan.chunks;
+        const char *base = (const char *)b.dev_table;
+        ta.column_at = (const int32_t *)(base + at_columns);
+        ta.row_at = (const int32_t *)(base + at_rows);
+        ta.active = (const uint32_t *)(base + at_active);
+        ta.index = (const uint16_t *)(base + at_index);
+        const uint64_t work = (uint64_t)plan.n_tiles * t.kv_heads * ta.parts;
+        if (work > 0x7FFFFFF0ull) return ISO_ERR_TOO_LARGE;
+        ta.per_xcd = (uint32_t)((work + 7) / 8);
+        return add_launch(b, tile_by_type<TileKernel>(t.dtype, t.head_dim, t.segments || c.mesh), (uint64_t)ta.per_xcd * 8, 256, ta, lds);
     }
 
     int forward() {
@@ -331,6 +419,8 @@ class AttentionBinder {
     BackwardWorkspace work;
     AttentionArgs a{};
     bool is_wide = false;
+    TilePlan plan;
+    size_t lds = 0, at_columns = 0, at_rows = 0, at_active = 0, at_index = 0;
 };
 
 // ---- rotary positions --------------------------------------------------------------

@@ -1,0 +1,168 @@
+// Tiles of ranks for the matrix kernels of attention: which keys a tile of the torus needs, in which order, and which
+// (rank, key) pairs of a tile are neighbours.  The neighbourhood is the same at every rank, so one table serves all tiles.
+// Pure host code.
+#pragma once
+
+#include <algorithm>
+#include <array>
+#include <cmath>
+#include <cstdint>
+#include <unordered_map>
+#include <vector>
+
+#include "iso_plan.hpp"
+
+namespace iso {
+
+constexpr int kTileWaves = 4;              // wavefronts of a workgroup, 16 columns (rank, head) each
+constexpr int kTileColumns = 16 * kTileWaves;
+constexpr int kChunkRows = 64;             // rows (keys) that a workgroup holds in LDS at a time
+constexpr int kTileMaxRows = 2048;         // rows of a tile
+
+struct TilePlan {
+    int heads = 1;                         // columns of one rank: column c is rank c / heads, head c % heads
+    std::array<int32_t, ISO_MAX_DIMS> tile{}, tiles{};      // ranks per tile and tiles, by dimension
+    int64_t n_tiles = 1;
+    int rows = 0, chunks = 0;              // rows in use; chunks of kChunkRows
+    int blocks = 0;                        // 16 x 16 blocks of pairs that hold a neighbour
+    std::vector<int32_t> column_at;        // [kTileColumns / heads][d]: position in the tile
+    std::vector<int32_t> row_at;           // [chunks * kChunkRows][d]: position relative to the tile's first rank
+    std::vector<uint32_t> active;          // [chunks]: bit 4 * wave + group: that block holds a neighbour
+    std::vector<uint16_t> index;           // [chunks * 4][kTileWaves][64][4]: neighbour of (lane's column, row 4 * (lane / 16) + r)
+                                           // of the 16 rows of a group, s where it is none
+};
+
+// back = false: columns are ranks, rows their sources R (-) C^i.  back = true: columns are sources, rows the ranks that read
+// them.  False where no table of that form exists (neighbours too many, or too far apart).
+inline bool build_tile_plan(const Comm &c, int heads, bool back, TilePlan &out) {
+    const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
+    if (c.s < 1 || c.s > 65534) return false;
+    // offsets as signed steps from a column to its row; what no rank of a mesh can reach is left out
+    std::vector<std::array<int32_t, ISO_MAX_DIMS>> step((size_t)c.s);
+    std::vector<uint8_t> used((size_t)c.s, 1);
+    std::array<int32_t, ISO_MAX_DIMS> low{}, high{}, wave{};
+    bool any = false;
+    for (int i = 0; i < c.s; ++i) {
+        for (int j = 0; j < d; ++j) {
+            const int64_t n = c.dims[j];
+            int64_t x = c.c(i, j);
+            if (c.periodic[j]) x = x > n / 2 ? x - n : x;
+            else if (x >= n || x <= -n) used[i] = 0;
+            step[i][j] = used[i] ? (int32_t)(back ? x : -x) : 0;
+        }
+        if (!used[i]) continue;
+        for (int j = 0; j < d; ++j) {
+            low[j] = any ? std::min(low[j], step[i][j]) : step[i][j];
+            high[j] = any ? std::max(high[j], step[i][j]) : step[i][j];
+        }
+        any = true;
+    }
+    // The tile: dimensions are doubled where that keeps the rows of all tiles together fewest; the ranks of a wavefront the same way.
+    TilePlan p;
+    p.heads = heads;
+    const auto grow = [&](std::array<int32_t, ISO_MAX_DIMS> &t, int total, const std::array<int32_t, ISO_MAX_DIMS> *limit) {
+        t.fill(1);
+        for (int have = 1; have < total; have *= 2) {
+            int best = -1;
+            double best_cost = 0;
+            for (int j = d - 1; j >= 0; --j) {
+                if (limit && t[j] * 2 > (*limit)[j]) continue;
+                const double n = c.dims[j], e = (double)high[j] - low[j], w = t[j];
+                const auto cost = [&](double x) { return (limit ? n / x : std::ceil(n / x)) * (x + e); };
+                const double gain = cost(2 * w) / cost(w);
+                if (best < 0 || gain < best_cost) best = j, best_cost = gain;
+            }
+            t[best] *= 2;
+        }
+    };
+    grow(p.tile, ranks, nullptr);
+    grow(wave, per_wave, &p.tile);
+    for (int j = 0; j < d; ++j) {
+        p.tiles[j] = (c.dims[j] + p.tile[j] - 1) / p.tile[j];
+        p.n_tiles *= p.tiles[j];
+    }
+    if (p.n_tiles > 0x7FFFFFFF) return false;
+    // columns: the wavefronts' boxes one after the other, the last dimension fastest inside and outside
+    p.column_at.resize((size_t)ranks * d);
+    for (int r = 0; r < ranks; ++r) {
+        int inside = r % per_wave, box = r / per_wave;
+        for (int j = d - 1; j >= 0; --j) {
+            const int boxes = p.tile[j] / wave[j];
+            p.column_at[(size_t)r * d + j] = box % boxes * wave[j] + inside % wave[j];
+            inside /= wave[j];
+            box /= boxes;
+        }
+    }
+    // rows by position: a number in the box that all positions span
+    std::array<int64_t, ISO_MAX_DIMS> span{};
+    int64_t volume = 1;
+    for (int j = 0; j < d; ++j) {
+        span[j] = (int64_t)high[j] - low[j] + p.tile[j];
+        if (span[j] > (int64_t(1) << 40) / volume) return false;
+        volume *= span[j];
+    }
+    struct Row {
+        std::array<int32_t, ISO_MAX_DIMS> at;
+        int copy;                          // a pair that is listed twice finds its second neighbour in a second row
+    };
+    std::vector<Row> rows;
+    std::unordered_map<int64_t, std::vector<int>> by_place;
+    std::unordered_map<int64_t, int> taken;                 // rank and row -> neighbour
+    for (int r = 0; r < ranks; ++r)
+        for (int i = 0; i < c.s; ++i) {
+            if (!used[i]) continue;
+            Row row;
+            row.at.fill(0);
+            int64_t place = 0;
+            for (int j = 0; j < d; ++j) {
+                row.at[j] = p.column_at[(size_t)r * d + j] + step[i][j];
+                place = place * span[j] + (row.at[j] - low[j]);
+            }
+            std::vector<int> &copies = by_place[place];
+            row.copy = 0;
+            while ((size_t)row.copy < copies.size() && taken.count((int64_t)r << 32 | copies[row.copy])) ++row.copy;
+            if ((size_t)row.copy == copies.size()) {
+                if (rows.size() == (size_t)kTileMaxRows) return false;
+                copies.push_back((int)rows.size());
+                rows.push_back(row);
+            }
+            taken[(int64_t)r << 32 | copies[row.copy]] = i;
+        }
+    // order: boxes of a wavefront's shape, so that the rows of 16 that a wavefront has no neighbour in are many
+    std::vector<int> order(rows.size());
+    for (size_t u = 0; u < order.size(); ++u) order[u] = (int)u;
+    std::sort(order.begin(), order.end(), [&](int a, int b) {
+        for (int pass = 0; pass < 2; ++pass)
+            for (int j = 0; j < d; ++j) {
+                const int x = rows[a].at[j] - low[j], y = rows[b].at[j] - low[j];
+                const int u = pass ? x % wave[j] : x / wave[j], v = pass ? y % wave[j] : y / wave[j];
+                if (u != v) return u < v;
+            }
+        return rows[a].copy < rows[b].copy;
+    });
+    p.rows = (int)rows.size();
+    p.chunks = (p.rows + kChunkRows - 1) / kChunkRows;
+    p.row_at.assign((size_t)p.chunks * kChunkRows * d, 0);
+    p.active.assign((size_t)p.chunks, 0);
+    p.index.assign((size_t)p.chunks * 4 * kTileWaves * 64 * 4, (uint16_t)c.s);
+    std::vector<int> rank_of((size_t)p.rows);
+    for (int u = 0; u < p.rows; ++u) {
+        rank_of[order[u]] = u;
+        for (int j = 0; j < d; ++j) p.row_at[(size_t)u * d + j] = rows[order[u]].at[j];
+    }
+    for (const auto &[pair, i] : taken) {
+        const int r = (int)(pair >> 32), u = rank_of[(size_t)(pair & 0xFFFFFFFF)];
+        const int group = u / 16, lane_row = u % 16;
+        for (int h = 0; h < heads; ++h) {
+            const int column = r * heads + h, w = column / 16;
+            const int lane = lane_row / 4 * 16 + column % 16;
+            p.index[(((size_t)group * kTileWaves + w) * 64 + lane) * 4 + lane_row % 4] = (uint16_t)i;
+            p.active[group / 4] |= 1u << (4 * w + group % 4);
+        }
+    }
+    for (uint32_t a : p.active) p.blocks += __builtin_popcount(a);
+    out = std::move(p);
+    return true;
+}
+
+}  // namespace iso

@@ -469,25 +469,27 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
     if (lane == 0) a.partials[(uint64_t)part * slots + slot] = sum;
 }
 
-// The parts of the bias's gradient added up in their order: 16 slots of a workgroup, 16 lanes over the parts of each.
+// The parts of the bias's gradient added up, always in the same order: 16 slots of a workgroup, 64 lanes over the parts of each.
 struct SumPartsArgs {
     const float *partials;
     void *out;
     uint32_t slots, parts;
 };
 template <typename T>
-__global__ __launch_bounds__(256) void sum_parts_kernel(const SumPartsArgs a) {
-    __shared__ float sums[16][17];
+__global__ __launch_bounds__(1024) void sum_parts_kernel(const SumPartsArgs a) {
+    __shared__ float sums[64][17];
     const uint32_t col = threadIdx.x & 15, row = threadIdx.x >> 4, slot = blockIdx.x * 16 + col;
     float sum = 0.f;
-    if (slot < a.slots)
-        for (uint32_t part = row; part < a.parts; part += 16) sum += a.partials[(uint64_t)part * a.slots + slot];
-    sums[row][col] = sum;
-    __syncthreads();
-    if (row == 0 && slot < a.slots) {
-        for (int r = 1; r < 16; ++r) sum += sums[r][col];
-        ((T *)a.out)[slot] = (T)sum;
+    if (slot < a.slots) {
+#pragma unroll 4
+        for (uint32_t part = row; part < a.parts; part += 64) sum += a.partials[(uint64_t)part * a.slots + slot];
     }
+    sums[row][col] = sum;
+    for (uint32_t half = 32; half; half /= 2) {
+        __syncthreads();
+        if (row < half) sums[row][col] += sums[row + half][col];
+    }
+    if (row == 0 && slot < a.slots) ((T *)a.out)[slot] = (T)sums[0][col];
 }
 
 }  // namespace iso

@@ -25,6 +25,9 @@ struct TileArgs {
     const int32_t *column_at, *row_at;
     const uint32_t *active;
     const uint16_t *index;
+    const uint32_t *slots_of;              // the bias's gradient, or null: see TilePlan
+    const TilePlan::Slot *slots;
+    const uint16_t *pairs;
 };
 
 template <typename T> struct Matrix;
@@ -235,7 +238,6 @@ __device__ __forceinline__ bool store_column(const Heads &h, int64_t rank, int h
 // A column is made again row by row where it is not finite: an infinity or NaN in a row that is a neighbour of another column
 // of the wavefront, and has weight 0 here, makes 0 * inf in the matrix product.
 template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &&redo) {
-    const int lane = threadIdx.x & 63;
     uint64_t columns = __ballot(bad);
     columns = (columns | columns >> 16 | columns >> 32 | columns >> 48) & 0xFFFF;
     while (columns) {
@@ -243,7 +245,6 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
         columns &= columns - 1;
         redo(column);
     }
-    (void)lane;
 }
 
 template <typename T, int DP, bool SEGMENTS>
@@ -337,6 +338,211 @@ __global__ __launch_bounds__(256) void attention_tile_kernel(const TileArgs t) {
         RowState<8> st;
         attend_row<T, true>(a, r, r, h, 0, 1, coords[wave], st);
         write_row<T, true, false>(a, r, h, st);       // lse does not depend on the values
+        __builtin_amdgcn_wave_barrier();
+    });
+}
+
+// ---- backward ------------------------------------------------------------------------
+//
+// Weights are made again from lse.  grad_q takes the forward pass's tiles: S and dP = V grad_out^T from the staged keys and
+// values, grad_q^T += K^T da.  grad_k and grad_v take tiles of keys against the ranks that read them, with queries and
+// grad_out staged: S and dP with the roles changed, grad_k^T += Q^T da, grad_v^T += grad_out^T P, head by head of the group.
+// Both gather: a tile's results are written once, by one workgroup, in one order.
+
+template <typename T, int DP, bool SEGMENTS>
+__global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileArgs t) {
+    typedef typename Matrix<T>::f4 f4;
+    extern __shared__ __align__(16) unsigned char lds_bytes[];
+    __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
+    const AttentionArgs &a = t.a;
+    const TileWork work = tile_work(t, a.kv_heads);
+    if (!work.any) return;
+    TileLds<T, DP> lds(lds_bytes, t.chunks);
+    tile_rows<T, DP>(t, work.tile, origin, lds);
+
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+    const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
+    const int s = a.torus.s, slots = t.heads * s;
+    if (a.bias)
+        for (int i = threadIdx.x; i < slots; i += 256)
+            lds.bias[i / s * (s + 1) + i % s] = (float)((const T *)a.bias)[(int64_t)first_head * s + i];
+    // behind the biases: dx of the wavefront's blocks of a chunk, and the sums of its slots over the chunks
+    float *dx_at = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4 + wave * 1024;
+    float *sums = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4 + kTileWaves * 1024 + wave * slots;
+    if (t.slots_of)
+        for (int i = lane; i < slots; i += 64) sums[i] = 0.f;
+    const int64_t rank = rank_at(t, origin, t.column_at + column / t.heads * a.torus.d, true);
+    int32_t own = kNoColumn;
+    if (rank >= 0) own = a.segments ? a.segments[rank] : 0;
+    if (own < 0) own = kNoColumn;
+    typename Matrix<T>::x8 q[DP / 32], g_out[DP / 32];
+    load_column<T, DP>(a.q, rank, head, a.head_dim, q);
+    load_column<T, DP>(a.grad_out, rank, head, a.head_dim, g_out);
+    float delta = 0.f;
+    {
+        typename Matrix<T>::x8 out[DP / 32];
+        load_column<T, DP>(a.out, rank, head, a.head_dim, out);
+#pragma unroll
+        for (int k = 0; k < DP / 32; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)g_out[k][e], (float)out[k][e], delta);
+        delta = column_sum(delta);
+    }
+    const float lse = rank >= 0 ? finite_floor(a.lse[rank * a.q_heads + head]) : 0.f;
+    if (rank >= 0 && lane < 16) a.delta[rank * a.q_heads + head] = delta;
+    __syncthreads();
+
+    const T *k0 = (const T *)a.k.data + work.key_head * a.k.head_stride, *v0 = (const T *)a.v.data + work.key_head * a.v.head_stride;
+    const float *bias = lds.bias + column % t.heads * (s + 1);
+    f4 acc[DP / 16] = {};
+    Staged<T, DP> next;
+    next.load(k0, a.k.rank_stride, v0, a.v.rank_stride, lds.rank, a.head_dim);
+    for (int chunk = 0; chunk < t.chunks; ++chunk) {
+        __syncthreads();
+        next.store(lds);
+        __syncthreads();
+        if (chunk + 1 < t.chunks)
+            next.load(k0, a.k.rank_stride, v0, a.v.rank_stride, lds.rank + (chunk + 1) * kChunkRows, a.head_dim);
+        const uint32_t active = __builtin_amdgcn_readfirstlane(t.active[chunk] >> (4 * wave) & 15);
+#pragma unroll
+        for (int pair = 0; pair < 2; ++pair) {
+            if (!(active >> (2 * pair) & 3)) continue;
+            f4 da[2] = {};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int g = 2 * pair + half;
+                if (!(active >> g & 1)) continue;
+                const uint2 who = *(const uint2 *)(t.index + (((int64_t)(chunk * 4 + g) * kTileWaves + wave) * 64 + lane) * 4);
+                const f4 dot = rows_times_columns<T, DP>(lds.first + g * 16 * lds.kStride, q);
+                const f4 dp = rows_times_columns<T, DP>(lds.second + g * 16 * lds.kStride, g_out);
+                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * kChunkRows + g * 16 + lane / 16 * 4) : int4{};
+                f4 dx;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = (r < 2 ? who.x : who.y) >> (r % 2 * 16) & 0xFFFF;
+                    const bool counts = i != s && (!SEGMENTS || (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                    const PairGradient pg = pair_gradient(dot[r], a.bias ? bias[i] : 0.f, lse, dp[r], delta, a.scale, a.cap);
+                    dx[r] = counts ? pg.dx : 0.f;
+                    da[half][r] = counts ? pg.da : 0.f;
+                }
+                if (t.slots_of) *(f4 *)(dx_at + (g * 64 + lane) * 4) = rank >= 0 ? dx : f4{0.f, 0.f, 0.f, 0.f};
+            }
+            add_weighted_rows<T, DP>(lds.first + pair * 32 * lds.kStride, as_weights<T>(da[0], da[1]), acc);
+        }
+        if (t.slots_of) {
+            // every lane adds up the pairs of one slot: blocks that hold none of its pairs are not read
+            __builtin_amdgcn_wave_barrier();
+            const uint32_t begin = t.slots_of[chunk * kTileWaves + wave], end = t.slots_of[chunk * kTileWaves + wave + 1];
+            for (uint32_t j = begin + lane; j < end; j += 64) {
+                const TilePlan::Slot slot = t.slots[j];
+                float sum = 0.f;
+                for (uint32_t n = 0; n < slot.count; ++n) sum += dx_at[t.pairs[slot.first + n]];
+                sums[slot.slot] += sum;
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    const bool fine = store_column<T, DP>(a.grad_q, rank, head, a.head_dim, acc, a.scale);
+    redo_columns(rank >= 0 && !fine, [&](int c) {
+        const uint32_t r = (uint32_t)__shfl((int)rank, c);
+        const int h = __shfl(head, c);
+        const float row_delta = __shfl(delta, c);
+        store_coordinates(a.torus, r, lane, coords[wave]);
+        __builtin_amdgcn_wave_barrier();
+        grad_q_row<T, true>(a, r, h, row_delta, coords[wave]);
+        __builtin_amdgcn_wave_barrier();
+    });
+    if (t.slots_of) {
+        __syncthreads();
+        const float *all = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4 + kTileWaves * 1024;
+        float *out = a.partials + (uint64_t)work.tile * a.q_heads * s + (int64_t)first_head * s;
+        for (int i = threadIdx.x; i < slots; i += 256) out[i] = all[i] + all[slots + i] + all[2 * slots + i] + all[3 * slots + i];
+    }
+}
+
+template <typename T, int DP, bool SEGMENTS>
+__global__ __launch_bounds__(256) void attention_grad_kv_tile_kernel(const TileArgs t) {
+    typedef typename Matrix<T>::f4 f4;
+    extern __shared__ __align__(16) unsigned char lds_bytes[];
+    __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
+    __shared__ __align__(16) float row_lse[kChunkRows], row_delta[kChunkRows];
+    const AttentionArgs &a = t.a;
+    const TileWork work = tile_work(t, a.kv_heads);
+    if (!work.any) return;
+    TileLds<T, DP> lds(lds_bytes, t.chunks);
+    tile_rows<T, DP>(t, work.tile, origin, lds);
+
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+    const int first_head = work.key_head * a.group, s = a.torus.s;
+    if (a.bias)
+        for (int i = threadIdx.x; i < a.group * s; i += 256)
+            lds.bias[i / s * (s + 1) + i % s] = (float)((const T *)a.bias)[(int64_t)first_head * s + i];
+    const int64_t rank = rank_at(t, origin, t.column_at + column * a.torus.d, true);
+    int32_t own = kNoColumn;
+    if (rank >= 0) own = a.segments ? a.segments[rank] : 0;
+    if (own < 0) own = kNoColumn;
+    typename Matrix<T>::x8 k[DP / 32], v[DP / 32];
+    load_column<T, DP>(a.k, rank, work.key_head, a.head_dim, k);
+    load_column<T, DP>(a.v, rank, work.key_head, a.head_dim, v);
+    __syncthreads();
+
+    f4 dk[DP / 16] = {}, dv[DP / 16] = {};
+    Staged<T, DP> next;
+    float next_lse = 0.f, next_delta = 0.f;
+    const auto fetch = [&](int step) {
+        const int h = first_head + step / t.chunks, chunk = step % t.chunks;
+        next.load((const T *)a.q.data + h * a.q.head_stride, a.q.rank_stride, (const T *)a.grad_out.data + h * a.grad_out.head_stride,
+                  a.grad_out.rank_stride, lds.rank + chunk * kChunkRows, a.head_dim);
+        if (threadIdx.x < kChunkRows) {
+            const int32_t r = lds.rank[chunk * kChunkRows + threadIdx.x];
+            next_lse = r >= 0 ? finite_floor(a.lse[(int64_t)r * a.q_heads + h]) : 0.f;
+            next_delta = r >= 0 ? a.delta[(int64_t)r * a.q_heads + h] : 0.f;
+        }
+    };
+    const int steps = a.group * t.chunks;
+    fetch(0);
+    for (int step = 0; step < steps; ++step) {
+        const int chunk = step % t.chunks;
+        const float *bias = lds.bias + step / t.chunks * (s + 1);
+        __syncthreads();
+        next.store(lds);
+        if (threadIdx.x < kChunkRows) row_lse[threadIdx.x] = next_lse, row_delta[threadIdx.x] = next_delta;
+        __syncthreads();
+        if (step + 1 < steps) fetch(step + 1);
+        const uint32_t active = __builtin_amdgcn_readfirstlane(t.active[chunk] >> (4 * wave) & 15);
+#pragma unroll
+        for (int pair = 0; pair < 2; ++pair) {
+            if (!(active >> (2 * pair) & 3)) continue;
+            f4 p[2] = {}, da[2] = {};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int g = 2 * pair + half;
+                if (!(active >> g & 1)) continue;
+                const uint2 who = *(const uint2 *)(t.index + (((int64_t)(chunk * 4 + g) * kTileWaves + wave) * 64 + lane) * 4);
+                const f4 dot = rows_times_columns<T, DP>(lds.first + g * 16 * lds.kStride, k);
+                const f4 dp = rows_times_columns<T, DP>(lds.second + g * 16 * lds.kStride, v);
+                const f4 lse = *(const f4 *)(row_lse + g * 16 + lane / 16 * 4), delta = *(const f4 *)(row_delta + g * 16 + lane / 16 * 4);
+                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * kChunkRows + g * 16 + lane / 16 * 4) : int4{};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = (r < 2 ? who.x : who.y) >> (r % 2 * 16) & 0xFFFF;
+                    const bool counts = i != s && (!SEGMENTS || (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                    const PairGradient pg = pair_gradient(dot[r], a.bias ? bias[i] : 0.f, lse[r], dp[r], delta[r], a.scale, a.cap);
+                    p[half][r] = counts ? pg.p : 0.f;
+                    da[half][r] = counts ? pg.da : 0.f;
+                }
+            }
+            add_weighted_rows<T, DP>(lds.second + pair * 32 * lds.kStride, as_weights<T>(p[0], p[1]), dv);
+            add_weighted_rows<T, DP>(lds.first + pair * 32 * lds.kStride, as_weights<T>(da[0], da[1]), dk);
+        }
+    }
+    const bool fine_v = store_column<T, DP>(a.grad_v, rank, work.key_head, a.head_dim, dv, 1.f);
+    const bool fine_k = store_column<T, DP>(a.grad_k, rank, work.key_head, a.head_dim, dk, a.scale);
+    redo_columns(rank >= 0 && !(fine_v && fine_k), [&](int c) {
+        const uint32_t r = (uint32_t)__shfl((int)rank, c);
+        store_coordinates(a.torus, r, lane, coords[wave]);
+        __builtin_amdgcn_wave_barrier();
+        grad_kv_row<T, true>(a, r, work.key_head, coords[wave]);
         __builtin_amdgcn_wave_barrier();
     });
 }

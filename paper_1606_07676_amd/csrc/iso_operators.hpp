@@ -217,6 +217,8 @@ const void *tile_by_type(int dtype, int head_dim, bool segments) {
         static const void *func() { return (const void *)(kernel<T, DP, SEGMENTS>); }           \
     };
 ISO_TILE_KERNEL(TileKernel, attention_tile_kernel)
+ISO_TILE_KERNEL(GradQTileKernel, attention_grad_q_tile_kernel)
+ISO_TILE_KERNEL(GradKVTileKernel, attention_grad_kv_tile_kernel)
 #undef ISO_TILE_KERNEL
 
 constexpr int kTileMaxHeadDim = 128;
@@ -248,13 +250,19 @@ inline uint64_t bias_parts(const Comm &c, int q_heads) {
 struct BackwardWorkspace {
     uint64_t delta = 0, partials = 0, bytes = 0;                 // offsets
 };
-inline int backward_workspace(const Comm &c, int q_heads, bool bias, BackwardWorkspace &w) {
+inline int tile_heads(int group) {             // q heads of a rank that one tile of columns takes together
+    int heads = 1;
+    while (heads < 8 && group % (2 * heads) == 0) heads *= 2;
+    return heads;
+}
+inline int backward_workspace(const Comm &c, int q_heads, int kv_heads, bool bias, BackwardWorkspace &w) {
     const uint64_t rows = (uint64_t)c.p * q_heads;               // below 2^47
     w.partials = (rows * 4 + 255) / 256 * 256;
     w.bytes = w.partials;
     if (bias) {
         if ((uint64_t)q_heads * c.s > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
-        w.bytes += bias_parts(c, q_heads) * q_heads * c.s * 4;
+        const uint64_t parts = std::max<uint64_t>(bias_parts(c, q_heads), (uint64_t)tile_shape(c, tile_heads(q_heads / kv_heads)).n_tiles);
+        w.bytes += parts * q_heads * c.s * 4;
     }
     return ISO_SUCCESS;
 }
@@ -282,10 +290,17 @@ class AttentionBinder {
         Table table;
         table.add(kernel_offsets(c));
         choose_width();
-        const bool tiles = !g && takes_tiles(table);
+        const int group = t.q_heads / t.kv_heads, heads = tile_heads(group);
+        const size_t biases = t.bias ? (size_t)heads * (c.s + 1) : 0;
+        if (!g) {
+            forward_side.take(*this, table, heads, false, false, biases);
+        } else {
+            const bool sums = g->grad_bias && c.s;                 // dx of the blocks of a chunk, and the slots of every wavefront
+            forward_side.take(*this, table, heads, false, sums, biases + 3 + (sums ? kTileWaves * (1024 + (size_t)heads * c.s) : 0));
+            backward_side.take(*this, table, 1, true, false, t.bias ? (size_t)group * (c.s + 1) : 0);
+        }
         ISO_TRY(upload_table(b, table.bytes.data(), table.bytes.size()));
         fill_args(workspace);
-        if (tiles) return forward_tiles();
         return g ? backward() : forward();
     }
 
@@ -310,7 +325,7 @@ class AttentionBinder {
             ISO_TRY(r.heads(g->grad_v, n, nk, D, dt, true));
             if (g->grad_bias && !t.bias && c.s) return ISO_ERR_ARG;
             if (g->grad_bias) ISO_TRY(r.array(g->grad_bias, slots * size, size, true));
-            ISO_TRY(backward_workspace(c, nq, g->grad_bias != nullptr, work));
+            ISO_TRY(backward_workspace(c, nq, nk, g->grad_bias != nullptr, work));
             if (!workspace || workspace_bytes < work.bytes) return ISO_ERR_WORKSPACE;
             ISO_TRY(r.array(workspace, work.bytes, 4, true));
         }
@@ -355,43 +370,59 @@ class AttentionBinder {
             is_wide = is_wide && wide(*x, t.head_dim, t.dtype);
     }
 
-    bool takes_tiles(Table &table) {
-        if (t.rows || t.dtype == ISO_DTYPE_F32 || !is_wide || t.head_dim > kTileMaxHeadDim) return false;
-        const int group = t.q_heads / t.kv_heads;
-        int heads = 1;
-        while (heads < 8 && group % (2 * heads) == 0) heads *= 2;
-        TilePlan p;
-        if (!build_tile_plan(c, heads, false, p)) return false;
-        lds = tile_lds_bytes(t.head_dim, p.chunks, t.bias ? (size_t)heads * (c.s + 1) : 0);
-        if (lds > kTileMaxLds || p.blocks * 256.0 > 12.0 * kTileColumns * c.s) return false;
-        at_columns = table.add(p.column_at);
-        at_rows = table.add(p.row_at);
-        at_active = table.add(p.active);
-        at_index = table.add(p.index);
-        plan = std::move(p);
-        return true;
-    }
+    // The tiles of one direction, where there are any.
+    struct Side {
+        bool tiles = false;
+        TilePlan plan;
+        size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots_of = 0, slots = 0, pairs = 0;
 
-    int forward_tiles() {
+        void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
+            if (o.t.rows || o.t.dtype == ISO_DTYPE_F32 || !o.is_wide || o.t.head_dim > kTileMaxHeadDim) return;
+            if (!build_tile_plan(o.c, heads, back, sums, plan)) return;
+            lds = tile_lds_bytes(o.t.head_dim, plan.chunks, floats);
+            if (lds > kTileMaxLds || plan.blocks * 256.0 > 12.0 * kTileColumns * o.c.s) return;
+            columns = table.add(plan.column_at);
+            rows = table.add(plan.row_at);
+            active = table.add(plan.active);
+            index = table.add(plan.index);
+            if (sums) {
+                slots_of = table.add(plan.slots_of);
+                slots = table.add(plan.slots);
+                pairs = table.add(plan.pairs);
+            }
+            tiles = true;
+        }
+    };
+
+    int add_tiles(const Side &side, const void *func, int parts) {
+        const TilePlan &p = side.plan;
         TileArgs ta{};
         ta.a = a;
-        for (int j = 0; j < c.d; ++j) ta.tile[j] = plan.tile[j], ta.tiles[j] = plan.tiles[j];
-        ta.n_tiles = (uint32_t)plan.n_tiles;
-        ta.heads = plan.heads;
-        ta.parts = a.group / plan.heads;
-        ta.chunks = plan.chunks;
+        for (int j = 0; j < c.d; ++j) ta.tile[j] = p.tile[j], ta.tiles[j] = p.tiles[j];
+        ta.n_tiles = (uint32_t)p.n_tiles;
+        ta.heads = p.heads;
+        ta.parts = parts;
+        ta.chunks = p.chunks;
         const char *base = (const char *)b.dev_table;
-        ta.column_at = (const int32_t *)(base + at_columns);
-        ta.row_at = (const int32_t *)(base + at_rows);
-        ta.active = (const uint32_t *)(base + at_active);
-        ta.index = (const uint16_t *)(base + at_index);
-        const uint64_t work = (uint64_t)plan.n_tiles * t.kv_heads * ta.parts;
+        ta.column_at = (const int32_t *)(base + side.columns);
+        ta.row_at = (const int32_t *)(base + side.rows);
+        ta.active = (const uint32_t *)(base + side.active);
+        ta.index = (const uint16_t *)(base + side.index);
+        if (!p.slots_of.empty()) {
+            ta.slots_of = (const uint32_t *)(base + side.slots_of);
+            ta.slots = (const TilePlan::Slot *)(base + side.slots);
+            ta.pairs = (const uint16_t *)(base + side.pairs);
+        }
+        const uint64_t work = (uint64_t)p.n_tiles * t.kv_heads * parts;
         if (work > 0x7FFFFFF0ull) return ISO_ERR_TOO_LARGE;
         ta.per_xcd = (uint32_t)((work + 7) / 8);
-        return add_launch(b, tile_by_type<TileKernel>(t.dtype, t.head_dim, t.segments || c.mesh), (uint64_t)ta.per_xcd * 8, 256, ta, lds);
+        return add_launch(b, func, (uint64_t)ta.per_xcd * 8, 256, ta, side.lds);
     }
 
     int forward() {
+        const bool segments = t.segments || c.mesh;
+        if (forward_side.tiles)
+            return add_tiles(forward_side, tile_by_type<TileKernel>(t.dtype, t.head_dim, segments), a.group / forward_side.plan.heads);
         const uint64_t items = n * t.q_heads;
         // Few rows: the wavefronts of a workgroup share the neighbours of one, so that the GPU has work.
         const uint64_t sets = 64 >> a.lanes_log2, takes = ((uint64_t)c.s + sets - 1) / sets;
@@ -401,13 +432,21 @@ class AttentionBinder {
     }
 
     int backward() {
-        ISO_TRY(add_launch(b, by_type<GradQRowKernel>(t.dtype, is_wide), (n * t.q_heads + 3) / 4, 256, a));
-        ISO_TRY(add_launch(b, by_type<GradKVRowKernel>(t.dtype, is_wide), (n * t.kv_heads + 3) / 4, 256, a));
-        if (!g->grad_bias || !c.s) return ISO_SUCCESS;
+        const bool segments = t.segments || c.mesh, bias = g->grad_bias && c.s;
+        if (forward_side.tiles)
+            ISO_TRY(add_tiles(forward_side, tile_by_type<GradQTileKernel>(t.dtype, t.head_dim, segments), a.group / forward_side.plan.heads));
+        else
+            ISO_TRY(add_launch(b, by_type<GradQRowKernel>(t.dtype, is_wide), (n * t.q_heads + 3) / 4, 256, a));
+        if (backward_side.tiles)
+            ISO_TRY(add_tiles(backward_side, tile_by_type<GradKVTileKernel>(t.dtype, t.head_dim, segments), 1));
+        else
+            ISO_TRY(add_launch(b, by_type<GradKVRowKernel>(t.dtype, is_wide), (n * t.kv_heads + 3) / 4, 256, a));
+        if (!bias) return ISO_SUCCESS;
         const uint64_t slots = (uint64_t)t.q_heads * c.s;
-        a.parts = (int)bias_parts(c, t.q_heads);
-        ISO_TRY(add_launch(b, by_type<GradBiasRowKernel>(t.dtype, is_wide), (slots * a.parts + 3) / 4, 256, a));
-        return add_launch(b, sum_parts_by_type(t.dtype), (slots + 15) / 16, 256,
+        a.parts = forward_side.tiles ? (int)forward_side.plan.n_tiles : (int)bias_parts(c, t.q_heads);
+        if (!forward_side.tiles)
+            ISO_TRY(add_launch(b, by_type<GradBiasRowKernel>(t.dtype, is_wide), (slots * a.parts + 3) / 4, 256, a));
+        return add_launch(b, sum_parts_by_type(t.dtype), (slots + 15) / 16, 1024,
                           SumPartsArgs{a.partials, g->grad_bias, (uint32_t)slots, (uint32_t)a.parts});
     }
 
@@ -419,8 +458,7 @@ class AttentionBinder {
     BackwardWorkspace work;
     AttentionArgs a{};
     bool is_wide = false;
-    TilePlan plan;
-    size_t lds = 0, at_columns = 0, at_rows = 0, at_active = 0, at_index = 0;
+    Side forward_side, backward_side;          // columns are ranks; columns are keys
 };
 
 // ---- rotary positions --------------------------------------------------------------

@@ -28,46 +28,39 @@ struct TilePlan {
     std::vector<int32_t> column_at;        // [kTileColumns / heads][d]: position in the tile
     std::vector<int32_t> row_at;           // [chunks * kChunkRows][d]: position relative to the tile's first rank
     std::vector<uint32_t> active;          // [chunks]: bit 4 * wave + group: that block holds a neighbour
+    // The bias's gradient, for columns that are ranks: which pairs of a (chunk, wavefront) belong to one slot
+    // (head of the column) * s + neighbour.  Slots with the most pairs first.
+    struct Slot {
+        uint32_t slot, first, count;
+    };
+    std::vector<uint32_t> slots_of;        // [chunks * kTileWaves + 1]: first of `slots`
+    std::vector<Slot> slots;
+    std::vector<uint16_t> pairs;           // slot_pair of each
     std::vector<uint16_t> index;           // [chunks * 4][kTileWaves][64][4]: neighbour of (lane's column, row 4 * (lane / 16) + r)
                                            // of the 16 rows of a group, s where it is none
 };
 
-// back = false: columns are ranks, rows their sources R (-) C^i.  back = true: columns are sources, rows the ranks that read
-// them.  False where no table of that form exists (neighbours too many, or too far apart).
-inline bool build_tile_plan(const Comm &c, int heads, bool back, TilePlan &out) {
-    const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
-    if (c.s < 1 || c.s > 65534) return false;
-    // offsets as signed steps from a column to its row; what no rank of a mesh can reach is left out
-    std::vector<std::array<int32_t, ISO_MAX_DIMS>> step((size_t)c.s);
-    std::vector<uint8_t> used((size_t)c.s, 1);
-    std::array<int32_t, ISO_MAX_DIMS> low{}, high{}, wave{};
-    bool any = false;
-    for (int i = 0; i < c.s; ++i) {
-        for (int j = 0; j < d; ++j) {
-            const int64_t n = c.dims[j];
-            int64_t x = c.c(i, j);
-            if (c.periodic[j]) x = x > n / 2 ? x - n : x;
-            else if (x >= n || x <= -n) used[i] = 0;
-            step[i][j] = used[i] ? (int32_t)(back ? x : -x) : 0;
-        }
-        if (!used[i]) continue;
-        for (int j = 0; j < d; ++j) {
-            low[j] = any ? std::min(low[j], step[i][j]) : step[i][j];
-            high[j] = any ? std::max(high[j], step[i][j]) : step[i][j];
-        }
-        any = true;
-    }
-    // The tile: dimensions are doubled where that keeps the rows of all tiles together fewest; the ranks of a wavefront the same way.
-    TilePlan p;
-    p.heads = heads;
+// Where a wavefront keeps the pair of a column (0..15) and a row of the chunk (0..63): lane (row % 16 / 4) * 16 + column writes
+// four rows at once.
+inline uint16_t slot_pair(int column, int row) { return (uint16_t)(((row / 16 * 64) + (row % 16 / 4) * 16 + column) * 4 + row % 4); }
+
+struct TileShape {
+    std::array<int32_t, ISO_MAX_DIMS> tile{}, wave{}, tiles{};
+    int64_t n_tiles = 1;
+};
+
+// The tile: dimensions are doubled where that keeps the rows of all tiles together fewest; the ranks of a wavefront the same way.
+// reach: highest less lowest step to a neighbour, by dimension.
+inline TileShape tile_shape(const Comm &c, int ranks, int per_wave, const std::array<int64_t, ISO_MAX_DIMS> &reach) {
+    TileShape s;
     const auto grow = [&](std::array<int32_t, ISO_MAX_DIMS> &t, int total, const std::array<int32_t, ISO_MAX_DIMS> *limit) {
         t.fill(1);
         for (int have = 1; have < total; have *= 2) {
             int best = -1;
             double best_cost = 0;
-            for (int j = d - 1; j >= 0; --j) {
+            for (int j = c.d - 1; j >= 0; --j) {
                 if (limit && t[j] * 2 > (*limit)[j]) continue;
-                const double n = c.dims[j], e = (double)high[j] - low[j], w = t[j];
+                const double n = c.dims[j], e = (double)reach[j], w = t[j];
                 const auto cost = [&](double x) { return (limit ? n / x : std::ceil(n / x)) * (x + e); };
                 const double gain = cost(2 * w) / cost(w);
                 if (best < 0 || gain < best_cost) best = j, best_cost = gain;
@@ -75,12 +68,68 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, TilePlan &out) 
             t[best] *= 2;
         }
     };
-    grow(p.tile, ranks, nullptr);
-    grow(wave, per_wave, &p.tile);
-    for (int j = 0; j < d; ++j) {
-        p.tiles[j] = (c.dims[j] + p.tile[j] - 1) / p.tile[j];
-        p.n_tiles *= p.tiles[j];
+    grow(s.tile, ranks, nullptr);
+    grow(s.wave, per_wave, &s.tile);
+    for (int j = 0; j < c.d; ++j) {
+        s.tiles[j] = (c.dims[j] + s.tile[j] - 1) / s.tile[j];
+        s.n_tiles *= s.tiles[j];
     }
+    return s;
+}
+
+// Steps from a rank to its sources, signed, and how far they reach; what no rank of a mesh can have is left out.
+struct Steps {
+    std::vector<std::array<int32_t, ISO_MAX_DIMS>> step;
+    std::vector<uint8_t> used;
+    std::array<int32_t, ISO_MAX_DIMS> low{}, high{};
+    std::array<int64_t, ISO_MAX_DIMS> reach{};
+};
+inline Steps source_steps(const Comm &c) {
+    Steps s;
+    s.step.resize((size_t)c.s);
+    s.used.assign((size_t)c.s, 1);
+    bool any = false;
+    for (int i = 0; i < c.s; ++i) {
+        s.step[i].fill(0);
+        for (int j = 0; j < c.d; ++j) {
+            const int64_t n = c.dims[j];
+            int64_t x = c.c(i, j);
+            if (c.periodic[j]) x = x > n / 2 ? x - n : x;
+            else if (x >= n || x <= -n) s.used[i] = 0;
+            s.step[i][j] = s.used[i] ? (int32_t)-x : 0;
+        }
+        if (!s.used[i]) continue;
+        for (int j = 0; j < c.d; ++j) {
+            s.low[j] = any ? std::min(s.low[j], s.step[i][j]) : s.step[i][j];
+            s.high[j] = any ? std::max(s.high[j], s.step[i][j]) : s.step[i][j];
+        }
+        any = true;
+    }
+    for (int j = 0; j < c.d; ++j) s.reach[j] = (int64_t)s.high[j] - s.low[j];
+    return s;
+}
+inline TileShape tile_shape(const Comm &c, int heads) { return tile_shape(c, kTileColumns / heads, 16 / heads, source_steps(c).reach); }
+
+// back = false: columns are ranks, rows their sources R (-) C^i.  back = true: columns are sources, rows the ranks that read
+// them.  False where no table of that form exists (neighbours too many, or too far apart).
+inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots, TilePlan &out) {
+    const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
+    if (c.s < 1 || c.s > 65534) return false;
+    Steps steps = source_steps(c);
+    if (back)                              // from a source to its readers
+        for (int i = 0; i < c.s; ++i)
+            for (int j = 0; j < d; ++j) steps.step[i][j] = -steps.step[i][j];
+    std::array<int32_t, ISO_MAX_DIMS> low = steps.low, high = steps.high;
+    for (int j = 0; back && j < d; ++j) low[j] = -steps.high[j], high[j] = -steps.low[j];
+    const auto &step = steps.step;
+    const auto &used = steps.used;
+    TilePlan p;
+    p.heads = heads;
+    const TileShape shape = tile_shape(c, ranks, per_wave, steps.reach);
+    const auto &wave = shape.wave;
+    p.tile = shape.tile;
+    p.tiles = shape.tiles;
+    p.n_tiles = shape.n_tiles;
     if (p.n_tiles > 0x7FFFFFFF) return false;
     // columns: the wavefronts' boxes one after the other, the last dimension fastest inside and outside
     p.column_at.resize((size_t)ranks * d);
@@ -161,6 +210,29 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, TilePlan &out) 
         }
     }
     for (uint32_t a : p.active) p.blocks += __builtin_popcount(a);
+    if (bias_slots) {
+        std::vector<std::vector<std::pair<uint32_t, uint16_t>>> of((size_t)p.chunks * kTileWaves);
+        for (const auto &[pair, i] : taken) {
+            const int r = (int)(pair >> 32), u = rank_of[(size_t)(pair & 0xFFFFFFFF)];
+            for (int h = 0; h < heads; ++h) {
+                const int column = r * heads + h;
+                of[(size_t)(u / kChunkRows) * kTileWaves + column / 16].push_back(
+                    {(uint32_t)(h * c.s + i), slot_pair(column % 16, u % kChunkRows)});
+            }
+        }
+        for (auto &list : of) {
+            p.slots_of.push_back((uint32_t)p.slots.size());
+            std::sort(list.begin(), list.end());
+            const size_t begin = p.slots.size();
+            for (const auto &[slot, at] : list) {
+                if (p.slots.size() == begin || p.slots.back().slot != slot) p.slots.push_back({slot, (uint32_t)p.pairs.size(), 0});
+                ++p.slots.back().count;
+                p.pairs.push_back(at);
+            }
+            std::stable_sort(p.slots.begin() + begin, p.slots.end(), [](const auto &x, const auto &y) { return x.count > y.count; });
+        }
+        p.slots_of.push_back((uint32_t)p.slots.size());
+    }
     out = std::move(p);
     return true;
 }

@@ -209,8 +209,9 @@ __device__ __forceinline__ void attend_row(const AttentionArgs &a, uint32_t row,
     }
 }
 
-template <typename T, bool WIDE, bool LSE = true>
-__device__ __forceinline__ void write_row(const AttentionArgs &a, uint32_t row, int h, const RowState<ElementTraits<T>::kPerLane> &st) {
+template <typename T, bool WIDE>
+__device__ __forceinline__ void write_row(const AttentionArgs &a, uint32_t row, int h, const RowState<ElementTraits<T>::kPerLane> &st,
+                                          bool lse = true) {
     constexpr int E = ElementTraits<T>::kPerLane;
     const int lane = threadIdx.x & 63;
     if (lane >> a.lanes_log2) return;
@@ -219,7 +220,7 @@ __device__ __forceinline__ void write_row(const AttentionArgs &a, uint32_t row, 
 #pragma unroll
     for (int e = 0; e < E; ++e) y[e] = st.acc[e] * inv;
     store_elements<T, WIDE>((T *)a.out.data + row * a.out.rank_stride + h * a.out.head_stride, lane * E, a.head_dim, y);
-    if (LSE && a.lse && lane == 0) a.lse[(int64_t)row * a.q_heads + h] = st.l == 0.f ? -INFINITY : st.m + __builtin_amdgcn_logf(st.l) * kLn2;
+    if (lse && a.lse && lane == 0) a.lse[(int64_t)row * a.q_heads + h] = st.l == 0.f ? -INFINITY : st.m + __builtin_amdgcn_logf(st.l) * kLn2;
 }
 
 // A row outside the torus, given in `rows`: treated as one without neighbours.

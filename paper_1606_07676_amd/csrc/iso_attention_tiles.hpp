@@ -9,6 +9,10 @@
 // Scores are computed transposed, S^T = K Q^T, so that a lane holds one column and four rows of each 16 x 16 block, and the
 // weights of two blocks are, in registers, the right-hand operand of out^T += V^T P^T: the order of rows inside a product
 // of 32 is free as long as both operands keep it.  V^T comes out of the row-major LDS tile through the transposing read.
+//
+// Vector arithmetic on the scores bounds these kernels, not the matrix products (8 % of the time), so a score costs as few
+// instructions as it can: the table holds the byte offset of the pair's bias in LDS, and for pairs that are no neighbours
+// that of a -inf.  Rows go from memory to LDS without passing through registers, one chunk ahead of the one in use.
 #pragma once
 
 #include "iso_attention_kernels.hpp"
@@ -21,13 +25,14 @@ struct TileArgs {
     int32_t tile[ISO_MAX_DIMS], tiles[ISO_MAX_DIMS];
     uint32_t n_tiles, per_xcd;             // workgroups of one XCD
     int32_t heads, parts;                  // columns of one rank; sets of `heads` q heads that share a key head
-    int32_t chunks;
+    int32_t chunks;                        // of TileLds<DP>::kRows rows
     const int32_t *column_at, *row_at;
     const uint32_t *active;
     const uint16_t *index;
     const uint32_t *slots_of;              // the bias's gradient, or null: see TilePlan
     const TilePlan::Slot *slots;
     const uint16_t *pairs;
+    const void *zeros;                     // a row of zeros
 };
 
 template <typename T> struct Matrix;
@@ -36,7 +41,7 @@ template <> struct Matrix<__bf16> {
     typedef __bf16 x4 __attribute__((ext_vector_type(4)));
     typedef float f4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f4 multiply(x8 a, x8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ x4 read_transposed(const __bf16 *at) {
+    static __device__ __forceinline__ x4 read_transposed(const unsigned char *at) {
         return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4 *)at);
     }
 };
@@ -45,7 +50,7 @@ template <> struct Matrix<_Float16> {
     typedef _Float16 x4 __attribute__((ext_vector_type(4)));
     typedef float f4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f4 multiply(x8 a, x8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ x4 read_transposed(const _Float16 *at) {
+    static __device__ __forceinline__ x4 read_transposed(const unsigned char *at) {
         typedef __fp16 h4 __attribute__((ext_vector_type(4)));
         return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)at));
     }
@@ -65,22 +70,33 @@ __device__ __forceinline__ float column_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// LDS of a tile kernel: two staged tensors of kChunkRows rows, padded by 16 bytes so that the 16 rows of a product start in
-// 16 different groups of banks, then per row of the tile its rank and segment, then the biases.
-template <typename T, int DP> struct TileLds {
-    static constexpr int kStride = DP + 8;
-    T *first, *second;
+// LDS of a tile kernel: two chunks of rows of two tensors, then per row of the tile its rank and segment, then the biases.
+//
+// Loads into LDS write a wavefront's 64 pieces of 16 bytes one after the other, so rows are dense; which piece of its row a
+// lane fetches is permuted by the row, so that the 16 rows of a product's operand lie in 16 different groups of banks.
+template <int DP> struct TileLds {
+    static constexpr int kRows = DP > 64 ? 32 : 64;                 // of a chunk: 16 KB for both tensors (96: 12)
+    static constexpr int kGroups = kRows / 16;
+    static constexpr int kRowBytes = DP * 2, kPieces = DP / 8, kTensor = kRows * kRowBytes;
+    static constexpr int kLoads = (kRows * kPieces + 255) / 256;
+    unsigned char *chunk;                  // [2][2][kTensor]
     int32_t *rank, *segment;
     float *bias;
-    static __host__ __device__ size_t bytes(int chunks, size_t biases) {
-        return 2 * sizeof(T) * kChunkRows * kStride + (size_t)chunks * kChunkRows * 8 + biases * 4;
-    }
+
+    static __host__ __device__ size_t bytes(int chunks, size_t floats) { return 4 * (size_t)kTensor + (size_t)chunks * kRows * 8 + floats * 4; }
     __device__ TileLds(unsigned char *at, int chunks) {
-        first = (T *)at;
-        second = first + kChunkRows * kStride;
-        rank = (int32_t *)(second + kChunkRows * kStride);
-        segment = rank + chunks * kChunkRows;
-        bias = (float *)(segment + chunks * kChunkRows);
+        chunk = at;
+        rank = (int32_t *)(at + 4 * kTensor);
+        segment = rank + chunks * kRows;
+        bias = (float *)(segment + chunks * kRows);
+    }
+    static __device__ __forceinline__ int place(int row, int piece) {
+        return DP == 32 ? piece ^ (row >> 2 & 3) : DP == 64 ? piece ^ (row >> 1 & 7) : DP == 128 ? piece ^ (row & 15)
+                                                                                              : (piece + (row >> 2 & 3)) % 12;
+    }
+    static __device__ __forceinline__ int piece_at(int row, int place) {
+        return DP == 32 ? place ^ (row >> 2 & 3) : DP == 64 ? place ^ (row >> 1 & 7) : DP == 128 ? place ^ (row & 15)
+                                                                                              : (place + 12 - (row >> 2 & 3)) % 12;
     }
 };
 
@@ -112,18 +128,20 @@ struct TileWork {
     int key_head, part;
     bool any;
 };
-__device__ __forceinline__ TileWork tile_work(const TileArgs &t, int key_heads) {
+__device__ __forceinline__ TileWork tile_work(const TileArgs &t) {
     TileWork w;
     const uint32_t item = (blockIdx.x & 7) * t.per_xcd + (blockIdx.x >> 3), pairs = item / t.parts;
     w.part = item % t.parts;
     w.tile = pairs % t.n_tiles;
     w.key_head = pairs / t.n_tiles;
-    w.any = w.key_head < key_heads;
+    w.any = w.key_head < t.a.kv_heads;
     return w;
 }
 
-template <typename T, int DP>
-__device__ __forceinline__ void tile_rows(const TileArgs &t, uint32_t tile, int32_t *origin, TileLds<T, DP> &lds) {
+// Ranks and segments of the tile's rows.  A row that is not there keeps rank -1 where segments are compared, and is then
+// staged as zeros; on a torus without segments only columns outside the torus refer to such rows, and any rank serves.
+template <int DP, bool SEGMENTS>
+__device__ __forceinline__ void tile_rows(const TileArgs &t, uint32_t tile, int32_t *origin, TileLds<DP> &lds) {
     const int d = t.a.torus.d;
     if ((int)threadIdx.x < d) {
         uint32_t rest = tile;
@@ -131,42 +149,88 @@ __device__ __forceinline__ void tile_rows(const TileArgs &t, uint32_t tile, int3
         origin[threadIdx.x] = (int32_t)(rest % (uint32_t)t.tiles[threadIdx.x]) * t.tile[threadIdx.x];
     }
     __syncthreads();
-    for (int u = threadIdx.x; u < t.chunks * kChunkRows; u += 256) {
+    for (int u = threadIdx.x; u < t.chunks * TileLds<DP>::kRows; u += 256) {
         const int32_t rank = rank_at(t, origin, t.row_at + (int64_t)u * d, false);
-        int32_t segment = rank < 0 ? kNoToken : t.a.segments ? t.a.segments[rank] : 0;
-        if (segment < 0) segment = kNoToken;
-        lds.rank[u] = segment < 0 ? -1 : rank;                      // rows without a token are staged as zeros
-        lds.segment[u] = segment;
+        if (SEGMENTS) {
+            int32_t segment = rank < 0 ? kNoToken : t.a.segments ? t.a.segments[rank] : 0;
+            if (segment < 0) segment = kNoToken;
+            lds.rank[u] = segment < 0 ? -1 : rank;
+            lds.segment[u] = segment;
+        } else {
+            lds.rank[u] = max(rank, 0);
+        }
     }
 }
 
-// One chunk of rows of two tensors: into registers, 16 bytes a lane, and from there into LDS.
-template <typename T, int DP> struct Staged {
-    static constexpr int kUnits = DP / 8, kPerThread = kChunkRows * kUnits / 256;
-    typename Matrix<T>::x8 first[kPerThread], second[kPerThread];
+__device__ __forceinline__ int32_t column_segment(const AttentionArgs &a, int64_t rank) {
+    const int32_t own = rank < 0 ? kNoColumn : a.segments ? a.segments[rank] : 0;
+    return own < 0 ? kNoColumn : own;
+}
 
-    __device__ __forceinline__ void load(const T *a, int64_t a_stride, const T *b, int64_t b_stride, const int32_t *rank, int head_dim) {
-#pragma unroll
-        for (int i = 0; i < kPerThread; ++i) {
-            const int unit = threadIdx.x + 256 * i, row = unit / kUnits, at = unit % kUnits * 8;
-            const int32_t r = rank[row];
-            first[i] = {};
-            second[i] = {};
-            if (r >= 0 && at < head_dim) {
-                first[i] = *(const typename Matrix<T>::x8 *)(a + r * a_stride + at);
-                second[i] = *(const typename Matrix<T>::x8 *)(b + r * b_stride + at);
-            }
-        }
+// Biases of `heads` q heads in LDS, a -inf behind each; zeros where there are none.
+template <typename T>
+__device__ __forceinline__ void tile_biases(const AttentionArgs &a, int first_head, int heads, float factor, float *at) {
+    const int s = a.torus.s;
+    for (int i = threadIdx.x; i < heads * (s + 1); i += 256) {
+        const int h = i / (s + 1), j = i % (s + 1);
+        float b = j == s ? -INFINITY : a.bias ? (float)((const T *)a.bias)[(int64_t)(first_head + h) * s + j] : 0.f;
+        // a factor must not make an infinity of a bias near the type's lowest value
+        if (factor != 1.f && b != -INFINITY) b = fminf(fmaxf(b * factor, -3.4e38f), 3.4e38f);
+        at[i] = b;
     }
-    __device__ __forceinline__ void store(TileLds<T, DP> &lds) const {
+}
+
+// One chunk of rows of two tensors on its way into LDS.  Tensors are given by the address of rank 0's row and the bytes
+// between ranks, below 2^32.
+template <int DP, bool SEGMENTS> struct RowLoads {
+    typedef TileLds<DP> Lds;
+    const unsigned char *first, *second, *zeros;
+    uint32_t first_stride, second_stride;
+    int head_dim;
+
+    __device__ __forceinline__ void start(const int32_t *rank, unsigned char *chunk) const {
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) {
-            const int unit = threadIdx.x + 256 * i, row = unit / kUnits, at = unit % kUnits * 8;
-            *(typename Matrix<T>::x8 *)(lds.first + row * lds.kStride + at) = first[i];
-            *(typename Matrix<T>::x8 *)(lds.second + row * lds.kStride + at) = second[i];
+        for (int i = 0; i < Lds::kLoads; ++i) {
+            const int unit = threadIdx.x + 256 * i, row = unit / Lds::kPieces;
+            if (Lds::kRows * Lds::kPieces % 256 && unit >= Lds::kRows * Lds::kPieces) break;      // whole wavefronts
+            const int piece = Lds::piece_at(row, unit % Lds::kPieces);
+            const int32_t r = rank[row];
+            const unsigned char *a = first + (uint64_t)(uint32_t)r * first_stride + piece * 16;
+            const unsigned char *b = second + (uint64_t)(uint32_t)r * second_stride + piece * 16;
+            if ((SEGMENTS && r < 0) || piece * 8 >= head_dim) a = b = zeros;
+            unsigned char *to = chunk + __builtin_amdgcn_readfirstlane((threadIdx.x & ~63u) * 16 + 4096 * i);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)a,
+                                             (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)b,
+                                             (__attribute__((address_space(3))) void *)(to + Lds::kTensor), 16, 0, 0);
         }
     }
 };
+// The chunk that was started is in LDS, and everybody has done with the one before it.
+__device__ __forceinline__ void wait_for_rows() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// The table's entries of a chunk: byte offsets of the biases of this lane's column and rows 4 (lane / 16) + 0..3 of each group.
+template <int GROUPS> struct Pairs {
+    uint2 of[GROUPS];
+    __device__ __forceinline__ void load(const TileArgs &t, int chunk) {
+        const uint2 *at = (const uint2 *)t.index + ((int64_t)chunk * GROUPS * kTileWaves + (threadIdx.x >> 6)) * 64 + (threadIdx.x & 63);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) of[g] = at[g * kTileWaves * 64];
+    }
+    __device__ __forceinline__ float bias(const unsigned char *base, int g, int r) const {
+        const uint32_t two = r < 2 ? of[g].x : of[g].y;
+        return *(const float *)(base + (r % 2 ? two >> 16 : two & 0xFFFF));
+    }
+};
+// Bit g: group g of the chunk holds a neighbour of one of the wavefront's columns.
+template <int GROUPS> __device__ __forceinline__ uint32_t active_groups(const TileArgs &t, int chunk) {
+    const uint32_t word = t.active[GROUPS == 4 ? chunk : chunk >> 1];
+    const uint32_t mine = __builtin_amdgcn_readfirstlane(word >> ((threadIdx.x >> 6) * 4)) & 15;
+    return GROUPS == 4 ? mine : mine >> (chunk % 2 * 2) & 3;
+}
 
 // A column's row as right-hand operand: lane holds column lane % 16, elements 32 k + 8 (lane / 16) + 0..7.
 template <typename T, int DP>
@@ -180,29 +244,34 @@ __device__ __forceinline__ void load_column(const Heads &h, int64_t rank, int he
     }
 }
 
-// 16 staged rows times the columns: lane holds column lane % 16, rows 4 (lane / 16) + 0..3.
-template <typename T, int DP>
-__device__ __forceinline__ typename Matrix<T>::f4 rows_times_columns(const T *rows, const typename Matrix<T>::x8 (&column)[DP / 32]) {
-    const int lane = threadIdx.x & 63;
-    const T *at = rows + lane % 16 * TileLds<T, DP>::kStride + lane / 16 * 8;
-    typename Matrix<T>::f4 s = {0.f, 0.f, 0.f, 0.f};
+// Where a lane finds its pieces of staged rows: the same for every group of 16.
+template <typename T, int DP> struct LanePieces {
+    uint32_t plain[DP / 32], turned[DP / 16];
+    __device__ LanePieces() {
+        const int lane = threadIdx.x & 63, quarter = lane / 16, within = lane % 16, row = quarter * 4 + within / 4;
 #pragma unroll
-    for (int k = 0; k < DP / 32; ++k) s = Matrix<T>::multiply(*(const typename Matrix<T>::x8 *)(at + 32 * k), column[k], s);
-    return s;
-}
-
-// acc^T += rows^T w for 32 rows: w holds, for each lane's column, its weights of 4 rows of either half.
-template <typename T, int DP>
-__device__ __forceinline__ void add_weighted_rows(const T *rows, typename Matrix<T>::x8 w, typename Matrix<T>::f4 (&acc)[DP / 16]) {
-    const int lane = threadIdx.x & 63, quarter = lane / 16, within = lane % 16;
-    const T *at = rows + (quarter * 4 + within / 4) * TileLds<T, DP>::kStride + within % 4 * 4;
+        for (int k = 0; k < DP / 32; ++k) plain[k] = within * TileLds<DP>::kRowBytes + TileLds<DP>::place(within, 4 * k + quarter) * 16;
 #pragma unroll
-    for (int e = 0; e < DP / 16; ++e) {
-        const typename Matrix<T>::x4 low = Matrix<T>::read_transposed(at + 16 * e);
-        const typename Matrix<T>::x4 high = Matrix<T>::read_transposed(at + 16 * e + 16 * TileLds<T, DP>::kStride);
-        acc[e] = Matrix<T>::multiply(__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[e]);
+        for (int e = 0; e < DP / 16; ++e)
+            turned[e] = row * TileLds<DP>::kRowBytes + TileLds<DP>::place(row, 2 * e + within % 4 / 2) * 16 + within % 2 * 8;
     }
-}
+    // 16 staged rows times the columns: lane holds column lane % 16, rows 4 (lane / 16) + 0..3.
+    __device__ __forceinline__ typename Matrix<T>::f4 rows_times_columns(const unsigned char *rows, const typename Matrix<T>::x8 (&column)[DP / 32]) const {
+        typename Matrix<T>::f4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < DP / 32; ++k) s = Matrix<T>::multiply(*(const typename Matrix<T>::x8 *)(rows + plain[k]), column[k], s);
+        return s;
+    }
+    // acc^T += rows^T w for 32 rows: w holds, for each lane's column, its weights of 4 rows of either half.
+    __device__ __forceinline__ void add_weighted_rows(const unsigned char *rows, typename Matrix<T>::x8 w, typename Matrix<T>::f4 (&acc)[DP / 16]) const {
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e) {
+            const typename Matrix<T>::x4 low = Matrix<T>::read_transposed(rows + turned[e]);
+            const typename Matrix<T>::x4 high = Matrix<T>::read_transposed(rows + turned[e] + 16 * TileLds<DP>::kRowBytes);
+            acc[e] = Matrix<T>::multiply(__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[e]);
+        }
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ typename Matrix<T>::x8 as_weights(const typename Matrix<T>::f4 &a, const typename Matrix<T>::f4 &b) {
@@ -214,7 +283,7 @@ __device__ __forceinline__ typename Matrix<T>::x8 as_weights(const typename Matr
     return w;
 }
 
-// A column's result: lane holds elements 16 e + 4 (lane / 16) + 0..3 of column lane % 16.
+// A column's result: lane holds elements 16 e + 4 (lane / 16) + 0..3 of column lane % 16.  Whether all are finite.
 template <typename T, int DP>
 __device__ __forceinline__ bool store_column(const Heads &h, int64_t rank, int head, int head_dim, const typename Matrix<T>::f4 (&acc)[DP / 16],
                                              float factor) {
@@ -250,94 +319,111 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256) void attention_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
+    typedef TileLds<DP> Lds;
+    constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
     __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
     const AttentionArgs &a = t.a;
-    const TileWork work = tile_work(t, a.kv_heads);
+    const TileWork work = tile_work(t);
     if (!work.any) return;
-    TileLds<T, DP> lds(lds_bytes, t.chunks);
-    tile_rows<T, DP>(t, work.tile, origin, lds);
+    Lds lds(lds_bytes, t.chunks);
+    tile_rows<DP, SEGMENTS>(t, work.tile, origin, lds);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
-    const int s = a.torus.s;
-    if (a.bias)
-        for (int i = threadIdx.x; i < t.heads * s; i += 256)
-            lds.bias[i / s * (s + 1) + i % s] = (float)((const T *)a.bias)[(int64_t)first_head * s + i];
+    tile_biases<T>(a, first_head, t.heads, kLog2e, lds.bias);
     const int64_t rank = rank_at(t, origin, t.column_at + column / t.heads * a.torus.d, true);
-    int32_t own = kNoColumn;
-    if (rank >= 0) own = a.segments ? a.segments[rank] : 0;
-    if (own < 0) own = kNoColumn;
+    const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 q[DP / 32];
     load_column<T, DP>(a.q, rank, head, a.head_dim, q);
+    const LanePieces<T, DP> pieces;
+    const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.k.data + work.key_head * a.k.head_stride),
+                                          (const unsigned char *)((const T *)a.v.data + work.key_head * a.v.head_stride),
+                                          (const unsigned char *)t.zeros, (uint32_t)(a.k.rank_stride * 2), (uint32_t)(a.v.rank_stride * 2), a.head_dim};
+    // scores times log2 e, so that the weights are powers of two
+    const float scale = a.scale * kLog2e, cap = a.cap * kLog2e, to_cap = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f;
     __syncthreads();
 
-    const T *k0 = (const T *)a.k.data + work.key_head * a.k.head_stride, *v0 = (const T *)a.v.data + work.key_head * a.v.head_stride;
-    const float *bias = lds.bias + column % t.heads * (s + 1);
     f4 acc[DP / 16] = {};
     float m = -INFINITY, l = 0.f;                                   // l: of this lane's rows
-    Staged<T, DP> next;
-    next.load(k0, a.k.rank_stride, v0, a.v.rank_stride, lds.rank, a.head_dim);
+    Pairs<G> next;
+    loads.start(lds.rank, lds.chunk);
+    next.load(t, 0);
     for (int chunk = 0; chunk < t.chunks; ++chunk) {
-        __syncthreads();
-        next.store(lds);
-        __syncthreads();
-        if (chunk + 1 < t.chunks)
-            next.load(k0, a.k.rank_stride, v0, a.v.rank_stride, lds.rank + (chunk + 1) * kChunkRows, a.head_dim);
-        const uint32_t active = __builtin_amdgcn_readfirstlane(t.active[chunk] >> (4 * wave) & 15);
+        wait_for_rows();
+        const Pairs<G> pairs = next;
+        const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
+        const uint32_t active = active_groups<G>(t, chunk);
+        if (chunk + 1 < t.chunks) {
+            loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
+            next.load(t, chunk + 1);
+        }
         if (!active) continue;
-        f4 x[4];
+        f4 x[G];
         float top = m;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < G; ++g) {
             x[g] = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             if (!(active >> g & 1)) continue;
-            const uint2 who = *(const uint2 *)(t.index + (((int64_t)(chunk * 4 + g) * kTileWaves + wave) * 64 + lane) * 4);
-            const f4 dot = rows_times_columns<T, DP>(lds.first + g * 16 * lds.kStride, q);
-            const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * kChunkRows + g * 16 + lane / 16 * 4) : int4{};
+            const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
+            if (a.cap > 0.f) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = (r < 2 ? who.x : who.y) >> (r % 2 * 16) & 0xFFFF;
-                float y = dot[r] * a.scale;
-                if (a.cap > 0.f) y = capped(y, a.cap);
-                if (a.bias) y += bias[i];
-                const bool counts = i != s && (!SEGMENTS || (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
-                x[g][r] = counts ? y : -INFINITY;
-                top = fmaxf(top, x[g][r]);
+                for (int r = 0; r < 4; ++r) {
+                    const float e = __builtin_amdgcn_exp2f(dot[r] * to_cap);
+                    x[g][r] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap) + pairs.bias((const unsigned char *)lds.bias, g, r);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[g][r] = fmaf(dot[r], scale, pairs.bias((const unsigned char *)lds.bias, g, r));
             }
+            if (SEGMENTS) {
+                const int4 seg = *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4);
+                x[g][0] = seg.x == own ? x[g][0] : -INFINITY;
+                x[g][1] = seg.y == own ? x[g][1] : -INFINITY;
+                x[g][2] = seg.z == own ? x[g][2] : -INFINITY;
+                x[g][3] = seg.w == own ? x[g][3] : -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, x[g][r]);
         }
         top = column_max(top);
         const float base = finite_floor(top);
         if (__any(top > m)) {
-            const float keep = exp_above(m, base);
+            const float keep = __builtin_amdgcn_exp2f(m - base);
             l *= keep;
 #pragma unroll
             for (int e = 0; e < DP / 16; ++e) acc[e] *= keep;
             m = top;
         }
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+        for (int pair = 0; pair < G / 2; ++pair) {
+            if (!(active >> (2 * pair) & 3)) continue;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[g][r] = exp_above(x[g][r], base);
-                l += x[g][r];
-            }
+            for (int g = 2 * pair; g < 2 * pair + 2; ++g)
 #pragma unroll
-        for (int pair = 0; pair < 2; ++pair)
-            if (active >> (2 * pair) & 3)
-                add_weighted_rows<T, DP>(lds.second + pair * 32 * lds.kStride, as_weights<T>(x[2 * pair], x[2 * pair + 1]), acc);
+                for (int r = 0; r < 4; ++r) {
+                    x[g][r] = __builtin_amdgcn_exp2f(x[g][r] - base);
+                    l += x[g][r];
+                }
+            pieces.add_weighted_rows(rows + Lds::kTensor + pair * 32 * Lds::kRowBytes, as_weights<T>(x[2 * pair], x[2 * pair + 1]), acc);
+        }
     }
     l = column_sum(l);
-    const bool fine = store_column<T, DP>(a.out, rank, head, a.head_dim, acc, l == 0.f ? 0.f : 1.f / l);
-    if (a.lse && rank >= 0 && lane < 16) a.lse[rank * a.q_heads + head] = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2;
-    redo_columns(rank >= 0 && !fine, [&](int c) {
+    bool fine = store_column<T, DP>(a.out, rank, head, a.head_dim, acc, l == 0.f ? 0.f : 1.f / l);
+    // biases near the type's lowest value alone: their products with log2 e were cut off
+    const bool low = m < -1e38f && m != -INFINITY, again = low || l != l;
+    fine = fine && !low;
+    if (a.lse && rank >= 0 && lane < 16 && !again)
+        a.lse[rank * a.q_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    redo_columns(rank >= 0 && !(fine && !again), [&](int c) {
         const uint32_t r = (uint32_t)__shfl((int)rank, c);
         const int h = __shfl(head, c);
+        const bool lse = __shfl((int)again, c);
         store_coordinates(a.torus, r, lane, coords[wave]);
         __builtin_amdgcn_wave_barrier();
         RowState<8> st;
         attend_row<T, true>(a, r, r, h, 0, 1, coords[wave], st);
-        write_row<T, true, false>(a, r, h, st);       // lse does not depend on the values
+        write_row<T, true>(a, r, h, st, lse);                      // lse stays where it does not depend on what was wrong
         __builtin_amdgcn_wave_barrier();
     });
 }
@@ -349,32 +435,56 @@ __global__ __launch_bounds__(256) void attention_tile_kernel(const TileArgs t) {
 // grad_out staged: S and dP with the roles changed, grad_k^T += Q^T da, grad_v^T += grad_out^T P, head by head of the group.
 // Both gather: a tile's results are written once, by one workgroup, in one order.
 
+// P, dx and da of a pair.  The bias is -inf, and P 0, for pairs that are no neighbours.
+struct GradientFactors {
+    float scale, cap, to_cap;
+    __device__ explicit GradientFactors(const AttentionArgs &a)
+        : scale(a.scale), cap(a.cap), to_cap(a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f) {}
+    template <bool SEGMENTS>
+    __device__ __forceinline__ PairGradient operator()(float dot, float bias, float lse, float dp, float delta, bool counts) const {
+        PairGradient g;
+        float x, slope = 1.f;
+        if (cap > 0.f) {
+            const float y = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(dot * to_cap)), 1.f);      // tanh
+            x = fmaf(cap, y, bias);
+            slope = fmaf(-y, y, 1.f);
+        } else {
+            x = fmaf(dot, scale, bias);
+        }
+        g.p = exp_above(x, lse);
+        g.dx = g.p * (dp - delta);
+        if (SEGMENTS) {                    // what a pair that does not count holds must not reach its slot of the bias's gradient
+            g.p = counts ? g.p : 0.f;
+            g.dx = counts ? g.dx : 0.f;
+        }
+        g.da = cap > 0.f ? g.dx * slope : g.dx;
+        return g;
+    }
+};
+
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
+    typedef TileLds<DP> Lds;
+    constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
     __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
     const AttentionArgs &a = t.a;
-    const TileWork work = tile_work(t, a.kv_heads);
+    const TileWork work = tile_work(t);
     if (!work.any) return;
-    TileLds<T, DP> lds(lds_bytes, t.chunks);
-    tile_rows<T, DP>(t, work.tile, origin, lds);
+    Lds lds(lds_bytes, t.chunks);
+    tile_rows<DP, SEGMENTS>(t, work.tile, origin, lds);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
     const int s = a.torus.s, slots = t.heads * s;
-    if (a.bias)
-        for (int i = threadIdx.x; i < slots; i += 256)
-            lds.bias[i / s * (s + 1) + i % s] = (float)((const T *)a.bias)[(int64_t)first_head * s + i];
-    // behind the biases: dx of the wavefront's blocks of a chunk, and the sums of its slots over the chunks
-    float *dx_at = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4 + wave * 1024;
-    float *sums = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4 + kTileWaves * 1024 + wave * slots;
+    tile_biases<T>(a, first_head, t.heads, 1.f, lds.bias);
+    // behind the biases: dx of the wavefront's blocks of 64 rows, and the sums of its slots over the tile's rows
+    float *behind = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4, *dx_at = behind + wave * 1024, *sums = behind + kTileWaves * 1024 + wave * slots;
     if (t.slots_of)
         for (int i = lane; i < slots; i += 64) sums[i] = 0.f;
     const int64_t rank = rank_at(t, origin, t.column_at + column / t.heads * a.torus.d, true);
-    int32_t own = kNoColumn;
-    if (rank >= 0) own = a.segments ? a.segments[rank] : 0;
-    if (own < 0) own = kNoColumn;
+    const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 q[DP / 32], g_out[DP / 32];
     load_column<T, DP>(a.q, rank, head, a.head_dim, q);
     load_column<T, DP>(a.grad_out, rank, head, a.head_dim, g_out);
@@ -390,49 +500,56 @@ __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileAr
     }
     const float lse = rank >= 0 ? finite_floor(a.lse[rank * a.q_heads + head]) : 0.f;
     if (rank >= 0 && lane < 16) a.delta[rank * a.q_heads + head] = delta;
+    const LanePieces<T, DP> pieces;
+    const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.k.data + work.key_head * a.k.head_stride),
+                                          (const unsigned char *)((const T *)a.v.data + work.key_head * a.v.head_stride),
+                                          (const unsigned char *)t.zeros, (uint32_t)(a.k.rank_stride * 2), (uint32_t)(a.v.rank_stride * 2), a.head_dim};
+    const GradientFactors factors(a);
     __syncthreads();
 
-    const T *k0 = (const T *)a.k.data + work.key_head * a.k.head_stride, *v0 = (const T *)a.v.data + work.key_head * a.v.head_stride;
-    const float *bias = lds.bias + column % t.heads * (s + 1);
     f4 acc[DP / 16] = {};
-    Staged<T, DP> next;
-    next.load(k0, a.k.rank_stride, v0, a.v.rank_stride, lds.rank, a.head_dim);
+    Pairs<G> next;
+    loads.start(lds.rank, lds.chunk);
+    next.load(t, 0);
     for (int chunk = 0; chunk < t.chunks; ++chunk) {
-        __syncthreads();
-        next.store(lds);
-        __syncthreads();
-        if (chunk + 1 < t.chunks)
-            next.load(k0, a.k.rank_stride, v0, a.v.rank_stride, lds.rank + (chunk + 1) * kChunkRows, a.head_dim);
-        const uint32_t active = __builtin_amdgcn_readfirstlane(t.active[chunk] >> (4 * wave) & 15);
+        wait_for_rows();
+        const Pairs<G> pairs = next;
+        const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
+        const uint32_t active = active_groups<G>(t, chunk);
+        if (chunk + 1 < t.chunks) {
+            loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
+            next.load(t, chunk + 1);
+        }
 #pragma unroll
-        for (int pair = 0; pair < 2; ++pair) {
+        for (int pair = 0; pair < G / 2; ++pair) {
             if (!(active >> (2 * pair) & 3)) continue;
             f4 da[2] = {};
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
                 if (!(active >> g & 1)) continue;
-                const uint2 who = *(const uint2 *)(t.index + (((int64_t)(chunk * 4 + g) * kTileWaves + wave) * 64 + lane) * 4);
-                const f4 dot = rows_times_columns<T, DP>(lds.first + g * 16 * lds.kStride, q);
-                const f4 dp = rows_times_columns<T, DP>(lds.second + g * 16 * lds.kStride, g_out);
-                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * kChunkRows + g * 16 + lane / 16 * 4) : int4{};
+                const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
+                const f4 dp = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, g_out);
+                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
                 f4 dx;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int i = (r < 2 ? who.x : who.y) >> (r % 2 * 16) & 0xFFFF;
-                    const bool counts = i != s && (!SEGMENTS || (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
-                    const PairGradient pg = pair_gradient(dot[r], a.bias ? bias[i] : 0.f, lse, dp[r], delta, a.scale, a.cap);
-                    dx[r] = counts ? pg.dx : 0.f;
-                    da[half][r] = counts ? pg.da : 0.f;
+                    const PairGradient pg = factors.template operator()<SEGMENTS>(
+                        dot[r], pairs.bias((const unsigned char *)lds.bias, g, r), lse, dp[r], delta,
+                        (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                    dx[r] = pg.dx;
+                    da[half][r] = pg.da;
                 }
-                if (t.slots_of) *(f4 *)(dx_at + (g * 64 + lane) * 4) = rank >= 0 ? dx : f4{0.f, 0.f, 0.f, 0.f};
+                if (t.slots_of)
+                    *(f4 *)(dx_at + (((G == 4 ? g : chunk % 2 * 2 + g) * 64) + lane) * 4) = rank >= 0 ? dx : f4{0.f, 0.f, 0.f, 0.f};
             }
-            add_weighted_rows<T, DP>(lds.first + pair * 32 * lds.kStride, as_weights<T>(da[0], da[1]), acc);
+            pieces.add_weighted_rows(rows + pair * 32 * Lds::kRowBytes, as_weights<T>(da[0], da[1]), acc);
         }
-        if (t.slots_of) {
-            // every lane adds up the pairs of one slot: blocks that hold none of its pairs are not read
+        if (t.slots_of && (G == 4 || chunk % 2 || chunk + 1 == t.chunks)) {
+            // every lane adds up the pairs of one slot in 64 rows
             __builtin_amdgcn_wave_barrier();
-            const uint32_t begin = t.slots_of[chunk * kTileWaves + wave], end = t.slots_of[chunk * kTileWaves + wave + 1];
+            const int list = (G == 4 ? chunk : chunk / 2) * kTileWaves + wave;
+            const uint32_t begin = t.slots_of[list], end = t.slots_of[list + 1];
             for (uint32_t j = begin + lane; j < end; j += 64) {
                 const TilePlan::Slot slot = t.slots[j];
                 float sum = 0.f;
@@ -454,7 +571,7 @@ __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileAr
     });
     if (t.slots_of) {
         __syncthreads();
-        const float *all = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4 + kTileWaves * 1024;
+        const float *all = behind + kTileWaves * 1024;
         float *out = a.partials + (uint64_t)work.tile * a.q_heads * s + (int64_t)first_head * s;
         for (int i = threadIdx.x; i < slots; i += 256) out[i] = all[i] + all[slots + i] + all[2 * slots + i] + all[3 * slots + i];
     }
@@ -463,77 +580,83 @@ __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileAr
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256) void attention_grad_kv_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
+    typedef TileLds<DP> Lds;
+    constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
     __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
-    __shared__ __align__(16) float row_lse[kChunkRows], row_delta[kChunkRows];
+    __shared__ __align__(16) float row_lse[2][Lds::kRows], row_delta[2][Lds::kRows];
     const AttentionArgs &a = t.a;
-    const TileWork work = tile_work(t, a.kv_heads);
+    const TileWork work = tile_work(t);
     if (!work.any) return;
-    TileLds<T, DP> lds(lds_bytes, t.chunks);
-    tile_rows<T, DP>(t, work.tile, origin, lds);
+    Lds lds(lds_bytes, t.chunks);
+    tile_rows<DP, SEGMENTS>(t, work.tile, origin, lds);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group, s = a.torus.s;
-    if (a.bias)
-        for (int i = threadIdx.x; i < a.group * s; i += 256)
-            lds.bias[i / s * (s + 1) + i % s] = (float)((const T *)a.bias)[(int64_t)first_head * s + i];
+    tile_biases<T>(a, first_head, a.bias ? a.group : 1, 1.f, lds.bias);
     const int64_t rank = rank_at(t, origin, t.column_at + column * a.torus.d, true);
-    int32_t own = kNoColumn;
-    if (rank >= 0) own = a.segments ? a.segments[rank] : 0;
-    if (own < 0) own = kNoColumn;
+    const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 k[DP / 32], v[DP / 32];
     load_column<T, DP>(a.k, rank, work.key_head, a.head_dim, k);
     load_column<T, DP>(a.v, rank, work.key_head, a.head_dim, v);
+    const LanePieces<T, DP> pieces;
+    const GradientFactors factors(a);
     __syncthreads();
 
     f4 dk[DP / 16] = {}, dv[DP / 16] = {};
-    Staged<T, DP> next;
+    Pairs<G> next;
     float next_lse = 0.f, next_delta = 0.f;
-    const auto fetch = [&](int step) {
-        const int h = first_head + step / t.chunks, chunk = step % t.chunks;
-        next.load((const T *)a.q.data + h * a.q.head_stride, a.q.rank_stride, (const T *)a.grad_out.data + h * a.grad_out.head_stride,
-                  a.grad_out.rank_stride, lds.rank + chunk * kChunkRows, a.head_dim);
-        if (threadIdx.x < kChunkRows) {
-            const int32_t r = lds.rank[chunk * kChunkRows + threadIdx.x];
+    // the rows of all chunks for the first head of the group, then for the next
+    const auto start = [&](int h, int chunk, int buffer) {
+        const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.q.data + h * a.q.head_stride),
+                                              (const unsigned char *)((const T *)a.grad_out.data + h * a.grad_out.head_stride),
+                                              (const unsigned char *)t.zeros, (uint32_t)(a.q.rank_stride * 2),
+                                              (uint32_t)(a.grad_out.rank_stride * 2), a.head_dim};
+        loads.start(lds.rank + chunk * Lds::kRows, lds.chunk + buffer * 2 * Lds::kTensor);
+        next.load(t, chunk);
+        if (threadIdx.x < Lds::kRows) {
+            const int32_t r = lds.rank[chunk * Lds::kRows + threadIdx.x];
             next_lse = r >= 0 ? finite_floor(a.lse[(int64_t)r * a.q_heads + h]) : 0.f;
             next_delta = r >= 0 ? a.delta[(int64_t)r * a.q_heads + h] : 0.f;
         }
     };
-    const int steps = a.group * t.chunks;
-    fetch(0);
-    for (int step = 0; step < steps; ++step) {
-        const int chunk = step % t.chunks;
-        const float *bias = lds.bias + step / t.chunks * (s + 1);
-        __syncthreads();
-        next.store(lds);
-        if (threadIdx.x < kChunkRows) row_lse[threadIdx.x] = next_lse, row_delta[threadIdx.x] = next_delta;
-        __syncthreads();
-        if (step + 1 < steps) fetch(step + 1);
-        const uint32_t active = __builtin_amdgcn_readfirstlane(t.active[chunk] >> (4 * wave) & 15);
+    start(first_head, 0, 0);
+    int chunk = 0, h = 0;
+    for (int step = 0; h < a.group; ++step) {
+        const int buffer = step % 2;
+        if (threadIdx.x < Lds::kRows) row_lse[buffer][threadIdx.x] = next_lse, row_delta[buffer][threadIdx.x] = next_delta;
+        wait_for_rows();
+        const Pairs<G> pairs = next;
+        const unsigned char *rows = lds.chunk + buffer * 2 * Lds::kTensor;
+        const unsigned char *bias = (const unsigned char *)(lds.bias + (a.bias ? h * (s + 1) : 0));
+        const uint32_t active = active_groups<G>(t, chunk);
+        const int now = chunk;
+        if (++chunk == t.chunks) chunk = 0, ++h;
+        if (h < a.group) start(first_head + h, chunk, 1 - buffer);
 #pragma unroll
-        for (int pair = 0; pair < 2; ++pair) {
+        for (int pair = 0; pair < G / 2; ++pair) {
             if (!(active >> (2 * pair) & 3)) continue;
             f4 p[2] = {}, da[2] = {};
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
                 if (!(active >> g & 1)) continue;
-                const uint2 who = *(const uint2 *)(t.index + (((int64_t)(chunk * 4 + g) * kTileWaves + wave) * 64 + lane) * 4);
-                const f4 dot = rows_times_columns<T, DP>(lds.first + g * 16 * lds.kStride, k);
-                const f4 dp = rows_times_columns<T, DP>(lds.second + g * 16 * lds.kStride, v);
-                const f4 lse = *(const f4 *)(row_lse + g * 16 + lane / 16 * 4), delta = *(const f4 *)(row_delta + g * 16 + lane / 16 * 4);
-                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * kChunkRows + g * 16 + lane / 16 * 4) : int4{};
+                const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, k);
+                const f4 dp = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, v);
+                const f4 lse = *(const f4 *)(row_lse[buffer] + g * 16 + lane / 16 * 4);
+                const f4 delta = *(const f4 *)(row_delta[buffer] + g * 16 + lane / 16 * 4);
+                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + now * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int i = (r < 2 ? who.x : who.y) >> (r % 2 * 16) & 0xFFFF;
-                    const bool counts = i != s && (!SEGMENTS || (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
-                    const PairGradient pg = pair_gradient(dot[r], a.bias ? bias[i] : 0.f, lse[r], dp[r], delta[r], a.scale, a.cap);
-                    p[half][r] = counts ? pg.p : 0.f;
-                    da[half][r] = counts ? pg.da : 0.f;
+                    const PairGradient pg = factors.template operator()<SEGMENTS>(
+                        dot[r], pairs.bias(bias, g, r), lse[r], dp[r], delta[r],
+                        (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                    p[half][r] = pg.p;
+                    da[half][r] = pg.da;
                 }
             }
-            add_weighted_rows<T, DP>(lds.second + pair * 32 * lds.kStride, as_weights<T>(p[0], p[1]), dv);
-            add_weighted_rows<T, DP>(lds.first + pair * 32 * lds.kStride, as_weights<T>(da[0], da[1]), dk);
+            pieces.add_weighted_rows(rows + Lds::kTensor + pair * 32 * Lds::kRowBytes, as_weights<T>(p[0], p[1]), dv);
+            pieces.add_weighted_rows(rows + pair * 32 * Lds::kRowBytes, as_weights<T>(da[0], da[1]), dk);
         }
     }
     const bool fine_v = store_column<T, DP>(a.grad_v, rank, work.key_head, a.head_dim, dv, 1.f);

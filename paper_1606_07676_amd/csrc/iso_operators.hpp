@@ -224,12 +224,13 @@ ISO_TILE_KERNEL(GradKVTileKernel, attention_grad_kv_tile_kernel)
 constexpr int kTileMaxHeadDim = 128;
 constexpr size_t kTileMaxLds = 64 << 10;
 inline int tile_head_dim(int head_dim) { return (head_dim + 31) / 32 * 32; }
+inline int tile_chunk_rows(int head_dim) { return tile_head_dim(head_dim) > 64 ? TileLds<128>::kRows : TileLds<64>::kRows; }
 inline size_t tile_lds_bytes(int head_dim, int chunks, size_t biases) {
     switch (tile_head_dim(head_dim)) {
-        case 32: return TileLds<__bf16, 32>::bytes(chunks, biases);
-        case 64: return TileLds<__bf16, 64>::bytes(chunks, biases);
-        case 96: return TileLds<__bf16, 96>::bytes(chunks, biases);
-        default: return TileLds<__bf16, 128>::bytes(chunks, biases);
+        case 32: return TileLds<32>::bytes(chunks, biases);
+        case 64: return TileLds<64>::bytes(chunks, biases);
+        case 96: return TileLds<96>::bytes(chunks, biases);
+        default: return TileLds<128>::bytes(chunks, biases);
     }
 }
 
@@ -291,13 +292,13 @@ class AttentionBinder {
         table.add(kernel_offsets(c));
         choose_width();
         const int group = t.q_heads / t.kv_heads, heads = tile_heads(group);
-        const size_t biases = t.bias ? (size_t)heads * (c.s + 1) : 0;
+        const size_t biases = (size_t)heads * (c.s + 1);
         if (!g) {
             forward_side.take(*this, table, heads, false, false, biases);
         } else {
             const bool sums = g->grad_bias && c.s;                 // dx of the blocks of a chunk, and the slots of every wavefront
             forward_side.take(*this, table, heads, false, sums, biases + 3 + (sums ? kTileWaves * (1024 + (size_t)heads * c.s) : 0));
-            backward_side.take(*this, table, 1, true, false, t.bias ? (size_t)group * (c.s + 1) : 0);
+            backward_side.take(*this, table, 1, true, false, (t.bias ? (size_t)group : 1) * (c.s + 1));
         }
         ISO_TRY(upload_table(b, table.bytes.data(), table.bytes.size()));
         fill_args(workspace);
@@ -374,17 +375,23 @@ class AttentionBinder {
     struct Side {
         bool tiles = false;
         TilePlan plan;
-        size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots_of = 0, slots = 0, pairs = 0;
+        size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots_of = 0, slots = 0, pairs = 0, zeros = 0;
+        int chunks = 0;
 
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
             if (o.t.rows || o.t.dtype == ISO_DTYPE_F32 || !o.is_wide || o.t.head_dim > kTileMaxHeadDim) return;
+            for (const iso_heads_t *x : {&o.t.q, &o.t.k, &o.t.v, o.g ? &o.g->grad_out : &o.t.q})
+                if (x->rank_stride >> 31) return;                  // strides in bytes: 32 bits
             if (!build_tile_plan(o.c, heads, back, sums, plan)) return;
-            lds = tile_lds_bytes(o.t.head_dim, plan.chunks, floats);
+            const int chunk = tile_chunk_rows(o.t.head_dim);
+            chunks = (plan.rows + chunk - 1) / chunk;
+            lds = tile_lds_bytes(o.t.head_dim, chunks, floats);
             if (lds > kTileMaxLds || plan.blocks * 256.0 > 12.0 * kTileColumns * o.c.s) return;
             columns = table.add(plan.column_at);
             rows = table.add(plan.row_at);
             active = table.add(plan.active);
             index = table.add(plan.index);
+            zeros = table.add(std::vector<uint16_t>(kTileMaxHeadDim));
             if (sums) {
                 slots_of = table.add(plan.slots_of);
                 slots = table.add(plan.slots);
@@ -402,12 +409,13 @@ class AttentionBinder {
         ta.n_tiles = (uint32_t)p.n_tiles;
         ta.heads = p.heads;
         ta.parts = parts;
-        ta.chunks = p.chunks;
+        ta.chunks = side.chunks;
         const char *base = (const char *)b.dev_table;
         ta.column_at = (const int32_t *)(base + side.columns);
         ta.row_at = (const int32_t *)(base + side.rows);
         ta.active = (const uint32_t *)(base + side.active);
         ta.index = (const uint16_t *)(base + side.index);
+        ta.zeros = base + side.zeros;
         if (!p.slots_of.empty()) {
             ta.slots_of = (const uint32_t *)(base + side.slots_of);
             ta.slots = (const TilePlan::Slot *)(base + side.slots);

@@ -36,8 +36,9 @@ struct TilePlan {
     std::vector<uint32_t> slots_of;        // [chunks * kTileWaves + 1]: first of `slots`
     std::vector<Slot> slots;
     std::vector<uint16_t> pairs;           // slot_pair of each
-    std::vector<uint16_t> index;           // [chunks * 4][kTileWaves][64][4]: neighbour of (lane's column, row 4 * (lane / 16) + r)
-                                           // of the 16 rows of a group, s where it is none
+    // [chunks * 4][kTileWaves][64][4]: of (lane's column, row 4 * (lane / 16) + r) of the 16 rows of a group, four times
+    // (column's head) * (s + 1) + neighbour, with s for the neighbour where it is none
+    std::vector<uint16_t> index;
 };
 
 // Where a wavefront keeps the pair of a column (0..15) and a row of the chunk (0..63): lane (row % 16 / 4) * 16 + column writes
@@ -114,7 +115,7 @@ inline TileShape tile_shape(const Comm &c, int heads) { return tile_shape(c, kTi
 // them.  False where no table of that form exists (neighbours too many, or too far apart).
 inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots, TilePlan &out) {
     const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
-    if (c.s < 1 || c.s > 65534) return false;
+    if (c.s < 1 || (int64_t)heads * (c.s + 1) * 4 > 65535) return false;
     Steps steps = source_steps(c);
     if (back)                              // from a source to its readers
         for (int i = 0; i < c.s; ++i)
@@ -193,7 +194,8 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     p.chunks = (p.rows + kChunkRows - 1) / kChunkRows;
     p.row_at.assign((size_t)p.chunks * kChunkRows * d, 0);
     p.active.assign((size_t)p.chunks, 0);
-    p.index.assign((size_t)p.chunks * 4 * kTileWaves * 64 * 4, (uint16_t)c.s);
+    p.index.resize((size_t)p.chunks * 4 * kTileWaves * 64 * 4);
+    for (size_t i = 0; i < p.index.size(); ++i) p.index[i] = (uint16_t)(4 * ((int)(i / 4 % 16) % heads * (c.s + 1) + c.s));
     std::vector<int> rank_of((size_t)p.rows);
     for (int u = 0; u < p.rows; ++u) {
         rank_of[order[u]] = u;
@@ -205,7 +207,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
         for (int h = 0; h < heads; ++h) {
             const int column = r * heads + h, w = column / 16;
             const int lane = lane_row / 4 * 16 + column % 16;
-            p.index[(((size_t)group * kTileWaves + w) * 64 + lane) * 4 + lane_row % 4] = (uint16_t)i;
+            p.index[(((size_t)group * kTileWaves + w) * 64 + lane) * 4 + lane_row % 4] = (uint16_t)(4 * (h * (c.s + 1) + i));
             p.active[group / 4] |= 1u << (4 * w + group % 4);
         }
     }

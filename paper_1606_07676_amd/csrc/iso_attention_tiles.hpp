@@ -215,22 +215,20 @@ __device__ __forceinline__ void wait_for_rows() {
 // The table's entries of a chunk: byte offsets of the biases of this lane's column and rows 4 (lane / 16) + 0..3 of each group.
 template <int GROUPS> struct Pairs {
     uint2 of[GROUPS];
+    uint32_t active_word;
     __device__ __forceinline__ void load(const TileArgs &t, int chunk) {
+        active_word = t.active[GROUPS == 4 ? chunk : chunk >> 1] >> ((threadIdx.x >> 6) * 4 + (GROUPS == 4 ? 0 : chunk % 2 * 2));
         const uint2 *at = (const uint2 *)t.index + ((int64_t)chunk * GROUPS * kTileWaves + (threadIdx.x >> 6)) * 64 + (threadIdx.x & 63);
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) of[g] = at[g * kTileWaves * 64];
     }
+    // Bit g: group g holds a neighbour of one of the wavefront's columns.
+    __device__ __forceinline__ uint32_t active() const { return __builtin_amdgcn_readfirstlane(active_word) & ((1u << GROUPS) - 1); }
     __device__ __forceinline__ float bias(const unsigned char *base, int g, int r) const {
         const uint32_t two = r < 2 ? of[g].x : of[g].y;
         return *(const float *)(base + (r % 2 ? two >> 16 : two & 0xFFFF));
     }
 };
-// Bit g: group g of the chunk holds a neighbour of one of the wavefront's columns.
-template <int GROUPS> __device__ __forceinline__ uint32_t active_groups(const TileArgs &t, int chunk) {
-    const uint32_t word = t.active[GROUPS == 4 ? chunk : chunk >> 1];
-    const uint32_t mine = __builtin_amdgcn_readfirstlane(word >> ((threadIdx.x >> 6) * 4)) & 15;
-    return GROUPS == 4 ? mine : mine >> (chunk % 2 * 2) & 3;
-}
 
 // A column's row as right-hand operand: lane holds column lane % 16, elements 32 k + 8 (lane / 16) + 0..7.
 template <typename T, int DP>
@@ -317,7 +315,7 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
 }
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256) void attention_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, 2) void attention_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
@@ -353,7 +351,7 @@ __global__ __launch_bounds__(256) void attention_tile_kernel(const TileArgs t) {
         wait_for_rows();
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
-        const uint32_t active = active_groups<G>(t, chunk);
+        const uint32_t active = pairs.active();
         if (chunk + 1 < t.chunks) {
             loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
             next.load(t, chunk + 1);
@@ -361,30 +359,41 @@ __global__ __launch_bounds__(256) void attention_tile_kernel(const TileArgs t) {
         if (!active) continue;
         f4 x[G];
         float top = m;
+        // 32 rows at a time, so that the reads of one product are under way while the other waits
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            x[g] = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            if (!(active >> g & 1)) continue;
-            const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
-            if (a.cap > 0.f) {
+        for (int pair = 0; pair < G / 2; ++pair) {
+            if (!(active >> (2 * pair) & 3)) continue;
+            f4 dot[2], bias[2];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(dot[r] * to_cap);
-                    x[g][r] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap) + pairs.bias((const unsigned char *)lds.bias, g, r);
+            for (int half = 0; half < 2; ++half) {
+                const int g = 2 * pair + half;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) bias[half][r] = pairs.bias((const unsigned char *)lds.bias, g, r);
+                dot[half] = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int g = 2 * pair + half;
+                if (a.cap > 0.f) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float e = __builtin_amdgcn_exp2f(dot[half][r] * to_cap);
+                        x[g][r] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap) + bias[half][r];
+                    }
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[g][r] = fmaf(dot[half][r], scale, bias[half][r]);
                 }
-            } else {
+                if (SEGMENTS) {
+                    const int4 seg = *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4);
+                    x[g][0] = seg.x == own ? x[g][0] : -INFINITY;
+                    x[g][1] = seg.y == own ? x[g][1] : -INFINITY;
+                    x[g][2] = seg.z == own ? x[g][2] : -INFINITY;
+                    x[g][3] = seg.w == own ? x[g][3] : -INFINITY;
+                }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[g][r] = fmaf(dot[r], scale, pairs.bias((const unsigned char *)lds.bias, g, r));
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, x[g][r]);
             }
-            if (SEGMENTS) {
-                const int4 seg = *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4);
-                x[g][0] = seg.x == own ? x[g][0] : -INFINITY;
-                x[g][1] = seg.y == own ? x[g][1] : -INFINITY;
-                x[g][2] = seg.z == own ? x[g][2] : -INFINITY;
-                x[g][3] = seg.w == own ? x[g][3] : -INFINITY;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, x[g][r]);
         }
         top = column_max(top);
         const float base = finite_floor(top);
@@ -463,7 +472,7 @@ struct GradientFactors {
 };
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
@@ -515,7 +524,7 @@ __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileAr
         wait_for_rows();
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
-        const uint32_t active = active_groups<G>(t, chunk);
+        const uint32_t active = pairs.active();
         if (chunk + 1 < t.chunks) {
             loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
             next.load(t, chunk + 1);
@@ -527,7 +536,6 @@ __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileAr
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
-                if (!(active >> g & 1)) continue;
                 const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
                 const f4 dp = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, g_out);
                 const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
@@ -578,7 +586,7 @@ __global__ __launch_bounds__(256) void attention_grad_q_tile_kernel(const TileAr
 }
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256) void attention_grad_kv_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
@@ -629,7 +637,7 @@ __global__ __launch_bounds__(256) void attention_grad_kv_tile_kernel(const TileA
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + buffer * 2 * Lds::kTensor;
         const unsigned char *bias = (const unsigned char *)(lds.bias + (a.bias ? h * (s + 1) : 0));
-        const uint32_t active = active_groups<G>(t, chunk);
+        const uint32_t active = pairs.active();
         const int now = chunk;
         if (++chunk == t.chunks) chunk = 0, ++h;
         if (h < a.group) start(first_head + h, chunk, 1 - buffer);
@@ -640,7 +648,6 @@ __global__ __launch_bounds__(256) void attention_grad_kv_tile_kernel(const TileA
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
-                if (!(active >> g & 1)) continue;
                 const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, k);
                 const f4 dp = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, v);
                 const f4 lse = *(const f4 *)(row_lse[buffer] + g * 16 + lane / 16 * 4);

@@ -16,17 +16,25 @@
 #pragma once
 
 #include "iso_attention_kernels.hpp"
+#include "iso_fastdiv.hpp"
 #include "iso_tiles.hpp"
 
 namespace iso {
 
+struct TileDim {                           // of the torus, the last dimension first
+    FastDiv tiles;
+    int32_t tile, size, inner, wraps;
+};
+
 struct TileArgs {
     AttentionArgs a;
-    int32_t tile[ISO_MAX_DIMS], tiles[ISO_MAX_DIMS];
-    uint32_t n_tiles, per_xcd;             // workgroups of one XCD
-    int32_t heads, parts;                  // columns of one rank; sets of `heads` q heads that share a key head
+    TileDim dim[ISO_MAX_DIMS];
+    FastDiv n_tiles, parts, biases;        // parts: sets of `heads` q heads that share a key head; biases: s + 1
+    uint32_t items, per_xcd;               // (key head, tile, part), and how many of them one XCD takes
+    int32_t heads;                         // columns of one rank
     int32_t chunks;                        // of TileLds<DP>::kRows rows
-    const int32_t *column_at, *row_at;
+    int32_t words;                         // of a position
+    const uint2 *column_at, *row_at;       // [][words]: positions relative to the tile's first rank, four dimensions in a word
     const uint32_t *active;
     const uint16_t *index;
     const uint32_t *slots_of;              // the bias's gradient, or null: see TilePlan
@@ -41,19 +49,12 @@ template <> struct Matrix<__bf16> {
     typedef __bf16 x4 __attribute__((ext_vector_type(4)));
     typedef float f4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f4 multiply(x8 a, x8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ x4 read_transposed(const unsigned char *at) {
-        return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4 *)at);
-    }
 };
 template <> struct Matrix<_Float16> {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x4 __attribute__((ext_vector_type(4)));
     typedef float f4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f4 multiply(x8 a, x8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-    static __device__ __forceinline__ x4 read_transposed(const unsigned char *at) {
-        typedef __fp16 h4 __attribute__((ext_vector_type(4)));
-        return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4 *)at));
-    }
 };
 
 // Maximum and sum over the four lanes that hold the rows of one column.
@@ -104,21 +105,37 @@ constexpr int32_t kNoToken = INT32_MIN;    // segment of a row that is outside t
 constexpr int32_t kNoColumn = INT32_MIN + 1;
 
 // Rank at a position relative to the tile's first rank, -1 outside the mesh (and for positions that only columns outside the
-// torus, of a ragged tile, refer to).
-__device__ __forceinline__ int32_t rank_at(const TileArgs &t, const int32_t *origin, const int32_t *at, bool column) {
+// torus, of a ragged tile, refer to).  The tile's own position is scalar work.
+template <bool COLUMN>
+__device__ __forceinline__ void add_dim(const TileDim &d, uint32_t &tile, int32_t at, int32_t &rank, bool &there) {
+    uint32_t rest, place;
+    fast_divmod(tile, d.tiles, rest, place);
+    tile = rest;
+    int32_t x = (int32_t)place * d.tile + at;
+    if (!COLUMN && d.wraps) {
+        x += x < 0 ? d.size : 0;
+        x -= x >= d.size ? d.size : 0;
+    }
+    there = there && (uint32_t)x < (uint32_t)d.size;
+    rank += x * d.inner;
+}
+template <bool COLUMN> __device__ __forceinline__ int32_t rank_at(const TileArgs &t, uint32_t tile, const uint2 *at, uint2 word) {
     int32_t rank = 0;
     bool there = true;
-    for (int j = 0; j < t.a.torus.d; ++j) {
-        const int32_t n = t.a.torus.dims[j];
-        int32_t x = origin[j] + at[j];
-        if (!column && !(t.a.torus.open >> j & 1)) {
-            x += x < 0 ? n : 0;
-            x -= x >= n ? n : 0;
-        }
-        there = there && (uint32_t)x < (uint32_t)n;
-        rank += x * t.a.torus.inner[j];
+    const int d = t.a.torus.d;
+    add_dim<COLUMN>(t.dim[0], tile, (int16_t)(word.x & 0xFFFF), rank, there);
+    if (d > 1) add_dim<COLUMN>(t.dim[1], tile, (int32_t)word.x >> 16, rank, there);
+    if (d > 2) add_dim<COLUMN>(t.dim[2], tile, (int16_t)(word.y & 0xFFFF), rank, there);
+    if (d > 3) add_dim<COLUMN>(t.dim[3], tile, (int32_t)word.y >> 16, rank, there);
+    for (int j = 4; j < d; ++j) {
+        const uint2 more = at[j / 4];
+        const uint32_t two = j % 4 < 2 ? more.x : more.y;
+        add_dim<COLUMN>(t.dim[j], tile, j % 2 ? (int32_t)two >> 16 : (int16_t)(two & 0xFFFF), rank, there);
     }
     return there ? rank : -1;
+}
+template <bool COLUMN> __device__ __forceinline__ int32_t rank_at(const TileArgs &t, uint32_t tile, const uint2 *at) {
+    return rank_at<COLUMN>(t, tile, at, at[0]);
 }
 
 // What a workgroup works on: workgroups are handed to the 8 XCDs in turn, and each XCD takes a run of consecutive tiles of
@@ -130,27 +147,23 @@ struct TileWork {
 };
 __device__ __forceinline__ TileWork tile_work(const TileArgs &t) {
     TileWork w;
-    const uint32_t item = (blockIdx.x & 7) * t.per_xcd + (blockIdx.x >> 3), pairs = item / t.parts;
-    w.part = item % t.parts;
-    w.tile = pairs % t.n_tiles;
-    w.key_head = pairs / t.n_tiles;
-    w.any = w.key_head < t.a.kv_heads;
+    const uint32_t item = (blockIdx.x & 7) * t.per_xcd + (blockIdx.x >> 3);
+    uint32_t pair, part, head, tile;
+    fast_divmod(item, t.parts, pair, part);
+    fast_divmod(pair, t.n_tiles, head, tile);
+    w.part = part;
+    w.tile = tile;
+    w.key_head = head;
+    w.any = item < t.items;
     return w;
 }
 
 // Ranks and segments of the tile's rows.  A row that is not there keeps rank -1 where segments are compared, and is then
 // staged as zeros; on a torus without segments only columns outside the torus refer to such rows, and any rank serves.
-template <int DP, bool SEGMENTS>
-__device__ __forceinline__ void tile_rows(const TileArgs &t, uint32_t tile, int32_t *origin, TileLds<DP> &lds) {
-    const int d = t.a.torus.d;
-    if ((int)threadIdx.x < d) {
-        uint32_t rest = tile;
-        for (int j = d - 1; j > (int)threadIdx.x; --j) rest /= (uint32_t)t.tiles[j];
-        origin[threadIdx.x] = (int32_t)(rest % (uint32_t)t.tiles[threadIdx.x]) * t.tile[threadIdx.x];
-    }
-    __syncthreads();
-    for (int u = threadIdx.x; u < t.chunks * TileLds<DP>::kRows; u += 256) {
-        const int32_t rank = rank_at(t, origin, t.row_at + (int64_t)u * d, false);
+template <int DP, bool SEGMENTS> __device__ __forceinline__ void tile_rows(const TileArgs &t, uint32_t tile, TileLds<DP> &lds) {
+    const int rows = t.chunks * TileLds<DP>::kRows;
+    const auto one = [&](int u, uint2 word) {
+        const int32_t rank = rank_at<false>(t, tile, t.row_at + (int64_t)u * t.words, word);
         if (SEGMENTS) {
             int32_t segment = rank < 0 ? kNoToken : t.a.segments ? t.a.segments[rank] : 0;
             if (segment < 0) segment = kNoToken;
@@ -159,6 +172,12 @@ __device__ __forceinline__ void tile_rows(const TileArgs &t, uint32_t tile, int3
         } else {
             lds.rank[u] = max(rank, 0);
         }
+    };
+    for (int u = threadIdx.x; u < rows; u += 512) {                 // two trips to memory under way at a time
+        const bool second = u + 256 < rows;
+        const uint2 a = t.row_at[(int64_t)u * t.words], b = t.row_at[(int64_t)(second ? u + 256 : u) * t.words];
+        one(u, a);
+        if (second) one(u + 256, b);
     }
 }
 
@@ -169,11 +188,13 @@ __device__ __forceinline__ int32_t column_segment(const AttentionArgs &a, int64_
 
 // Biases of `heads` q heads in LDS, a -inf behind each; zeros where there are none.
 template <typename T>
-__device__ __forceinline__ void tile_biases(const AttentionArgs &a, int first_head, int heads, float factor, float *at) {
+__device__ __forceinline__ void tile_biases(const TileArgs &t, int first_head, int heads, float factor, float *at) {
+    const AttentionArgs &a = t.a;
     const int s = a.torus.s;
     for (int i = threadIdx.x; i < heads * (s + 1); i += 256) {
-        const int h = i / (s + 1), j = i % (s + 1);
-        float b = j == s ? -INFINITY : a.bias ? (float)((const T *)a.bias)[(int64_t)(first_head + h) * s + j] : 0.f;
+        uint32_t h, j;
+        fast_divmod(i, t.biases, h, j);
+        float b = (int)j == s ? -INFINITY : a.bias ? (float)((const T *)a.bias)[(int64_t)(first_head + h) * s + j] : 0.f;
         // a factor must not make an infinity of a bias near the type's lowest value
         if (factor != 1.f && b != -INFINITY) b = fminf(fmaxf(b * factor, -3.4e38f), 3.4e38f);
         at[i] = b;
@@ -217,13 +238,16 @@ template <int GROUPS> struct Pairs {
     uint2 of[GROUPS];
     uint32_t active_word;
     __device__ __forceinline__ void load(const TileArgs &t, int chunk) {
-        active_word = t.active[GROUPS == 4 ? chunk : chunk >> 1] >> ((threadIdx.x >> 6) * 4 + (GROUPS == 4 ? 0 : chunk % 2 * 2));
+        active_word = t.active[GROUPS == 4 ? chunk : chunk >> 1];
         const uint2 *at = (const uint2 *)t.index + ((int64_t)chunk * GROUPS * kTileWaves + (threadIdx.x >> 6)) * 64 + (threadIdx.x & 63);
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) of[g] = at[g * kTileWaves * 64];
     }
     // Bit g: group g holds a neighbour of one of the wavefront's columns.
-    __device__ __forceinline__ uint32_t active() const { return __builtin_amdgcn_readfirstlane(active_word) & ((1u << GROUPS) - 1); }
+    __device__ __forceinline__ uint32_t active(int chunk) const {
+        const int shift = (threadIdx.x >> 6) * 4 + (GROUPS == 4 ? 0 : chunk % 2 * 2);
+        return __builtin_amdgcn_readfirstlane(active_word >> shift) & ((1u << GROUPS) - 1);
+    }
     __device__ __forceinline__ float bias(const unsigned char *base, int g, int r) const {
         const uint32_t two = r < 2 ? of[g].x : of[g].y;
         return *(const float *)(base + (r % 2 ? two >> 16 : two & 0xFFFF));
@@ -240,6 +264,22 @@ __device__ __forceinline__ void load_column(const Heads &h, int64_t rank, int he
         x[k] = {};
         if (rank >= 0 && 32 * k + at < head_dim) x[k] = *(const typename Matrix<T>::x8 *)(row + 32 * k + at);
     }
+}
+
+// Transposing reads: lane i of 16 gets column i of four rows whose 16 columns the lanes' addresses name, four columns each.
+// The compiler takes the builtin for a read of whatever is on its way into LDS and waits for the next chunk's rows before
+// it (a quarter of the time of 256 x 256, 169 neighbours); here the reads are waited for where they are issued.
+struct Turned {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    u4 first, second;
+};
+template <int HALF> __device__ __forceinline__ Turned read_transposed(uint32_t first, uint32_t second) {
+    uint2 a, b, c, d;
+    asm volatile("ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %4 offset:%6\n\t"
+                 "ds_read_b64_tr_b16 %2, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
+                 : "v"(first), "v"(second), "n"(HALF));
+    return {Turned::u4{a.x, a.y, b.x, b.y}, Turned::u4{c.x, c.y, d.x, d.y}};
 }
 
 // Where a lane finds its pieces of staged rows: the same for every group of 16.
@@ -262,11 +302,12 @@ template <typename T, int DP> struct LanePieces {
     }
     // acc^T += rows^T w for 32 rows: w holds, for each lane's column, its weights of 4 rows of either half.
     __device__ __forceinline__ void add_weighted_rows(const unsigned char *rows, typename Matrix<T>::x8 w, typename Matrix<T>::f4 (&acc)[DP / 16]) const {
+        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)rows;
 #pragma unroll
-        for (int e = 0; e < DP / 16; ++e) {
-            const typename Matrix<T>::x4 low = Matrix<T>::read_transposed(rows + turned[e]);
-            const typename Matrix<T>::x4 high = Matrix<T>::read_transposed(rows + turned[e] + 16 * TileLds<DP>::kRowBytes);
-            acc[e] = Matrix<T>::multiply(__builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7), w, acc[e]);
+        for (int e = 0; e < DP / 16; e += 2) {
+            const Turned x = read_transposed<16 * TileLds<DP>::kRowBytes>(base + turned[e], base + turned[e + 1]);
+            acc[e] = Matrix<T>::multiply(__builtin_bit_cast(typename Matrix<T>::x8, x.first), w, acc[e]);
+            acc[e + 1] = Matrix<T>::multiply(__builtin_bit_cast(typename Matrix<T>::x8, x.second), w, acc[e + 1]);
         }
     }
 };
@@ -315,25 +356,24 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
 }
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256, 2) void attention_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
-    __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
+    __shared__ int32_t coords[kTileWaves][ISO_MAX_DIMS];
     const AttentionArgs &a = t.a;
     const TileWork work = tile_work(t);
     if (!work.any) return;
     Lds lds(lds_bytes, t.chunks);
-    tile_rows<DP, SEGMENTS>(t, work.tile, origin, lds);
-
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
-    tile_biases<T>(a, first_head, t.heads, kLog2e, lds.bias);
-    const int64_t rank = rank_at(t, origin, t.column_at + column / t.heads * a.torus.d, true);
+    const int64_t rank = rank_at<true>(t, work.tile, t.column_at + column / t.heads * t.words);
     const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 q[DP / 32];
     load_column<T, DP>(a.q, rank, head, a.head_dim, q);
+    tile_rows<DP, SEGMENTS>(t, work.tile, lds);
+    tile_biases<T>(t, first_head, t.heads, kLog2e, lds.bias);
     const LanePieces<T, DP> pieces;
     const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.k.data + work.key_head * a.k.head_stride),
                                           (const unsigned char *)((const T *)a.v.data + work.key_head * a.v.head_stride),
@@ -351,7 +391,7 @@ __global__ __launch_bounds__(256, 2) void attention_tile_kernel(const TileArgs t
         wait_for_rows();
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
-        const uint32_t active = pairs.active();
+        const uint32_t active = pairs.active(chunk);
         if (chunk + 1 < t.chunks) {
             loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
             next.load(t, chunk + 1);
@@ -477,37 +517,36 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
-    __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
+    __shared__ int32_t coords[kTileWaves][ISO_MAX_DIMS];
     const AttentionArgs &a = t.a;
     const TileWork work = tile_work(t);
     if (!work.any) return;
     Lds lds(lds_bytes, t.chunks);
-    tile_rows<DP, SEGMENTS>(t, work.tile, origin, lds);
-
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
     const int s = a.torus.s, slots = t.heads * s;
-    tile_biases<T>(a, first_head, t.heads, 1.f, lds.bias);
     // behind the biases: dx of the wavefront's blocks of 64 rows, and the sums of its slots over the tile's rows
     float *behind = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4, *dx_at = behind + wave * 1024, *sums = behind + kTileWaves * 1024 + wave * slots;
     if (t.slots_of)
         for (int i = lane; i < slots; i += 64) sums[i] = 0.f;
-    const int64_t rank = rank_at(t, origin, t.column_at + column / t.heads * a.torus.d, true);
+    const int64_t rank = rank_at<true>(t, work.tile, t.column_at + column / t.heads * t.words);
     const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 q[DP / 32], g_out[DP / 32];
     load_column<T, DP>(a.q, rank, head, a.head_dim, q);
     load_column<T, DP>(a.grad_out, rank, head, a.head_dim, g_out);
-    float delta = 0.f;
+    float delta = 0.f, lse = rank >= 0 ? a.lse[rank * a.q_heads + head] : 0.f;
     {
         typename Matrix<T>::x8 out[DP / 32];
         load_column<T, DP>(a.out, rank, head, a.head_dim, out);
+        tile_rows<DP, SEGMENTS>(t, work.tile, lds);                 // while these are on their way
+        tile_biases<T>(t, first_head, t.heads, 1.f, lds.bias);
 #pragma unroll
         for (int k = 0; k < DP / 32; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) delta = fmaf((float)g_out[k][e], (float)out[k][e], delta);
         delta = column_sum(delta);
     }
-    const float lse = rank >= 0 ? finite_floor(a.lse[rank * a.q_heads + head]) : 0.f;
+    lse = finite_floor(lse);
     if (rank >= 0 && lane < 16) a.delta[rank * a.q_heads + head] = delta;
     const LanePieces<T, DP> pieces;
     const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.k.data + work.key_head * a.k.head_stride),
@@ -524,7 +563,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
         wait_for_rows();
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
-        const uint32_t active = pairs.active();
+        const uint32_t active = pairs.active(chunk);
         if (chunk + 1 < t.chunks) {
             loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
             next.load(t, chunk + 1);
@@ -591,22 +630,21 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
-    __shared__ int32_t origin[ISO_MAX_DIMS], coords[kTileWaves][ISO_MAX_DIMS];
+    __shared__ int32_t coords[kTileWaves][ISO_MAX_DIMS];
     __shared__ __align__(16) float row_lse[2][Lds::kRows], row_delta[2][Lds::kRows];
     const AttentionArgs &a = t.a;
     const TileWork work = tile_work(t);
     if (!work.any) return;
     Lds lds(lds_bytes, t.chunks);
-    tile_rows<DP, SEGMENTS>(t, work.tile, origin, lds);
-
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group, s = a.torus.s;
-    tile_biases<T>(a, first_head, a.bias ? a.group : 1, 1.f, lds.bias);
-    const int64_t rank = rank_at(t, origin, t.column_at + column * a.torus.d, true);
+    const int64_t rank = rank_at<true>(t, work.tile, t.column_at + column * t.words);
     const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 k[DP / 32], v[DP / 32];
     load_column<T, DP>(a.k, rank, work.key_head, a.head_dim, k);
     load_column<T, DP>(a.v, rank, work.key_head, a.head_dim, v);
+    tile_rows<DP, SEGMENTS>(t, work.tile, lds);
+    tile_biases<T>(t, first_head, a.bias ? a.group : 1, 1.f, lds.bias);
     const LanePieces<T, DP> pieces;
     const GradientFactors factors(a);
     __syncthreads();
@@ -637,7 +675,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + buffer * 2 * Lds::kTensor;
         const unsigned char *bias = (const unsigned char *)(lds.bias + (a.bias ? h * (s + 1) : 0));
-        const uint32_t active = pairs.active();
+        const uint32_t active = pairs.active(chunk);
         const int now = chunk;
         if (++chunk == t.chunks) chunk = 0, ++h;
         if (h < a.group) start(first_head + h, chunk, 1 - buffer);

@@ -405,14 +405,22 @@ class AttentionBinder {
         const TilePlan &p = side.plan;
         TileArgs ta{};
         ta.a = a;
-        for (int j = 0; j < c.d; ++j) ta.tile[j] = p.tile[j], ta.tiles[j] = p.tiles[j];
-        ta.n_tiles = (uint32_t)p.n_tiles;
+        const uint64_t work = (uint64_t)p.n_tiles * t.kv_heads * parts;
+        if (work > 0x7FFFFFF0ull) return ISO_ERR_TOO_LARGE;
+        for (int i = 0; i < c.d; ++i) {
+            const int j = c.d - 1 - i;
+            ta.dim[i] = {make_fastdiv((uint32_t)p.tiles[j]), p.tile[j], c.dims[j], (int32_t)c.inner[j], c.periodic[j]};
+        }
+        ta.n_tiles = make_fastdiv((uint32_t)p.n_tiles);
+        ta.parts = make_fastdiv((uint32_t)parts);
+        ta.biases = make_fastdiv((uint32_t)c.s + 1);
+        ta.items = (uint32_t)work;
         ta.heads = p.heads;
-        ta.parts = parts;
+        ta.words = (c.d + 3) / 4;
         ta.chunks = side.chunks;
         const char *base = (const char *)b.dev_table;
-        ta.column_at = (const int32_t *)(base + side.columns);
-        ta.row_at = (const int32_t *)(base + side.rows);
+        ta.column_at = (const uint2 *)(base + side.columns);
+        ta.row_at = (const uint2 *)(base + side.rows);
         ta.active = (const uint32_t *)(base + side.active);
         ta.index = (const uint16_t *)(base + side.index);
         ta.zeros = base + side.zeros;
@@ -421,8 +429,6 @@ class AttentionBinder {
             ta.slots = (const TilePlan::Slot *)(base + side.slots);
             ta.pairs = (const uint16_t *)(base + side.pairs);
         }
-        const uint64_t work = (uint64_t)p.n_tiles * t.kv_heads * parts;
-        if (work > 0x7FFFFFF0ull) return ISO_ERR_TOO_LARGE;
         ta.per_xcd = (uint32_t)((work + 7) / 8);
         return add_launch(b, func, (uint64_t)ta.per_xcd * 8, 256, ta, side.lds);
     }

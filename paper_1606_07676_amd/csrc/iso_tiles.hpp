@@ -25,8 +25,9 @@ struct TilePlan {
     int64_t n_tiles = 1;
     int rows = 0, chunks = 0;              // rows in use; chunks of kChunkRows
     int blocks = 0;                        // 16 x 16 blocks of pairs that hold a neighbour
-    std::vector<int32_t> column_at;        // [kTileColumns / heads][d]: position in the tile
-    std::vector<int32_t> row_at;           // [chunks * kChunkRows][d]: position relative to the tile's first rank
+    // positions relative to the tile's first rank, the last dimension first, in words of four
+    std::vector<int16_t> column_at;        // [kTileColumns / heads][words * 4]
+    std::vector<int16_t> row_at;           // [chunks * kChunkRows][words * 4]
     std::vector<uint32_t> active;          // [chunks]: bit 4 * wave + group: that block holds a neighbour
     // The bias's gradient, for columns that are ranks: which pairs of a (chunk, wavefront) belong to one slot
     // (head of the column) * s + neighbour.  Slots with the most pairs first.
@@ -133,12 +134,15 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     p.n_tiles = shape.n_tiles;
     if (p.n_tiles > 0x7FFFFFFF) return false;
     // columns: the wavefronts' boxes one after the other, the last dimension fastest inside and outside
-    p.column_at.resize((size_t)ranks * d);
+    const int width = (d + 3) / 4 * 4;
+    std::vector<int32_t> column_at((size_t)ranks * d);
+    p.column_at.assign((size_t)ranks * width, 0);
     for (int r = 0; r < ranks; ++r) {
         int inside = r % per_wave, box = r / per_wave;
         for (int j = d - 1; j >= 0; --j) {
             const int boxes = p.tile[j] / wave[j];
-            p.column_at[(size_t)r * d + j] = box % boxes * wave[j] + inside % wave[j];
+            column_at[(size_t)r * d + j] = box % boxes * wave[j] + inside % wave[j];
+            p.column_at[(size_t)r * width + d - 1 - j] = (int16_t)column_at[(size_t)r * d + j];
             inside /= wave[j];
             box /= boxes;
         }
@@ -148,7 +152,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     int64_t volume = 1;
     for (int j = 0; j < d; ++j) {
         span[j] = (int64_t)high[j] - low[j] + p.tile[j];
-        if (span[j] > (int64_t(1) << 40) / volume) return false;
+        if (low[j] < -32768 || (int64_t)high[j] + p.tile[j] > 32768 || span[j] > (int64_t(1) << 40) / volume) return false;
         volume *= span[j];
     }
     struct Row {
@@ -165,7 +169,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
             row.at.fill(0);
             int64_t place = 0;
             for (int j = 0; j < d; ++j) {
-                row.at[j] = p.column_at[(size_t)r * d + j] + step[i][j];
+                row.at[j] = column_at[(size_t)r * d + j] + step[i][j];
                 place = place * span[j] + (row.at[j] - low[j]);
             }
             std::vector<int> &copies = by_place[place];
@@ -192,14 +196,14 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     });
     p.rows = (int)rows.size();
     p.chunks = (p.rows + kChunkRows - 1) / kChunkRows;
-    p.row_at.assign((size_t)p.chunks * kChunkRows * d, 0);
+    p.row_at.assign((size_t)p.chunks * kChunkRows * width, 0);
     p.active.assign((size_t)p.chunks, 0);
     p.index.resize((size_t)p.chunks * 4 * kTileWaves * 64 * 4);
     for (size_t i = 0; i < p.index.size(); ++i) p.index[i] = (uint16_t)(4 * ((int)(i / 4 % 16) % heads * (c.s + 1) + c.s));
     std::vector<int> rank_of((size_t)p.rows);
     for (int u = 0; u < p.rows; ++u) {
         rank_of[order[u]] = u;
-        for (int j = 0; j < d; ++j) p.row_at[(size_t)u * d + j] = rows[order[u]].at[j];
+        for (int j = 0; j < d; ++j) p.row_at[(size_t)u * width + d - 1 - j] = (int16_t)rows[order[u]].at[j];
     }
     for (const auto &[pair, i] : taken) {
         const int r = (int)(pair >> 32), u = rank_of[(size_t)(pair & 0xFFFFFFFF)];

@@ -76,7 +76,7 @@ __device__ __forceinline__ float column_sum(float x) {
 // Loads into LDS write a wavefront's 64 pieces of 16 bytes one after the other, so rows are dense; which piece of its row a
 // lane fetches is permuted by the row, so that the 16 rows of a product's operand lie in 16 different groups of banks.
 template <int DP> struct TileLds {
-    static constexpr int kRows = DP > 64 ? 32 : 64;                 // of a chunk: 16 KB for both tensors (96: 12)
+    static constexpr int kRows = DP > 32 ? 32 : 64;                 // of a chunk
     static constexpr int kGroups = kRows / 16;
     static constexpr int kRowBytes = DP * 2, kPieces = DP / 8, kTensor = kRows * kRowBytes;
     static constexpr int kLoads = (kRows * kPieces + 255) / 256;
@@ -186,39 +186,48 @@ __device__ __forceinline__ int32_t column_segment(const AttentionArgs &a, int64_
     return own < 0 ? kNoColumn : own;
 }
 
-// Biases of `heads` q heads in LDS, a -inf behind each; zeros where there are none.
+// Biases of `heads` q heads times log2 e in LDS, a -inf behind each; zeros where there are none.
 template <typename T>
-__device__ __forceinline__ void tile_biases(const TileArgs &t, int first_head, int heads, float factor, float *at) {
+__device__ __forceinline__ void tile_biases(const TileArgs &t, int first_head, int heads, float *at) {
     const AttentionArgs &a = t.a;
     const int s = a.torus.s;
     for (int i = threadIdx.x; i < heads * (s + 1); i += 256) {
         uint32_t h, j;
         fast_divmod(i, t.biases, h, j);
         float b = (int)j == s ? -INFINITY : a.bias ? (float)((const T *)a.bias)[(int64_t)(first_head + h) * s + j] : 0.f;
-        // a factor must not make an infinity of a bias near the type's lowest value
-        if (factor != 1.f && b != -INFINITY) b = fminf(fmaxf(b * factor, -3.4e38f), 3.4e38f);
+        // the product must not make an infinity of a bias near the type's lowest value
+        if (fabsf(b) < INFINITY) b = fminf(fmaxf(b * kLog2e, -3.4e38f), 3.4e38f);
         at[i] = b;
     }
 }
 
 // One chunk of rows of two tensors on its way into LDS.  Tensors are given by the address of rank 0's row and the bytes
-// between ranks, below 2^32.
+// between ranks, below 2^32; a lane whose piece lies behind the row's end reads zeros for every rank.
 template <int DP, bool SEGMENTS> struct RowLoads {
     typedef TileLds<DP> Lds;
-    const unsigned char *first, *second, *zeros;
-    uint32_t first_stride, second_stride;
-    int head_dim;
+    const unsigned char *first[Lds::kLoads], *second[Lds::kLoads], *zeros;
+    uint32_t first_stride[Lds::kLoads], second_stride[Lds::kLoads];
 
+    __device__ __forceinline__ RowLoads(const TileArgs &t, const Heads &a, const Heads &b, int head) : zeros((const unsigned char *)t.zeros) {
+#pragma unroll
+        for (int i = 0; i < Lds::kLoads; ++i) {
+            const int unit = threadIdx.x + 256 * i, piece = Lds::piece_at(unit / Lds::kPieces, unit % Lds::kPieces);
+            const bool inside = piece * 8 < t.a.head_dim;
+            first[i] = inside ? (const unsigned char *)a.data + head * a.head_stride * 2 + piece * 16 : zeros;
+            second[i] = inside ? (const unsigned char *)b.data + head * b.head_stride * 2 + piece * 16 : zeros;
+            first_stride[i] = inside ? (uint32_t)(a.rank_stride * 2) : 0;
+            second_stride[i] = inside ? (uint32_t)(b.rank_stride * 2) : 0;
+        }
+    }
     __device__ __forceinline__ void start(const int32_t *rank, unsigned char *chunk) const {
 #pragma unroll
         for (int i = 0; i < Lds::kLoads; ++i) {
             const int unit = threadIdx.x + 256 * i, row = unit / Lds::kPieces;
             if (Lds::kRows * Lds::kPieces % 256 && unit >= Lds::kRows * Lds::kPieces) break;      // whole wavefronts
-            const int piece = Lds::piece_at(row, unit % Lds::kPieces);
             const int32_t r = rank[row];
-            const unsigned char *a = first + (uint64_t)(uint32_t)r * first_stride + piece * 16;
-            const unsigned char *b = second + (uint64_t)(uint32_t)r * second_stride + piece * 16;
-            if ((SEGMENTS && r < 0) || piece * 8 >= head_dim) a = b = zeros;
+            const unsigned char *a = first[i] + (uint64_t)(uint32_t)r * first_stride[i];
+            const unsigned char *b = second[i] + (uint64_t)(uint32_t)r * second_stride[i];
+            if (SEGMENTS && r < 0) a = b = zeros;
             unsigned char *to = chunk + __builtin_amdgcn_readfirstlane((threadIdx.x & ~63u) * 16 + 4096 * i);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)a,
                                              (__attribute__((address_space(3))) void *)to, 16, 0, 0);
@@ -248,10 +257,11 @@ template <int GROUPS> struct Pairs {
         const int shift = (threadIdx.x >> 6) * 4 + (GROUPS == 4 ? 0 : chunk % 2 * 2);
         return __builtin_amdgcn_readfirstlane(active_word >> shift) & ((1u << GROUPS) - 1);
     }
-    __device__ __forceinline__ float bias(const unsigned char *base, int g, int r) const {
+    __device__ __forceinline__ uint32_t at(int g, int r) const {
         const uint32_t two = r < 2 ? of[g].x : of[g].y;
-        return *(const float *)(base + (r % 2 ? two >> 16 : two & 0xFFFF));
+        return r % 2 ? two >> 16 : two & 0xFFFF;
     }
+    __device__ __forceinline__ float bias(const unsigned char *base, int g, int r) const { return *(const float *)(base + at(g, r)); }
 };
 
 // A column's row as right-hand operand: lane holds column lane % 16, elements 32 k + 8 (lane / 16) + 0..7.
@@ -293,9 +303,9 @@ template <typename T, int DP> struct LanePieces {
         for (int e = 0; e < DP / 16; ++e)
             turned[e] = row * TileLds<DP>::kRowBytes + TileLds<DP>::place(row, 2 * e + within % 4 / 2) * 16 + within % 2 * 8;
     }
-    // 16 staged rows times the columns: lane holds column lane % 16, rows 4 (lane / 16) + 0..3.
-    __device__ __forceinline__ typename Matrix<T>::f4 rows_times_columns(const unsigned char *rows, const typename Matrix<T>::x8 (&column)[DP / 32]) const {
-        typename Matrix<T>::f4 s = {0.f, 0.f, 0.f, 0.f};
+    // 16 staged rows times the columns, on top of s: lane holds column lane % 16, rows 4 (lane / 16) + 0..3.
+    __device__ __forceinline__ typename Matrix<T>::f4 rows_times_columns(const unsigned char *rows, const typename Matrix<T>::x8 (&column)[DP / 32],
+                                                                         typename Matrix<T>::f4 s) const {
 #pragma unroll
         for (int k = 0; k < DP / 32; ++k) s = Matrix<T>::multiply(*(const typename Matrix<T>::x8 *)(rows + plain[k]), column[k], s);
         return s;
@@ -356,7 +366,7 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
 }
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, DP > 64 ? 3 : 4) void attention_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
@@ -373,17 +383,18 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
     typename Matrix<T>::x8 q[DP / 32];
     load_column<T, DP>(a.q, rank, head, a.head_dim, q);
     tile_rows<DP, SEGMENTS>(t, work.tile, lds);
-    tile_biases<T>(t, first_head, t.heads, kLog2e, lds.bias);
+    tile_biases<T>(t, first_head, t.heads, lds.bias);
     const LanePieces<T, DP> pieces;
-    const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.k.data + work.key_head * a.k.head_stride),
-                                          (const unsigned char *)((const T *)a.v.data + work.key_head * a.v.head_stride),
-                                          (const unsigned char *)t.zeros, (uint32_t)(a.k.rank_stride * 2), (uint32_t)(a.v.rank_stride * 2), a.head_dim};
-    // scores times log2 e, so that the weights are powers of two
-    const float scale = a.scale * kLog2e, cap = a.cap * kLog2e, to_cap = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f;
+    const RowLoads<DP, SEGMENTS> loads(t, a.k, a.v, work.key_head);
+    // Scores times log2 e and less the column's base, so that the weights are powers of two.  The base comes into the
+    // products' start value (the cap's constant); it is raised, and what was added up before scaled, only when a score exceeds
+    // it by more than 8: weights of up to 256 lose nothing, and most chunks need no maximum over the lanes of a column.
+    const float scale = a.scale * kLog2e, per_scale = 1.f / scale, cap = a.cap * kLog2e, to_cap = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f;
     __syncthreads();
 
-    f4 acc[DP / 16] = {};
-    float m = -INFINITY, l = 0.f;                                   // l: of this lane's rows
+    f4 acc[DP / 16] = {}, from = {0.f, 0.f, 0.f, 0.f};              // from: - base / scale
+    float base = 0.f, limit = -INFINITY, l = 0.f;                   // l: of this lane's rows; limit: 8 once the column has a base
+    float cap_less_base = cap;
     Pairs<G> next;
     loads.start(lds.rank, lds.chunk);
     next.load(t, 0);
@@ -398,7 +409,7 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
         }
         if (!active) continue;
         f4 x[G];
-        float top = m;
+        float top = -INFINITY;
         // 32 rows at a time, so that the reads of one product are under way while the other waits
 #pragma unroll
         for (int pair = 0; pair < G / 2; ++pair) {
@@ -409,21 +420,24 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
                 const int g = 2 * pair + half;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) bias[half][r] = pairs.bias((const unsigned char *)lds.bias, g, r);
-                dot[half] = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
+                dot[half] = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q, from);
             }
+            if (a.cap > 0.f) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int g = 2 * pair + half;
-                if (a.cap > 0.f) {
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float e = __builtin_amdgcn_exp2f(dot[half][r] * to_cap);
-                        x[g][r] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap) + bias[half][r];
+                        x[2 * pair + half][r] = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap_less_base) + bias[half][r];
                     }
-                } else {
+            } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[g][r] = fmaf(dot[half][r], scale, bias[half][r]);
-                }
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[2 * pair + half][r] = fmaf(dot[half][r], scale, bias[half][r]);
+            }
+#pragma unroll
+            for (int g = 2 * pair; g < 2 * pair + 2; ++g) {
                 if (SEGMENTS) {
                     const int4 seg = *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4);
                     x[g][0] = seg.x == own ? x[g][0] : -INFINITY;
@@ -435,14 +449,19 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
                 for (int r = 0; r < 4; ++r) top = fmaxf(top, x[g][r]);
             }
         }
-        top = column_max(top);
-        const float base = finite_floor(top);
-        if (__any(top > m)) {
-            const float keep = __builtin_amdgcn_exp2f(m - base);
+        if (__any(top > limit)) {
+            top = column_max(top);
+            const bool based = limit > 0.f;
+            const float raise = based ? fmaxf(top, 0.f) : finite_floor(top), keep = based ? __builtin_amdgcn_exp2f(-raise) : 1.f;
+            if (top > -INFINITY) limit = 8.f;
+            base += raise;
+            from = a.cap > 0.f ? from : f4{1.f, 1.f, 1.f, 1.f} * (-base * per_scale);
+            cap_less_base = cap - base;
             l *= keep;
 #pragma unroll
             for (int e = 0; e < DP / 16; ++e) acc[e] *= keep;
-            m = top;
+#pragma unroll
+            for (int g = 0; g < G; ++g) x[g] -= raise;
         }
 #pragma unroll
         for (int pair = 0; pair < G / 2; ++pair) {
@@ -451,7 +470,7 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
             for (int g = 2 * pair; g < 2 * pair + 2; ++g)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    x[g][r] = __builtin_amdgcn_exp2f(x[g][r] - base);
+                    x[g][r] = __builtin_amdgcn_exp2f(x[g][r]);
                     l += x[g][r];
                 }
             pieces.add_weighted_rows(rows + Lds::kTensor + pair * 32 * Lds::kRowBytes, as_weights<T>(x[2 * pair], x[2 * pair + 1]), acc);
@@ -459,11 +478,11 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
     }
     l = column_sum(l);
     bool fine = store_column<T, DP>(a.out, rank, head, a.head_dim, acc, l == 0.f ? 0.f : 1.f / l);
-    // biases near the type's lowest value alone: their products with log2 e were cut off
-    const bool low = m < -1e38f && m != -INFINITY, again = low || l != l;
-    fine = fine && !low;
+    // again: NaN or infinities among the scores, or biases near the type's lowest value alone, whose products with log2 e and
+    // 1 / scale leave the range
+    const bool again = !(l < INFINITY) || !(fabsf(base) < 1e30f);
     if (a.lse && rank >= 0 && lane < 16 && !again)
-        a.lse[rank * a.q_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        a.lse[rank * a.q_heads + head] = l == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * kLn2;
     redo_columns(rank >= 0 && !(fine && !again), [&](int c) {
         const uint32_t r = (uint32_t)__shfl((int)rank, c);
         const int h = __shfl(head, c);
@@ -484,29 +503,31 @@ __global__ __launch_bounds__(256, 4) void attention_tile_kernel(const TileArgs t
 // grad_out staged: S and dP with the roles changed, grad_k^T += Q^T da, grad_v^T += grad_out^T P, head by head of the group.
 // Both gather: a tile's results are written once, by one workgroup, in one order.
 
-// P, dx and da of a pair.  The bias is -inf, and P 0, for pairs that are no neighbours.
+// P, dx and da of a pair, the bias times log2 e: -inf, and P 0, for pairs that are no neighbours.  Without a cap `dot` started
+// at -lse / scale, with one `lse` (times log2 e) is taken off here; dp started at -delta.
 struct GradientFactors {
     float scale, cap, to_cap;
     __device__ explicit GradientFactors(const AttentionArgs &a)
-        : scale(a.scale), cap(a.cap), to_cap(a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f) {}
-    template <bool SEGMENTS>
-    __device__ __forceinline__ PairGradient operator()(float dot, float bias, float lse, float dp, float delta, bool counts) const {
+        : scale(a.scale * kLog2e), cap(a.cap * kLog2e), to_cap(a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f) {}
+    // what dot starts at for an lse (natural, finite), and what operator() is given for it
+    __device__ __forceinline__ float start(const AttentionArgs &a, float lse) const { return a.cap > 0.f ? 0.f : -lse / a.scale; }
+    template <bool SEGMENTS> __device__ __forceinline__ PairGradient operator()(float dot, float bias, float lse, float dp, bool counts) const {
         PairGradient g;
-        float x, slope = 1.f;
         if (cap > 0.f) {
             const float y = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(dot * to_cap)), 1.f);      // tanh
-            x = fmaf(cap, y, bias);
-            slope = fmaf(-y, y, 1.f);
+            g.p = __builtin_amdgcn_exp2f(fmaf(cap, y, bias) - lse);
+            g.dx = g.p * dp;
+            g.da = g.dx * fmaf(-y, y, 1.f);
         } else {
-            x = fmaf(dot, scale, bias);
+            g.p = __builtin_amdgcn_exp2f(fmaf(dot, scale, bias));
+            g.dx = g.p * dp;
+            g.da = g.dx;
         }
-        g.p = exp_above(x, lse);
-        g.dx = g.p * (dp - delta);
         if (SEGMENTS) {                    // what a pair that does not count holds must not reach its slot of the bias's gradient
             g.p = counts ? g.p : 0.f;
             g.dx = counts ? g.dx : 0.f;
+            g.da = counts ? g.da : 0.f;
         }
-        g.da = cap > 0.f ? g.dx * slope : g.dx;
         return g;
     }
 };
@@ -539,7 +560,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
         typename Matrix<T>::x8 out[DP / 32];
         load_column<T, DP>(a.out, rank, head, a.head_dim, out);
         tile_rows<DP, SEGMENTS>(t, work.tile, lds);                 // while these are on their way
-        tile_biases<T>(t, first_head, t.heads, 1.f, lds.bias);
+        tile_biases<T>(t, first_head, t.heads, lds.bias);
 #pragma unroll
         for (int k = 0; k < DP / 32; ++k)
 #pragma unroll
@@ -549,10 +570,18 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
     lse = finite_floor(lse);
     if (rank >= 0 && lane < 16) a.delta[rank * a.q_heads + head] = delta;
     const LanePieces<T, DP> pieces;
-    const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.k.data + work.key_head * a.k.head_stride),
-                                          (const unsigned char *)((const T *)a.v.data + work.key_head * a.v.head_stride),
-                                          (const unsigned char *)t.zeros, (uint32_t)(a.k.rank_stride * 2), (uint32_t)(a.v.rank_stride * 2), a.head_dim};
+    const RowLoads<DP, SEGMENTS> loads(t, a.k, a.v, work.key_head);
     const GradientFactors factors(a);
+    // Biases near the type's lowest value alone: lse cannot be scaled.  Such a wavefront makes its weights the long way.
+    const bool low = __any(fabsf(lse) > 1e30f);
+    const f4 from = f4{1.f, 1.f, 1.f, 1.f} * (low ? 0.f : factors.start(a, lse)), from_dp = f4{-1.f, -1.f, -1.f, -1.f} * delta;
+    const float lse2 = lse * kLog2e;
+    const auto low_pair = [&](float dot, uint32_t at, float dp, bool counts) {
+        const int n = (int)at / 4 - column % t.heads * (s + 1);
+        const PairGradient none = {0.f, 0.f, 0.f};
+        if (n == s || (SEGMENTS && !counts)) return none;
+        return pair_gradient(dot, (float)((const T *)a.bias)[(int64_t)head * s + n], lse, dp, 0.f, a.scale, a.cap);
+    };
     __syncthreads();
 
     f4 acc[DP / 16] = {};
@@ -571,19 +600,25 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
 #pragma unroll
         for (int pair = 0; pair < G / 2; ++pair) {
             if (!(active >> (2 * pair) & 3)) continue;
-            f4 da[2] = {};
+            f4 da[2], dot[2], dp[2], bias[2];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
-                const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q);
-                const f4 dp = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, g_out);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) bias[half][r] = pairs.bias((const unsigned char *)lds.bias, g, r);
+                dot[half] = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, q, from);
+                dp[half] = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, g_out, from_dp);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int g = 2 * pair + half;
                 const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
                 f4 dx;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const PairGradient pg = factors.template operator()<SEGMENTS>(
-                        dot[r], pairs.bias((const unsigned char *)lds.bias, g, r), lse, dp[r], delta,
-                        (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                    const bool counts = (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own;
+                    const PairGradient pg = low ? low_pair(dot[half][r], pairs.at(g, r), dp[half][r], counts)
+                                                : factors.template operator()<SEGMENTS>(dot[half][r], bias[half][r], lse2, dp[half][r], counts);
                     dx[r] = pg.dx;
                     da[half][r] = pg.da;
                 }
@@ -644,7 +679,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     load_column<T, DP>(a.k, rank, work.key_head, a.head_dim, k);
     load_column<T, DP>(a.v, rank, work.key_head, a.head_dim, v);
     tile_rows<DP, SEGMENTS>(t, work.tile, lds);
-    tile_biases<T>(t, first_head, a.bias ? a.group : 1, 1.f, lds.bias);
+    tile_biases<T>(t, first_head, a.bias ? a.group : 1, lds.bias);
     const LanePieces<T, DP> pieces;
     const GradientFactors factors(a);
     __syncthreads();
@@ -654,10 +689,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     float next_lse = 0.f, next_delta = 0.f;
     // the rows of all chunks for the first head of the group, then for the next
     const auto start = [&](int h, int chunk, int buffer) {
-        const RowLoads<DP, SEGMENTS> loads = {(const unsigned char *)((const T *)a.q.data + h * a.q.head_stride),
-                                              (const unsigned char *)((const T *)a.grad_out.data + h * a.grad_out.head_stride),
-                                              (const unsigned char *)t.zeros, (uint32_t)(a.q.rank_stride * 2),
-                                              (uint32_t)(a.grad_out.rank_stride * 2), a.head_dim};
+        const RowLoads<DP, SEGMENTS> loads(t, a.q, a.grad_out, h);
         loads.start(lds.rank + chunk * Lds::kRows, lds.chunk + buffer * 2 * Lds::kTensor);
         next.load(t, chunk);
         if (threadIdx.x < Lds::kRows) {
@@ -670,11 +702,16 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     int chunk = 0, h = 0;
     for (int step = 0; h < a.group; ++step) {
         const int buffer = step % 2;
-        if (threadIdx.x < Lds::kRows) row_lse[buffer][threadIdx.x] = next_lse, row_delta[buffer][threadIdx.x] = next_delta;
+        if (threadIdx.x < Lds::kRows) {
+            // lse that cannot be scaled (see grad_q): NaN, and whoever reads the row is made again
+            const float lse = fabsf(next_lse) > 1e30f ? NAN : next_lse;
+            row_lse[buffer][threadIdx.x] = a.cap > 0.f ? lse * kLog2e : factors.start(a, lse);
+            row_delta[buffer][threadIdx.x] = -next_delta;
+        }
         wait_for_rows();
         const Pairs<G> pairs = next;
         const unsigned char *rows = lds.chunk + buffer * 2 * Lds::kTensor;
-        const unsigned char *bias = (const unsigned char *)(lds.bias + (a.bias ? h * (s + 1) : 0));
+        const unsigned char *biases = (const unsigned char *)(lds.bias + (a.bias ? h * (s + 1) : 0));
         const uint32_t active = pairs.active(chunk);
         const int now = chunk;
         if (++chunk == t.chunks) chunk = 0, ++h;
@@ -682,20 +719,25 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
 #pragma unroll
         for (int pair = 0; pair < G / 2; ++pair) {
             if (!(active >> (2 * pair) & 3)) continue;
-            f4 p[2] = {}, da[2] = {};
+            f4 p[2], da[2], dot[2], dp[2], bias[2], lse[2];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
-                const f4 dot = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, k);
-                const f4 dp = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, v);
-                const f4 lse = *(const f4 *)(row_lse[buffer] + g * 16 + lane / 16 * 4);
-                const f4 delta = *(const f4 *)(row_delta[buffer] + g * 16 + lane / 16 * 4);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) bias[half][r] = pairs.bias(biases, g, r);
+                lse[half] = *(const f4 *)(row_lse[buffer] + g * 16 + lane / 16 * 4);
+                dot[half] = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, k, a.cap > 0.f ? f4{0.f, 0.f, 0.f, 0.f} : lse[half]);
+                dp[half] = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, v,
+                                                     *(const f4 *)(row_delta[buffer] + g * 16 + lane / 16 * 4));
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int g = 2 * pair + half;
                 const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + now * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const PairGradient pg = factors.template operator()<SEGMENTS>(
-                        dot[r], pairs.bias(bias, g, r), lse[r], dp[r], delta[r],
-                        (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                        dot[half][r], bias[half][r], lse[half][r], dp[half][r], (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
                     p[half][r] = pg.p;
                     da[half][r] = pg.da;
                 }

@@ -224,7 +224,7 @@ ISO_TILE_KERNEL(GradKVTileKernel, attention_grad_kv_tile_kernel)
 constexpr int kTileMaxHeadDim = 128;
 constexpr size_t kTileMaxLds = 64 << 10;
 inline int tile_head_dim(int head_dim) { return (head_dim + 31) / 32 * 32; }
-inline int tile_chunk_rows(int head_dim) { return tile_head_dim(head_dim) > 64 ? TileLds<128>::kRows : TileLds<64>::kRows; }
+inline int tile_chunk_rows(int head_dim) { return tile_head_dim(head_dim) > 32 ? TileLds<64>::kRows : TileLds<32>::kRows; }
 inline size_t tile_lds_bytes(int head_dim, int chunks, size_t biases) {
     switch (tile_head_dim(head_dim)) {
         case 32: return TileLds<32>::bytes(chunks, biases);
@@ -380,6 +380,7 @@ class AttentionBinder {
 
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
             if (o.t.rows || o.t.dtype == ISO_DTYPE_F32 || !o.is_wide || o.t.head_dim > kTileMaxHeadDim) return;
+            if (!(std::fabs(o.t.scale) > 1e-20f && std::fabs(o.t.scale) < 1e20f)) return;      // the kernels divide by it
             for (const iso_heads_t *x : {&o.t.q, &o.t.k, &o.t.v, o.g ? &o.g->grad_out : &o.t.q})
                 if (x->rank_stride >> 31) return;                  // strides in bytes: 32 bits
             if (!build_tile_plan(o.c, heads, back, sums, plan)) return;

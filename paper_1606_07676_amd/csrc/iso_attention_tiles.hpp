@@ -37,11 +37,15 @@ struct TileArgs {
     const uint2 *column_at, *row_at;       // [][words]: positions relative to the tile's first rank, four dimensions in a word
     const uint32_t *active;
     const uint16_t *index;
-    const uint32_t *slots_of;              // the bias's gradient, or null: see TilePlan
-    const TilePlan::Slot *slots;
-    const uint16_t *pairs;
+    const uint32_t *slots;                 // the bias's gradient, or null: see TilePlan
+    int32_t slot_rounds, slot_words;
     const void *zeros;                     // a row of zeros
 };
+
+// What is read from LDS while rows are on their way there has to be of these types: the compiler takes a read of a struct for
+// one of those rows, and waits for all of them first.
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef int32_t i4 __attribute__((ext_vector_type(4)));
 
 template <typename T> struct Matrix;
 template <> struct Matrix<__bf16> {
@@ -71,7 +75,7 @@ __device__ __forceinline__ float column_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// LDS of a tile kernel: two chunks of rows of two tensors, then per row of the tile its rank and segment, then the biases.
+// LDS of a tile kernel: chunks of rows of two tensors, then per row of the tile its rank and segment, then the biases.
 //
 // Loads into LDS write a wavefront's 64 pieces of 16 bytes one after the other, so rows are dense; which piece of its row a
 // lane fetches is permuted by the row, so that the 16 rows of a product's operand lie in 16 different groups of banks.
@@ -80,16 +84,27 @@ template <int DP> struct TileLds {
     static constexpr int kGroups = kRows / 16;
     static constexpr int kRowBytes = DP * 2, kPieces = DP / 8, kTensor = kRows * kRowBytes;
     static constexpr int kLoads = (kRows * kPieces + 255) / 256;
-    unsigned char *chunk;                  // [2][2][kTensor]
+    // The table of a chunk goes to LDS with its rows, or to registers where LDS is what limits the workgroups of a CU (rows of
+    // 128: 53 us in place of 59 for 32 x 32 x 32, 27 neighbours; rows of 64 the other way round: 121 in place of 131 us for
+    // 256 x 256, 169 neighbours).
+    static constexpr bool kIndexInLds = DP <= 96;
+    static constexpr int kIndex = kIndexInLds ? kGroups * 4 * 512 : 0;
+    static constexpr int kStage = 2 * kTensor + kIndex;
+    unsigned char *chunk;                  // [2]: rows of the first tensor, of the second, table
     int32_t *rank, *segment;
+    uint32_t *active;                      // [chunks]: bit 4 * wave + g: group g holds a neighbour of one of the wavefront's columns
     float *bias;
 
-    static __host__ __device__ size_t bytes(int chunks, size_t floats) { return 4 * (size_t)kTensor + (size_t)chunks * kRows * 8 + floats * 4; }
+    static __host__ __device__ int words(int chunks) { return (chunks + 3) / 4 * 4; }
+    static __host__ __device__ size_t bytes(int chunks, size_t floats) {
+        return 2 * (size_t)kStage + (size_t)chunks * kRows * 8 + words(chunks) * 4 + floats * 4;
+    }
     __device__ TileLds(unsigned char *at, int chunks) {
         chunk = at;
-        rank = (int32_t *)(at + 4 * kTensor);
+        rank = (int32_t *)(at + 2 * kStage);
         segment = rank + chunks * kRows;
-        bias = (float *)(segment + chunks * kRows);
+        active = (uint32_t *)(segment + chunks * kRows);
+        bias = (float *)(active + words(chunks));
     }
     static __device__ __forceinline__ int place(int row, int piece) {
         return DP == 32 ? piece ^ (row >> 2 & 3) : DP == 64 ? piece ^ (row >> 1 & 7) : DP == 128 ? piece ^ (row & 15)
@@ -173,6 +188,8 @@ template <int DP, bool SEGMENTS> __device__ __forceinline__ void tile_rows(const
             lds.rank[u] = max(rank, 0);
         }
     };
+    for (int c = threadIdx.x; c < t.chunks; c += 256)
+        lds.active[c] = TileLds<DP>::kGroups == 4 ? t.active[c] : t.active[c / 2] >> (c % 2 * 2) & 0x3333;
     for (int u = threadIdx.x; u < rows; u += 512) {                 // two trips to memory under way at a time
         const bool second = u + 256 < rows;
         const uint2 a = t.row_at[(int64_t)u * t.words], b = t.row_at[(int64_t)(second ? u + 256 : u) * t.words];
@@ -205,10 +222,10 @@ __device__ __forceinline__ void tile_biases(const TileArgs &t, int first_head, i
 // between ranks, below 2^32; a lane whose piece lies behind the row's end reads zeros for every rank.
 template <int DP, bool SEGMENTS> struct RowLoads {
     typedef TileLds<DP> Lds;
-    const unsigned char *first[Lds::kLoads], *second[Lds::kLoads], *zeros;
+    const unsigned char *first[Lds::kLoads], *second[Lds::kLoads], *zeros, *index;
     uint32_t first_stride[Lds::kLoads], second_stride[Lds::kLoads];
 
-    __device__ __forceinline__ RowLoads(const TileArgs &t, const Heads &a, const Heads &b, int head) : zeros((const unsigned char *)t.zeros) {
+    __device__ __forceinline__ RowLoads(const TileArgs &t, const Heads &a, const Heads &b, int head) : zeros((const unsigned char *)t.zeros), index((const unsigned char *)t.index + threadIdx.x * 16) {
 #pragma unroll
         for (int i = 0; i < Lds::kLoads; ++i) {
             const int unit = threadIdx.x + 256 * i, piece = Lds::piece_at(unit / Lds::kPieces, unit % Lds::kPieces);
@@ -219,7 +236,9 @@ template <int DP, bool SEGMENTS> struct RowLoads {
             second_stride[i] = inside ? (uint32_t)(b.rank_stride * 2) : 0;
         }
     }
-    __device__ __forceinline__ void start(const int32_t *rank, unsigned char *chunk) const {
+    __device__ __forceinline__ void start(const TileLds<DP> &lds, int chunk_number, int stage) const {
+        const int32_t *rank = lds.rank + chunk_number * Lds::kRows;
+        unsigned char *chunk = lds.chunk + stage * Lds::kStage;
 #pragma unroll
         for (int i = 0; i < Lds::kLoads; ++i) {
             const int unit = threadIdx.x + 256 * i, row = unit / Lds::kPieces;
@@ -234,31 +253,46 @@ template <int DP, bool SEGMENTS> struct RowLoads {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)b,
                                              (__attribute__((address_space(3))) void *)(to + Lds::kTensor), 16, 0, 0);
         }
+#pragma unroll
+        for (int i = 0; i < Lds::kIndex / 4096; ++i) {
+            unsigned char *to = chunk + 2 * Lds::kTensor + __builtin_amdgcn_readfirstlane((threadIdx.x & ~63u) * 16 + 4096 * i);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(index + (int64_t)chunk_number * Lds::kIndex + 4096 * i),
+                                             (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+        }
     }
 };
-// The chunk that was started is in LDS, and everybody has done with the one before it.
-__device__ __forceinline__ void wait_for_rows() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-}
+// The chunk that was started is in LDS, and all wavefronts have done with the one before.
+__device__ __forceinline__ void wait_for_rows() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // The table's entries of a chunk: byte offsets of the biases of this lane's column and rows 4 (lane / 16) + 0..3 of each group.
-template <int GROUPS> struct Pairs {
-    uint2 of[GROUPS];
-    uint32_t active_word;
-    __device__ __forceinline__ void load(const TileArgs &t, int chunk) {
-        active_word = t.active[GROUPS == 4 ? chunk : chunk >> 1];
-        const uint2 *at = (const uint2 *)t.index + ((int64_t)chunk * GROUPS * kTileWaves + (threadIdx.x >> 6)) * 64 + (threadIdx.x & 63);
+template <int DP> struct Pairs {
+    static constexpr int kPairs = TileLds<DP>::kGroups / 2;
+    u4 of[kPairs];
+    uint32_t active;
+
+    __device__ __forceinline__ void read(const u4 *at) {
+        at += (threadIdx.x >> 6) * 64 + (threadIdx.x & 63);
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) of[g] = at[g * kTileWaves * 64];
+        for (int n = 0; n < kPairs; ++n) of[n] = at[n * kTileWaves * 64];
     }
-    // Bit g: group g holds a neighbour of one of the wavefront's columns.
-    __device__ __forceinline__ uint32_t active(int chunk) const {
-        const int shift = (threadIdx.x >> 6) * 4 + (GROUPS == 4 ? 0 : chunk % 2 * 2);
-        return __builtin_amdgcn_readfirstlane(active_word >> shift) & ((1u << GROUPS) - 1);
+    // before a chunk's rows are started
+    __device__ __forceinline__ void prefetch(const TileArgs &t, int chunk) {
+        if constexpr (!TileLds<DP>::kIndexInLds) read((const u4 *)t.index + (int64_t)chunk * kPairs * kTileWaves * 64);
     }
+    // once they are there; next: what was prefetched
+    __device__ __forceinline__ Pairs(const TileLds<DP> &lds, const Pairs &next, int chunk, int stage) {
+        active = __builtin_amdgcn_readfirstlane(lds.active[chunk] >> ((threadIdx.x >> 6) * 4)) & 15;
+        if constexpr (TileLds<DP>::kIndexInLds) {
+            read((const u4 *)(lds.chunk + stage * TileLds<DP>::kStage + 2 * TileLds<DP>::kTensor));
+        } else {
+#pragma unroll
+            for (int n = 0; n < kPairs; ++n) of[n] = next.of[n];
+        }
+    }
+    __device__ Pairs() {}
     __device__ __forceinline__ uint32_t at(int g, int r) const {
-        const uint32_t two = r < 2 ? of[g].x : of[g].y;
+        const u4 &eight = of[g / 2];
+        const uint32_t two = g % 2 ? (r < 2 ? eight.z : eight.w) : (r < 2 ? eight.x : eight.y);
         return r % 2 ? two >> 16 : two & 0xFFFF;
     }
     __device__ __forceinline__ float bias(const unsigned char *base, int g, int r) const { return *(const float *)(base + at(g, r)); }
@@ -280,7 +314,6 @@ __device__ __forceinline__ void load_column(const Heads &h, int64_t rank, int he
 // The compiler takes the builtin for a read of whatever is on its way into LDS and waits for the next chunk's rows before
 // it (a quarter of the time of 256 x 256, 169 neighbours); here the reads are waited for where they are issued.
 struct Turned {
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
     u4 first, second;
 };
 template <int HALF> __device__ __forceinline__ Turned read_transposed(uint32_t first, uint32_t second) {
@@ -289,7 +322,7 @@ template <int HALF> __device__ __forceinline__ Turned read_transposed(uint32_t f
                  "ds_read_b64_tr_b16 %2, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\ts_waitcnt lgkmcnt(0)"
                  : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
                  : "v"(first), "v"(second), "n"(HALF));
-    return {Turned::u4{a.x, a.y, b.x, b.y}, Turned::u4{c.x, c.y, d.x, d.y}};
+    return {u4{a.x, a.y, b.x, b.y}, u4{c.x, c.y, d.x, d.y}};
 }
 
 // Where a lane finds its pieces of staged rows: the same for every group of 16.
@@ -366,7 +399,7 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
 }
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256, DP > 64 ? 3 : 4) void attention_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, DP > 64 ? 3 : SEGMENTS ? 4 : 5) void attention_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
@@ -395,18 +428,18 @@ __global__ __launch_bounds__(256, DP > 64 ? 3 : 4) void attention_tile_kernel(co
     f4 acc[DP / 16] = {}, from = {0.f, 0.f, 0.f, 0.f};              // from: - base / scale
     float base = 0.f, limit = -INFINITY, l = 0.f;                   // l: of this lane's rows; limit: 8 once the column has a base
     float cap_less_base = cap;
-    Pairs<G> next;
-    loads.start(lds.rank, lds.chunk);
-    next.load(t, 0);
+    Pairs<DP> next;
+    next.prefetch(t, 0);
+    loads.start(lds, 0, 0);
     for (int chunk = 0; chunk < t.chunks; ++chunk) {
         wait_for_rows();
-        const Pairs<G> pairs = next;
-        const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
-        const uint32_t active = pairs.active(chunk);
+        const Pairs<DP> pairs(lds, next, chunk, chunk % 2);
         if (chunk + 1 < t.chunks) {
-            loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
-            next.load(t, chunk + 1);
+            next.prefetch(t, chunk + 1);
+            loads.start(lds, chunk + 1, 1 - chunk % 2);
         }
+        const unsigned char *rows = lds.chunk + chunk % 2 * Lds::kStage;
+        const uint32_t active = pairs.active;
         if (!active) continue;
         f4 x[G];
         float top = -INFINITY;
@@ -439,7 +472,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 3 : 4) void attention_tile_kernel(co
 #pragma unroll
             for (int g = 2 * pair; g < 2 * pair + 2; ++g) {
                 if (SEGMENTS) {
-                    const int4 seg = *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4);
+                    const i4 seg = *(const i4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4);
                     x[g][0] = seg.x == own ? x[g][0] : -INFINITY;
                     x[g][1] = seg.y == own ? x[g][1] : -INFINITY;
                     x[g][2] = seg.z == own ? x[g][2] : -INFINITY;
@@ -532,6 +565,30 @@ struct GradientFactors {
     }
 };
 
+// A lane's part of the bias's gradient: the places of up to 16 pairs of one slot among a wavefront's dx of 32 rows, in which
+// every lane has written four rows of its column, 16 bytes at once.
+constexpr int kDxFloats = 516;
+struct SlotRound {
+    uint32_t slot;
+    u4 first, second;
+    __device__ __forceinline__ void load(const TileArgs &t, int pair, int round, int wave, int lane) {
+        const uint32_t *at = t.slots + (((int64_t)pair * kTileWaves + wave) * t.slot_rounds + round) * (64 + 256 * t.slot_words);
+        slot = at[lane];
+        first = *(const u4 *)(at + 64 + lane * 4);
+        if (t.slot_words > 1) second = *(const u4 *)(at + 64 + 256 + lane * 4);
+    }
+    static __device__ __forceinline__ float eight(const float *dx, const u4 &w) {
+        const float a = dx[w.x & 0xFFFF] + dx[w.x >> 16], b = dx[w.y & 0xFFFF] + dx[w.y >> 16];
+        const float c = dx[w.z & 0xFFFF] + dx[w.z >> 16], d = dx[w.w & 0xFFFF] + dx[w.w >> 16];
+        return (a + b) + (c + d);
+    }
+    __device__ __forceinline__ float sum(const float *dx, int words) const {
+        float x = eight(dx, first);
+        if (words > 1) x += eight(dx, second);
+        return x;
+    }
+};
+
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
@@ -546,10 +603,13 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
     const int s = a.torus.s, slots = t.heads * s;
-    // behind the biases: dx of the wavefront's blocks of 64 rows, and the sums of its slots over the tile's rows
-    float *behind = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4, *dx_at = behind + wave * 1024, *sums = behind + kTileWaves * 1024 + wave * slots;
-    if (t.slots_of)
-        for (int i = lane; i < slots; i += 64) sums[i] = 0.f;
+    // behind the biases: dx of 32 rows and the wavefront's columns, a zero, and the sums of its slots over the tile's rows
+    float *behind = lds.bias + (t.heads * (s + 1) + 3) / 4 * 4, *dx_at = behind + wave * kDxFloats;
+    float *sums = behind + kTileWaves * kDxFloats + wave * (slots + 1);
+    if (t.slots) {
+        for (int i = lane; i <= slots; i += 64) sums[i] = 0.f;
+        if (lane == 0) dx_at[512] = 0.f;
+    }
     const int64_t rank = rank_at<true>(t, work.tile, t.column_at + column / t.heads * t.words);
     const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
     typename Matrix<T>::x8 q[DP / 32], g_out[DP / 32];
@@ -568,7 +628,15 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
         delta = column_sum(delta);
     }
     lse = finite_floor(lse);
-    if (rank >= 0 && lane < 16) a.delta[rank * a.q_heads + head] = delta;
+    if (rank >= 0 && lane < 16) {
+        // what the other pass starts its products at; an lse that cannot be scaled (see below) is a NaN there, and whoever reads
+        // the row is made again
+        const int64_t at = rank * a.q_heads + head;
+        const GradientFactors f(a);
+        a.delta[at] = delta;
+        a.starts[at] = fabsf(lse) > 1e30f ? NAN : a.cap > 0.f ? lse * kLog2e : f.start(a, lse);
+        a.starts[(int64_t)a.n * a.q_heads + at] = -delta;
+    }
     const LanePieces<T, DP> pieces;
     const RowLoads<DP, SEGMENTS> loads(t, a.k, a.v, work.key_head);
     const GradientFactors factors(a);
@@ -585,18 +653,20 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
     __syncthreads();
 
     f4 acc[DP / 16] = {};
-    Pairs<G> next;
-    loads.start(lds.rank, lds.chunk);
-    next.load(t, 0);
+    Pairs<DP> next;
+    next.prefetch(t, 0);
+    loads.start(lds, 0, 0);
     for (int chunk = 0; chunk < t.chunks; ++chunk) {
         wait_for_rows();
-        const Pairs<G> pairs = next;
-        const unsigned char *rows = lds.chunk + chunk % 2 * 2 * Lds::kTensor;
-        const uint32_t active = pairs.active(chunk);
+        const Pairs<DP> pairs(lds, next, chunk, chunk % 2);
+        SlotRound round;
+        if (t.slots) round.load(t, chunk * (G / 2), 0, wave, lane);
         if (chunk + 1 < t.chunks) {
-            loads.start(lds.rank + (chunk + 1) * Lds::kRows, lds.chunk + (chunk + 1) % 2 * 2 * Lds::kTensor);
-            next.load(t, chunk + 1);
+            next.prefetch(t, chunk + 1);
+            loads.start(lds, chunk + 1, 1 - chunk % 2);
         }
+        const unsigned char *rows = lds.chunk + chunk % 2 * Lds::kStage;
+        const uint32_t active = pairs.active;
 #pragma unroll
         for (int pair = 0; pair < G / 2; ++pair) {
             if (!(active >> (2 * pair) & 3)) continue;
@@ -612,33 +682,33 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
-                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
+                const i4 seg = SEGMENTS ? *(const i4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4) : i4{};
                 f4 dx;
+                if (low) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool counts = (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own;
-                    const PairGradient pg = low ? low_pair(dot[half][r], pairs.at(g, r), dp[half][r], counts)
-                                                : factors.template operator()<SEGMENTS>(dot[half][r], bias[half][r], lse2, dp[half][r], counts);
-                    dx[r] = pg.dx;
-                    da[half][r] = pg.da;
+                    for (int r = 0; r < 4; ++r) {
+                        const PairGradient pg = low_pair(dot[half][r], pairs.at(g, r), dp[half][r],
+                                                         (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                        dx[r] = pg.dx;
+                        da[half][r] = pg.da;
+                    }
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const PairGradient pg = factors.template operator()<SEGMENTS>(
+                            dot[half][r], bias[half][r], lse2, dp[half][r], (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                        dx[r] = pg.dx;
+                        da[half][r] = pg.da;
+                    }
                 }
-                if (t.slots_of)
-                    *(f4 *)(dx_at + (((G == 4 ? g : chunk % 2 * 2 + g) * 64) + lane) * 4) = rank >= 0 ? dx : f4{0.f, 0.f, 0.f, 0.f};
+                if (t.slots) *(f4 *)(dx_at + (half * 64 + lane) * 4) = rank >= 0 ? dx : f4{0.f, 0.f, 0.f, 0.f};
             }
             pieces.add_weighted_rows(rows + pair * 32 * Lds::kRowBytes, as_weights<T>(da[0], da[1]), acc);
-        }
-        if (t.slots_of && (G == 4 || chunk % 2 || chunk + 1 == t.chunks)) {
-            // every lane adds up the pairs of one slot in 64 rows
-            __builtin_amdgcn_wave_barrier();
-            const int list = (G == 4 ? chunk : chunk / 2) * kTileWaves + wave;
-            const uint32_t begin = t.slots_of[list], end = t.slots_of[list + 1];
-            for (uint32_t j = begin + lane; j < end; j += 64) {
-                const TilePlan::Slot slot = t.slots[j];
-                float sum = 0.f;
-                for (uint32_t n = 0; n < slot.count; ++n) sum += dx_at[t.pairs[slot.first + n]];
-                sums[slot.slot] += sum;
-            }
-            __builtin_amdgcn_wave_barrier();
+            if (t.slots)                                            // every lane adds up the pairs of one slot in 32 rows
+                for (int n = 0; n < t.slot_rounds; ++n) {
+                    if (n || pair) round.load(t, chunk * (G / 2) + pair, n, wave, lane);
+                    sums[round.slot] += round.sum(dx_at, t.slot_words);
+                }
         }
     }
     const bool fine = store_column<T, DP>(a.grad_q, rank, head, a.head_dim, acc, a.scale);
@@ -651,11 +721,12 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
         grad_q_row<T, true>(a, r, h, row_delta, coords[wave]);
         __builtin_amdgcn_wave_barrier();
     });
-    if (t.slots_of) {
+    if (t.slots) {
         __syncthreads();
-        const float *all = behind + kTileWaves * 1024;
+        const float *all = behind + kTileWaves * kDxFloats;
         float *out = a.partials + (uint64_t)work.tile * a.q_heads * s + (int64_t)first_head * s;
-        for (int i = threadIdx.x; i < slots; i += 256) out[i] = all[i] + all[slots + i] + all[2 * slots + i] + all[3 * slots + i];
+        for (int i = threadIdx.x; i < slots; i += 256)
+            out[i] = all[i] + all[slots + 1 + i] + all[2 * (slots + 1) + i] + all[3 * (slots + 1) + i];
     }
 }
 
@@ -666,7 +737,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     constexpr int G = Lds::kGroups;
     extern __shared__ __align__(16) unsigned char lds_bytes[];
     __shared__ int32_t coords[kTileWaves][ISO_MAX_DIMS];
-    __shared__ __align__(16) float row_lse[2][Lds::kRows], row_delta[2][Lds::kRows];
+    __shared__ __align__(16) float row_starts[2][2 * Lds::kRows];
     const AttentionArgs &a = t.a;
     const TileWork work = tile_work(t);
     if (!work.any) return;
@@ -685,37 +756,32 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     __syncthreads();
 
     f4 dk[DP / 16] = {}, dv[DP / 16] = {};
-    Pairs<G> next;
-    float next_lse = 0.f, next_delta = 0.f;
-    // the rows of all chunks for the first head of the group, then for the next
-    const auto start = [&](int h, int chunk, int buffer) {
-        const RowLoads<DP, SEGMENTS> loads(t, a.q, a.grad_out, h);
-        loads.start(lds.rank + chunk * Lds::kRows, lds.chunk + buffer * 2 * Lds::kTensor);
-        next.load(t, chunk);
-        if (threadIdx.x < Lds::kRows) {
-            const int32_t r = lds.rank[chunk * Lds::kRows + threadIdx.x];
-            next_lse = r >= 0 ? finite_floor(a.lse[(int64_t)r * a.q_heads + h]) : 0.f;
-            next_delta = r >= 0 ? a.delta[(int64_t)r * a.q_heads + h] : 0.f;
+    // the rows of all chunks for the first head of the group, then for the next, and what products with them start at
+    Pairs<DP> next;
+    const auto start = [&](int h, int chunk, int stage) {
+        next.prefetch(t, chunk);
+        const RowLoads<DP, SEGMENTS> loads(t, a.q, a.grad_out, first_head + h);
+        loads.start(lds, chunk, stage);
+        const float *from = a.starts + first_head + h;
+#pragma unroll
+        for (int i = 0; i < Lds::kRows / 32; ++i) {                 // every wavefront the same: -lse / scale, then -delta
+            const int n = lane + 64 * i;
+            const int64_t r = max(lds.rank[chunk * Lds::kRows + n % Lds::kRows], 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + (n / Lds::kRows * (int64_t)a.n + r) * a.q_heads),
+                                             (__attribute__((address_space(3))) void *)(row_starts[stage] + 64 * i), 4, 0, 0);
         }
     };
-    start(first_head, 0, 0);
+    start(0, 0, 0);
     int chunk = 0, h = 0;
-    for (int step = 0; h < a.group; ++step) {
-        const int buffer = step % 2;
-        if (threadIdx.x < Lds::kRows) {
-            // lse that cannot be scaled (see grad_q): NaN, and whoever reads the row is made again
-            const float lse = fabsf(next_lse) > 1e30f ? NAN : next_lse;
-            row_lse[buffer][threadIdx.x] = a.cap > 0.f ? lse * kLog2e : factors.start(a, lse);
-            row_delta[buffer][threadIdx.x] = -next_delta;
-        }
+    for (int stage = 0; h < a.group; stage = 1 - stage) {
         wait_for_rows();
-        const Pairs<G> pairs = next;
-        const unsigned char *rows = lds.chunk + buffer * 2 * Lds::kTensor;
-        const unsigned char *biases = (const unsigned char *)(lds.bias + (a.bias ? h * (s + 1) : 0));
-        const uint32_t active = pairs.active(chunk);
-        const int now = chunk;
+        const Pairs<DP> pairs(lds, next, chunk, stage);
+        const int now = chunk, now_h = h;
         if (++chunk == t.chunks) chunk = 0, ++h;
-        if (h < a.group) start(first_head + h, chunk, 1 - buffer);
+        if (h < a.group) start(h, chunk, 1 - stage);
+        const unsigned char *rows = lds.chunk + stage * Lds::kStage;
+        const unsigned char *biases = (const unsigned char *)(lds.bias + (a.bias ? now_h * (s + 1) : 0));
+        const uint32_t active = pairs.active;
 #pragma unroll
         for (int pair = 0; pair < G / 2; ++pair) {
             if (!(active >> (2 * pair) & 3)) continue;
@@ -725,15 +791,15 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
                 const int g = 2 * pair + half;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) bias[half][r] = pairs.bias(biases, g, r);
-                lse[half] = *(const f4 *)(row_lse[buffer] + g * 16 + lane / 16 * 4);
+                lse[half] = *(const f4 *)(row_starts[stage] + g * 16 + lane / 16 * 4);
                 dot[half] = pieces.rows_times_columns(rows + g * 16 * Lds::kRowBytes, k, a.cap > 0.f ? f4{0.f, 0.f, 0.f, 0.f} : lse[half]);
                 dp[half] = pieces.rows_times_columns(rows + Lds::kTensor + g * 16 * Lds::kRowBytes, v,
-                                                     *(const f4 *)(row_delta[buffer] + g * 16 + lane / 16 * 4));
+                                                     *(const f4 *)(row_starts[stage] + Lds::kRows + g * 16 + lane / 16 * 4));
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int g = 2 * pair + half;
-                const int4 seg = SEGMENTS ? *(const int4 *)(lds.segment + now * Lds::kRows + g * 16 + lane / 16 * 4) : int4{};
+                const i4 seg = SEGMENTS ? *(const i4 *)(lds.segment + now * Lds::kRows + g * 16 + lane / 16 * 4) : i4{};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const PairGradient pg = factors.template operator()<SEGMENTS>(

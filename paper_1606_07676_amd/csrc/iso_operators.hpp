@@ -249,7 +249,7 @@ inline uint64_t bias_parts(const Comm &c, int q_heads) {
 }
 
 struct BackwardWorkspace {
-    uint64_t delta = 0, partials = 0, bytes = 0;                 // offsets
+    uint64_t delta = 0, starts = 0, partials = 0, bytes = 0;     // offsets
 };
 inline int tile_heads(int group) {             // q heads of a rank that one tile of columns takes together
     int heads = 1;
@@ -258,7 +258,8 @@ inline int tile_heads(int group) {             // q heads of a rank that one til
 }
 inline int backward_workspace(const Comm &c, int q_heads, int kv_heads, bool bias, BackwardWorkspace &w) {
     const uint64_t rows = (uint64_t)c.p * q_heads;               // below 2^47
-    w.partials = (rows * 4 + 255) / 256 * 256;
+    w.starts = (rows * 4 + 255) / 256 * 256;
+    w.partials = w.starts + (rows * 8 + 255) / 256 * 256;
     w.bytes = w.partials;
     if (bias) {
         if ((uint64_t)q_heads * c.s > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
@@ -296,8 +297,8 @@ class AttentionBinder {
         if (!g) {
             forward_side.take(*this, table, heads, false, false, biases);
         } else {
-            const bool sums = g->grad_bias && c.s;                 // dx of the blocks of a chunk, and the slots of every wavefront
-            forward_side.take(*this, table, heads, false, sums, biases + 3 + (sums ? kTileWaves * (1024 + (size_t)heads * c.s) : 0));
+            const bool sums = g->grad_bias && c.s;                 // dx of 32 rows and the slots, of every wavefront
+            forward_side.take(*this, table, heads, false, sums, biases + 3 + (sums ? kTileWaves * (kDxFloats + (size_t)heads * c.s + 1) : 0));
             backward_side.take(*this, table, 1, true, false, (t.bias ? (size_t)group : 1) * (c.s + 1));
         }
         ISO_TRY(upload_table(b, table.bytes.data(), table.bytes.size()));
@@ -359,6 +360,7 @@ class AttentionBinder {
             a.grad_k = device_heads(g->grad_k);
             a.grad_v = device_heads(g->grad_v);
             a.delta = (float *)((char *)workspace + work.delta);
+            a.starts = (float *)((char *)workspace + work.starts);
             a.partials = (float *)((char *)workspace + work.partials);
         }
     }
@@ -375,7 +377,7 @@ class AttentionBinder {
     struct Side {
         bool tiles = false;
         TilePlan plan;
-        size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots_of = 0, slots = 0, pairs = 0, zeros = 0;
+        size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots = 0, zeros = 0;
         int chunks = 0;
 
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
@@ -393,11 +395,7 @@ class AttentionBinder {
             active = table.add(plan.active);
             index = table.add(plan.index);
             zeros = table.add(std::vector<uint16_t>(kTileMaxHeadDim));
-            if (sums) {
-                slots_of = table.add(plan.slots_of);
-                slots = table.add(plan.slots);
-                pairs = table.add(plan.pairs);
-            }
+            if (sums) slots = table.add(plan.slots);
             tiles = true;
         }
     };
@@ -425,10 +423,10 @@ class AttentionBinder {
         ta.active = (const uint32_t *)(base + side.active);
         ta.index = (const uint16_t *)(base + side.index);
         ta.zeros = base + side.zeros;
-        if (!p.slots_of.empty()) {
-            ta.slots_of = (const uint32_t *)(base + side.slots_of);
-            ta.slots = (const TilePlan::Slot *)(base + side.slots);
-            ta.pairs = (const uint16_t *)(base + side.pairs);
+        if (!p.slots.empty()) {
+            ta.slots = (const uint32_t *)(base + side.slots);
+            ta.slot_rounds = p.slot_rounds;
+            ta.slot_words = p.slot_words;
         }
         ta.per_xcd = (uint32_t)((work + 7) / 8);
         return add_launch(b, func, (uint64_t)ta.per_xcd * 8, 256, ta, side.lds);

@@ -29,22 +29,20 @@ struct TilePlan {
     std::vector<int16_t> column_at;        // [kTileColumns / heads][words * 4]
     std::vector<int16_t> row_at;           // [chunks * kChunkRows][words * 4]
     std::vector<uint32_t> active;          // [chunks]: bit 4 * wave + group: that block holds a neighbour
-    // The bias's gradient, for columns that are ranks: which pairs of a (chunk, wavefront) belong to one slot
-    // (head of the column) * s + neighbour.  Slots with the most pairs first.
-    struct Slot {
-        uint32_t slot, first, count;
-    };
-    std::vector<uint32_t> slots_of;        // [chunks * kTileWaves + 1]: first of `slots`
-    std::vector<Slot> slots;
-    std::vector<uint16_t> pairs;           // slot_pair of each
-    // [chunks * 4][kTileWaves][64][4]: of (lane's column, row 4 * (lane / 16) + r) of the 16 rows of a group, four times
-    // (column's head) * (s + 1) + neighbour, with s for the neighbour where it is none
+    // The bias's gradient, for columns that are ranks.  A slot is (head of the column) * s + neighbour; its pairs among 32 rows and
+    // the 16 columns of a wavefront, at most one a column, are places in what the wavefront's lanes wrote (slot_place).
+    // [chunks * 2][kTileWaves][slot_rounds]: 64 slots, one a lane, then [slot_words][64][8] places as 16-bit numbers.  Lanes
+    // without a slot name the one behind the last, and places without a pair the zero behind the last.
+    int slot_rounds = 0, slot_words = 0;
+    std::vector<uint32_t> slots;
+    // [chunks * 2][kTileWaves][64][2][4]: of (lane's column, row 4 * (lane / 16) + r) of the 16 rows of either group of a pair, four
+    // times (column's head) * (s + 1) + neighbour, with s for the neighbour where it is none
     std::vector<uint16_t> index;
 };
 
-// Where a wavefront keeps the pair of a column (0..15) and a row of the chunk (0..63): lane (row % 16 / 4) * 16 + column writes
-// four rows at once.
-inline uint16_t slot_pair(int column, int row) { return (uint16_t)(((row / 16 * 64) + (row % 16 / 4) * 16 + column) * 4 + row % 4); }
+// Lane (row % 16 / 4) * 16 + column writes four rows of either half at once.
+inline uint32_t slot_place(int column, int row) { return (uint32_t)((row / 16 * 64 + row % 16 / 4 * 16 + column) * 4 + row % 4); }
+constexpr uint32_t kSlotZero = 512;
 
 struct TileShape {
     std::array<int32_t, ISO_MAX_DIMS> tile{}, wave{}, tiles{};
@@ -199,7 +197,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     p.row_at.assign((size_t)p.chunks * kChunkRows * width, 0);
     p.active.assign((size_t)p.chunks, 0);
     p.index.resize((size_t)p.chunks * 4 * kTileWaves * 64 * 4);
-    for (size_t i = 0; i < p.index.size(); ++i) p.index[i] = (uint16_t)(4 * ((int)(i / 4 % 16) % heads * (c.s + 1) + c.s));
+    for (size_t i = 0; i < p.index.size(); ++i) p.index[i] = (uint16_t)(4 * ((int)(i / 8 % 16) % heads * (c.s + 1) + c.s));
     std::vector<int> rank_of((size_t)p.rows);
     for (int u = 0; u < p.rows; ++u) {
         rank_of[order[u]] = u;
@@ -211,33 +209,45 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
         for (int h = 0; h < heads; ++h) {
             const int column = r * heads + h, w = column / 16;
             const int lane = lane_row / 4 * 16 + column % 16;
-            p.index[(((size_t)group * kTileWaves + w) * 64 + lane) * 4 + lane_row % 4] = (uint16_t)(4 * (h * (c.s + 1) + i));
+            p.index[(((size_t)(group / 2) * kTileWaves + w) * 64 + lane) * 8 + group % 2 * 4 + lane_row % 4] = (uint16_t)(4 * (h * (c.s + 1) + i));
             p.active[group / 4] |= 1u << (4 * w + group % 4);
         }
     }
     for (uint32_t a : p.active) p.blocks += __builtin_popcount(a);
     if (bias_slots) {
-        std::vector<std::vector<std::pair<uint32_t, uint16_t>>> of((size_t)p.chunks * kTileWaves);
+        std::vector<std::vector<std::pair<uint32_t, uint32_t>>> of((size_t)p.chunks * 2 * kTileWaves);
         for (const auto &[pair, i] : taken) {
             const int r = (int)(pair >> 32), u = rank_of[(size_t)(pair & 0xFFFFFFFF)];
             for (int h = 0; h < heads; ++h) {
                 const int column = r * heads + h;
-                of[(size_t)(u / kChunkRows) * kTileWaves + column / 16].push_back(
-                    {(uint32_t)(h * c.s + i), slot_pair(column % 16, u % kChunkRows)});
+                of[(size_t)(u / 32) * kTileWaves + column / 16].push_back({(uint32_t)(h * c.s + i), slot_place(column % 16, u % 32)});
             }
         }
+        size_t most = 1;
         for (auto &list : of) {
-            p.slots_of.push_back((uint32_t)p.slots.size());
             std::sort(list.begin(), list.end());
-            const size_t begin = p.slots.size();
-            for (const auto &[slot, at] : list) {
-                if (p.slots.size() == begin || p.slots.back().slot != slot) p.slots.push_back({slot, (uint32_t)p.pairs.size(), 0});
-                ++p.slots.back().count;
-                p.pairs.push_back(at);
-            }
-            std::stable_sort(p.slots.begin() + begin, p.slots.end(), [](const auto &x, const auto &y) { return x.count > y.count; });
+            size_t n = 0;
+            for (size_t k = 0; k < list.size(); ++k) n += !k || list[k].first != list[k - 1].first;
+            most = std::max(most, n);
         }
-        p.slots_of.push_back((uint32_t)p.slots.size());
+        p.slot_rounds = (int)((most + 63) / 64);
+        p.slot_words = 16 / heads > 8 ? 2 : 1;
+        const size_t round = 64 + 256 * (size_t)p.slot_words;
+        p.slots.assign(of.size() * p.slot_rounds * round, kSlotZero | kSlotZero << 16);
+        for (size_t l = 0; l < of.size(); ++l) {
+            uint32_t *at = p.slots.data() + l * p.slot_rounds * round;
+            for (int n = 0; n < p.slot_rounds; ++n) std::fill_n(at + n * round, 64, (uint32_t)(heads * c.s));
+            int lane = -1, count = 0;
+            for (size_t k = 0; k < of[l].size(); ++k) {
+                const auto &[slot, place] = of[l][k];
+                if (!k || slot != of[l][k - 1].first) ++lane, count = 0;
+                uint32_t *mine = at + lane / 64 * round;
+                mine[lane % 64] = slot;
+                uint32_t &word = mine[64 + count / 8 * 256 + lane % 64 * 4 + count % 8 / 2];
+                word = count % 2 ? (word & 0xFFFF) | place << 16 : (word & 0xFFFF0000) | place;
+                ++count;
+            }
+        }
     }
     out = std::move(p);
     return true;

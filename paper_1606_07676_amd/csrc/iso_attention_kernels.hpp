@@ -46,6 +46,7 @@ struct AttentionArgs {
     float *lse;                            // [n][q_heads]
     float *delta;                          // [p][q_heads]: grad_out . out of every row, for the gradients of k and v
     float *starts;                         // [2][p][q_heads]: -lse / scale (cap: lse log2 e) and -delta, for the tile kernels
+    float *norms;                          // [p][q_heads]: 1 / (sum of the weights), of rows with a large lse
     float *partials;                       // [parts][q_heads * s] of the bias's gradient
     const void *bias;                      // [q_heads][s] of the tensors' type, or null
     const int32_t *segments;               // [p] or null
@@ -122,16 +123,24 @@ __device__ __forceinline__ int32_t neighbour_rank(const NeighbourTorus &t, const
     int32_t rank = 0;
     bool there = true;
     const int32_t *c = t.offsets + (int64_t)i * t.d;
-    for (int j = 0; j < t.d; ++j) {
-        const int32_t n = t.dims[j];
-        int32_t x = TARGET ? coords[j] + c[j] : coords[j] - c[j];
-        if (t.open >> j & 1) {
-            there = there && (uint32_t)x < (uint32_t)n;
-        } else {
-            x += x < 0 ? n : 0;
-            x -= x >= n ? n : 0;
+    for (int first = 0; first < t.d; first += 4) {                  // four offsets under way at a time
+        int32_t step[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) step[q] = first + q < t.d ? c[first + q] : 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int j = first + q;
+            if (j >= t.d) break;
+            const int32_t n = t.dims[j];
+            int32_t x = TARGET ? coords[j] + step[q] : coords[j] - step[q];
+            if (t.open >> j & 1) {
+                there = there && (uint32_t)x < (uint32_t)n;
+            } else {
+                x += x < 0 ? n : 0;
+                x -= x >= n ? n : 0;
+            }
+            rank += x * t.inner[j];
         }
-        rank += x * t.inner[j];
     }
     return there ? rank : -1;
 }
@@ -262,19 +271,31 @@ __global__ __launch_bounds__(1024) void attention_split_row_kernel(const Attenti
     RowState<E> st;
     if (inside) attend_row<T, WIDE>(a, row, (uint32_t)rank, h, wave, a.waves, coords, st);
     const bool holds = lane >> a.lanes_log2 == 0 && lane * E < kAttentionMaxHeadDim;
-    if (wave > 0) {
-        if (lane == 0) part_m[wave] = st.m, part_l[wave] = st.l;
-        if (holds)
+    if (lane == 0) part_m[wave] = st.m, part_l[wave] = st.l;
+    if (holds)
 #pragma unroll
-            for (int e = 0; e < E; ++e) part_acc[wave][lane * E + e] = st.acc[e];
-    }
+        for (int e = 0; e < E; ++e) part_acc[wave][lane * E + e] = st.acc[e];
     __syncthreads();
     if (wave > 0) return;
-    for (int w = 1; w < a.waves; ++w) {
-        float o[E];
+    // lane w weighs part w; then every lane adds up its elements of all parts, whose reads do not wait for each other
+    const float m = lane < a.waves ? part_m[lane] : -INFINITY;
+    float top = m;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = holds ? part_acc[w][lane * E + e] : 0.f;
-        st.merge(part_m[w], part_l[w], o);
+    for (int b = 0; b < 4; ++b) top = fmaxf(top, __shfl_xor(top, 1 << b));
+    top = __shfl(top, 0);
+    const float weight = exp_above(m, finite_floor(top));
+    float l = lane < a.waves ? part_l[lane] * weight : 0.f;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) l += __shfl_xor(l, 1 << b);
+    st.m = top;
+    st.l = __shfl(l, 0);
+#pragma unroll
+    for (int e = 0; e < E; ++e) st.acc[e] = 0.f;
+    for (int w = 0; w < a.waves; ++w) {
+        const float by = __shfl(weight, w);
+        if (holds)
+#pragma unroll
+            for (int e = 0; e < E; ++e) st.acc[e] = fmaf(part_acc[w][lane * E + e], by, st.acc[e]);
     }
     write_row<T, WIDE>(a, row, h, st);
 }
@@ -287,11 +308,15 @@ __global__ __launch_bounds__(1024) void attention_split_row_kernel(const Attenti
 //
 // Every gradient is gathered by the row that it belongs to: no atomics, and the same sum in the same order every time.
 
-// P_i and da_i of one neighbour whose dot products are given; x without the neighbour's own bias.
+// Beyond this lse its own rounding shows in the weights (by 2^-11 and more; where every bias of a row is the type's lowest
+// value, the logarithm of their sum is lost whole): weights are then divided by what they add up to.
+constexpr float kLargeLse = 8192.f;
+
+// P_i and da_i of one neighbour whose dot products are given; norm: 1, or what corrects the weights of a large lse.
 struct PairGradient {
     float p, dx, da;
 };
-__device__ __forceinline__ PairGradient pair_gradient(float dot, float bias, float lse, float dp, float delta, float scale, float cap) {
+__device__ __forceinline__ PairGradient pair_gradient(float dot, float bias, float lse, float norm, float dp, float delta, float scale, float cap) {
     float t = dot * scale, slope = 1.f;
     if (cap > 0.f) {
         t = capped(t, cap);
@@ -299,7 +324,7 @@ __device__ __forceinline__ PairGradient pair_gradient(float dot, float bias, flo
         slope = 1.f - y * y;
     }
     PairGradient g;
-    g.p = exp_above(t + bias, finite_floor(lse));
+    g.p = exp_above(t + bias, finite_floor(lse)) * norm;
     g.dx = g.p * (dp - delta);
     g.da = g.dx * slope;
     return g;
@@ -316,8 +341,10 @@ __device__ __forceinline__ float row_delta(const AttentionArgs &a, uint32_t rank
     return sum_over_lanes<E>(x, a.lanes_log2);
 }
 
+// bias_sums: of the row's head, to which dx is added, or null.
 template <typename T, bool WIDE>
-__device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank, int h, float delta, const int32_t *coords) {
+__device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank, int h, float delta, const int32_t *coords,
+                                           float *bias_sums = nullptr) {
     constexpr int E = ElementTraits<T>::kPerLane;
     const NeighbourTorus &t = a.torus;
     const int lane = threadIdx.x & 63, L = a.lanes_log2, sets = 64 >> L;
@@ -329,6 +356,24 @@ __device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank
     load_elements<T, WIDE>((const T *)a.grad_out.data + rank * a.grad_out.rank_stride + h * a.grad_out.head_stride, at, a.head_dim, g);
     const T *k0 = (const T *)a.k.data + hk * a.k.head_stride, *v0 = (const T *)a.v.data + hk * a.v.head_stride;
     const T *bias = a.bias ? (const T *)a.bias + (int64_t)h * t.s : nullptr;
+    float norm = 1.f, sum = 0.f;
+    const bool large = fabsf(lse) > kLargeLse && fabsf(lse) < INFINITY;
+    if (large) {                                                    // what the weights add up to
+        for (int i0 = 0; i0 < (own < 0 ? 0 : t.s); i0 += sets) {
+            const int i = i0 + (lane >> L);
+            int32_t src = i < t.s ? neighbour_rank<false>(t, coords, i) : -1;
+            if (src >= 0 && a.segments && a.segments[src] != own) src = -1;
+            float k[E], x = 0.f;
+            load_elements<T, WIDE>(k0 + (src < 0 ? 0 : src) * a.k.rank_stride, at, src < 0 ? 0 : a.head_dim, k);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
+            x = sum_over_lanes<E>(x, L);
+            if (src >= 0) sum += pair_gradient(x, bias ? (float)bias[i] : 0.f, lse, 1.f, 0.f, 0.f, a.scale, a.cap).p;
+        }
+        sum = sum_across_groups(sum, L);
+        norm = sum > 0.f ? 1.f / sum : 1.f;
+        if (lane == 0) a.norms[(int64_t)rank * a.q_heads + h] = norm;
+    }
     for (int i0 = 0; i0 < (own < 0 ? 0 : t.s); i0 += sets) {
         const int i = i0 + (lane >> L);
         int32_t src = i < t.s ? neighbour_rank<false>(t, coords, i) : -1;
@@ -341,9 +386,10 @@ __device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank
         x = sum_over_lanes<E>(x, L);
         dp = sum_over_lanes<E>(dp, L);
         if (src >= 0) {
-            const float da = pair_gradient(x, bias ? (float)bias[i] : 0.f, lse, dp, delta, a.scale, a.cap).da;
+            const PairGradient pg = pair_gradient(x, bias ? (float)bias[i] : 0.f, lse, norm, dp, delta, a.scale, a.cap);
+            if (bias_sums && at == 0) bias_sums[i] += pg.dx;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(da, k[e], acc[e]);
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(pg.da, k[e], acc[e]);
         }
     }
 #pragma unroll
@@ -368,10 +414,15 @@ __global__ __launch_bounds__(256) void attention_grad_q_row_kernel(const Attenti
         const int64_t at = (int64_t)rank * a.q_heads + h;
         const float lse = finite_floor(a.lse[at]);
         a.delta[at] = delta;
-        a.starts[at] = fabsf(lse) > 1e30f ? NAN : a.cap > 0.f ? lse * kLog2e : -lse / a.scale;
+        a.starts[at] = fabsf(lse) > kLargeLse ? NAN : a.cap > 0.f ? lse * kLog2e : -lse / a.scale;
         a.starts[(int64_t)a.n * a.q_heads + at] = -delta;
     }
     grad_q_row<T, WIDE>(a, rank, h, delta, coords[wave]);
+}
+
+// The grad_q kernels, which run first, have left it for rows with a large lse.
+__device__ __forceinline__ float norm_of(const AttentionArgs &a, int64_t rank, int h, float lse) {
+    return fabsf(lse) > kLargeLse && fabsf(lse) < INFINITY ? a.norms[rank * a.q_heads + h] : 1.f;
 }
 
 // grad_k and grad_v of one (rank, kv head): all ranks R (+) C^i and all q heads of the group.
@@ -401,7 +452,8 @@ __device__ __forceinline__ void grad_kv_row(const AttentionArgs &a, uint32_t ran
             dp = sum_over_lanes<E>(dp, L);
             if (dst >= 0) {
                 const float b = a.bias ? (float)((const T *)a.bias)[(int64_t)h * t.s + i] : 0.f;
-                const PairGradient pg = pair_gradient(x, b, a.lse[r * a.q_heads + h], dp, a.delta[r * a.q_heads + h], a.scale, a.cap);
+                const float lse = a.lse[r * a.q_heads + h], norm = norm_of(a, r, h, lse);
+                const PairGradient pg = pair_gradient(x, b, lse, norm, dp, a.delta[r * a.q_heads + h], a.scale, a.cap);
 #pragma unroll
                 for (int e = 0; e < E; ++e) dk[e] = fmaf(pg.da, q[e], dk[e]), dv[e] = fmaf(pg.p, g[e], dv[e]);
             }
@@ -470,8 +522,10 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
         for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x), dp = fmaf(g[e], v[e], dp);
         x = sum_over_lanes<E>(x, L);
         dp = sum_over_lanes<E>(dp, L);
-        if (src >= 0)
-            sum += pair_gradient(x, bias, a.lse[r * a.q_heads + h], dp, a.delta[r * a.q_heads + h], a.scale, a.cap).dx;
+        if (src >= 0) {
+            const float lse = a.lse[r * a.q_heads + h];
+            sum += pair_gradient(x, bias, lse, norm_of(a, r, h, lse), dp, a.delta[r * a.q_heads + h], a.scale, a.cap).dx;
+        }
     }
     sum = sum_across_groups(sum, L);
     if (lane == 0) a.partials[(uint64_t)part * slots + slot] = sum;

@@ -590,7 +590,7 @@ struct SlotRound {
 };
 
 template <typename T, int DP, bool SEGMENTS>
-__global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const TileArgs t) {
+__global__ __launch_bounds__(256, 3) void attention_grad_q_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
     typedef TileLds<DP> Lds;
     constexpr int G = Lds::kGroups;
@@ -629,27 +629,20 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
     }
     lse = finite_floor(lse);
     if (rank >= 0 && lane < 16) {
-        // what the other pass starts its products at; an lse that cannot be scaled (see below) is a NaN there, and whoever reads
-        // the row is made again
+        // what the other pass starts its products at; a large lse is a NaN there, and whoever reads the row is made again
         const int64_t at = rank * a.q_heads + head;
         const GradientFactors f(a);
         a.delta[at] = delta;
-        a.starts[at] = fabsf(lse) > 1e30f ? NAN : a.cap > 0.f ? lse * kLog2e : f.start(a, lse);
+        a.starts[at] = fabsf(lse) > kLargeLse ? NAN : a.cap > 0.f ? lse * kLog2e : f.start(a, lse);
         a.starts[(int64_t)a.n * a.q_heads + at] = -delta;
     }
     const LanePieces<T, DP> pieces;
     const RowLoads<DP, SEGMENTS> loads(t, a.k, a.v, work.key_head);
     const GradientFactors factors(a);
-    // Biases near the type's lowest value alone: lse cannot be scaled.  Such a wavefront makes its weights the long way.
-    const bool low = __any(fabsf(lse) > 1e30f);
-    const f4 from = f4{1.f, 1.f, 1.f, 1.f} * (low ? 0.f : factors.start(a, lse)), from_dp = f4{-1.f, -1.f, -1.f, -1.f} * delta;
-    const float lse2 = lse * kLog2e;
-    const auto low_pair = [&](float dot, uint32_t at, float dp, bool counts) {
-        const int n = (int)at / 4 - column % t.heads * (s + 1);
-        const PairGradient none = {0.f, 0.f, 0.f};
-        if (n == s || (SEGMENTS && !counts)) return none;
-        return pair_gradient(dot, (float)((const T *)a.bias)[(int64_t)head * s + n], lse, dp, 0.f, a.scale, a.cap);
-    };
+    // A column with a large lse is made again below, its part of the bias's gradient with it.
+    const bool large = fabsf(lse) > kLargeLse;
+    const f4 from = f4{1.f, 1.f, 1.f, 1.f} * (large ? NAN : factors.start(a, lse)), from_dp = f4{-1.f, -1.f, -1.f, -1.f} * delta;
+    const float lse2 = large ? NAN : lse * kLog2e;
     __syncthreads();
 
     f4 acc[DP / 16] = {};
@@ -684,24 +677,14 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
                 const int g = 2 * pair + half;
                 const i4 seg = SEGMENTS ? *(const i4 *)(lds.segment + chunk * Lds::kRows + g * 16 + lane / 16 * 4) : i4{};
                 f4 dx;
-                if (low) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const PairGradient pg = low_pair(dot[half][r], pairs.at(g, r), dp[half][r],
-                                                         (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
-                        dx[r] = pg.dx;
-                        da[half][r] = pg.da;
-                    }
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const PairGradient pg = factors.template operator()<SEGMENTS>(
-                            dot[half][r], bias[half][r], lse2, dp[half][r], (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
-                        dx[r] = pg.dx;
-                        da[half][r] = pg.da;
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    const PairGradient pg = factors.template operator()<SEGMENTS>(
+                        dot[half][r], bias[half][r], lse2, dp[half][r], (r == 0 ? seg.x : r == 1 ? seg.y : r == 2 ? seg.z : seg.w) == own);
+                    dx[r] = pg.dx;
+                    da[half][r] = pg.da;
                 }
-                if (t.slots) *(f4 *)(dx_at + (half * 64 + lane) * 4) = rank >= 0 ? dx : f4{0.f, 0.f, 0.f, 0.f};
+                if (t.slots) *(f4 *)(dx_at + (half * 64 + lane) * 4) = rank >= 0 && !large ? dx : f4{0.f, 0.f, 0.f, 0.f};
             }
             pieces.add_weighted_rows(rows + pair * 32 * Lds::kRowBytes, as_weights<T>(da[0], da[1]), acc);
             if (t.slots)                                            // every lane adds up the pairs of one slot in 32 rows
@@ -718,7 +701,8 @@ __global__ __launch_bounds__(256, 2) void attention_grad_q_tile_kernel(const Til
         const float row_delta = __shfl(delta, c);
         store_coordinates(a.torus, r, lane, coords[wave]);
         __builtin_amdgcn_wave_barrier();
-        grad_q_row<T, true>(a, r, h, row_delta, coords[wave]);
+        const bool bias_too = t.slots && __shfl((int)large, c);
+        grad_q_row<T, true>(a, r, h, row_delta, coords[wave], bias_too ? sums + (h - first_head) * s : nullptr);
         __builtin_amdgcn_wave_barrier();
     });
     if (t.slots) {

@@ -242,14 +242,14 @@ inline const void *sum_parts_by_type(int dtype) {
     }
 }
 
-// Parts of the ranks that the bias's gradient is summed over: enough wavefronts for the GPU, 64 ranks or more in each.
+// Parts of the ranks that the bias's gradient is summed over: enough wavefronts for the GPU, 16 ranks or more in each.
 inline uint64_t bias_parts(const Comm &c, int q_heads) {
     const uint64_t slots = std::max<uint64_t>(1, (uint64_t)q_heads * c.s);
-    return std::clamp<uint64_t>(8192 / slots, 1, ((uint64_t)c.p + 63) / 64);
+    return std::clamp<uint64_t>(8192 / slots, 1, ((uint64_t)c.p + 15) / 16);
 }
 
 struct BackwardWorkspace {
-    uint64_t delta = 0, starts = 0, partials = 0, bytes = 0;     // offsets
+    uint64_t delta = 0, starts = 0, norms = 0, partials = 0, bytes = 0;     // offsets
 };
 inline int tile_heads(int group) {             // q heads of a rank that one tile of columns takes together
     int heads = 1;
@@ -259,7 +259,8 @@ inline int tile_heads(int group) {             // q heads of a rank that one til
 inline int backward_workspace(const Comm &c, int q_heads, int kv_heads, bool bias, BackwardWorkspace &w) {
     const uint64_t rows = (uint64_t)c.p * q_heads;               // below 2^47
     w.starts = (rows * 4 + 255) / 256 * 256;
-    w.partials = w.starts + (rows * 8 + 255) / 256 * 256;
+    w.norms = w.starts + (rows * 8 + 255) / 256 * 256;
+    w.partials = w.norms + (rows * 4 + 255) / 256 * 256;
     w.bytes = w.partials;
     if (bias) {
         if ((uint64_t)q_heads * c.s > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
@@ -361,6 +362,7 @@ class AttentionBinder {
             a.grad_v = device_heads(g->grad_v);
             a.delta = (float *)((char *)workspace + work.delta);
             a.starts = (float *)((char *)workspace + work.starts);
+            a.norms = (float *)((char *)workspace + work.norms);
             a.partials = (float *)((char *)workspace + work.partials);
         }
     }

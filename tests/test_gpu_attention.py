@@ -258,6 +258,24 @@ def test_biases_that_mask(shape, dtype):
     assert bool(torch.isfinite(lse[:, 0]).all()) and bool((lse[:, 0] < -3e38).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("shape", ["picture", "volume", "volume_mesh"])
+def test_gradients_of_rows_whose_biases_are_all_lowest(shape, cap, dtype):
+    """Equal weights, whatever the scores, in every gradient that depends on the weights alone."""
+    t = tensors(10, shape, dtype, bias=True)
+    t["bias"][0, :] = torch.finfo(TYPES[dtype]).min
+    out, lse = forward(shape, t, cap)
+    grad_out = torch.randn(t["q"].shape, device=DEV, generator=torch.Generator(DEV).manual_seed(9)).to(out.dtype)
+    got = backward(shape, t, out, lse, grad_out, cap)
+    flat = {k: v.clone() if v is not None else None for k, v in t.items()}
+    flat["q"][:, 0], flat["bias"][0] = 0, 0
+    want = oracle(shape, flat, cap).backward(host(grad_out), host(out))
+    for name in ("grad_v", "grad_bias"):
+        within(got[name], want[name][0], orc.gradient_bound(*want[name], out.dtype), name)
+    assert all(bool(torch.isfinite(g).all()) for g in got.values())
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_large_scores(dtype):
     t = tensors(11, "picture", dtype, bias=True)

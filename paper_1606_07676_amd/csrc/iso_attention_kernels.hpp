@@ -98,8 +98,9 @@ __device__ __forceinline__ void store_elements(T *row, int at, int end, const fl
     }
 }
 
-// cap * tanh(a / cap): tanh y = 1 - 2 / (1 + e^2y), whose error is absolute (2^-23 of the cap), as a score's has to be.
-__device__ __forceinline__ float capped(float a, float cap) {
+// cap * tanh(a / cap).  For 16-bit tensors tanh y = 1 - 2 / (1 + e^2y), whose error is 2^-23 of the cap whatever the score.
+template <typename T> __device__ __forceinline__ float capped(float a, float cap) {
+    if constexpr (sizeof(T) == 4) return cap * tanhf(a / cap);
     const float e = __builtin_amdgcn_exp2f(a * (2.f * kLog2e / cap));
     return cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + e);
 }
@@ -200,7 +201,7 @@ __device__ __forceinline__ void attend_row(const AttentionArgs &a, uint32_t row,
 #pragma unroll
         for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
         x = sum_over_lanes<E>(x, L) * a.scale;
-        if (a.cap > 0.f) x = capped(x, a.cap);
+        if (a.cap > 0.f) x = capped<T>(x, a.cap);
         if (bias && src >= 0) x += (float)bias[i];
         if (src < 0) x = -INFINITY;
         const float top = fmaxf(st.m, x), base = finite_floor(top);
@@ -316,10 +317,11 @@ constexpr float kLargeLse = 8192.f;
 struct PairGradient {
     float p, dx, da;
 };
+template <typename T>
 __device__ __forceinline__ PairGradient pair_gradient(float dot, float bias, float lse, float norm, float dp, float delta, float scale, float cap) {
     float t = dot * scale, slope = 1.f;
     if (cap > 0.f) {
-        t = capped(t, cap);
+        t = capped<T>(t, cap);
         const float y = t / cap;
         slope = 1.f - y * y;
     }
@@ -368,7 +370,7 @@ __device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank
 #pragma unroll
             for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
             x = sum_over_lanes<E>(x, L);
-            if (src >= 0) sum += pair_gradient(x, bias ? (float)bias[i] : 0.f, lse, 1.f, 0.f, 0.f, a.scale, a.cap).p;
+            if (src >= 0) sum += pair_gradient<T>(x, bias ? (float)bias[i] : 0.f, lse, 1.f, 0.f, 0.f, a.scale, a.cap).p;
         }
         sum = sum_across_groups(sum, L);
         norm = sum > 0.f ? 1.f / sum : 1.f;
@@ -386,7 +388,7 @@ __device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank
         x = sum_over_lanes<E>(x, L);
         dp = sum_over_lanes<E>(dp, L);
         if (src >= 0) {
-            const PairGradient pg = pair_gradient(x, bias ? (float)bias[i] : 0.f, lse, norm, dp, delta, a.scale, a.cap);
+            const PairGradient pg = pair_gradient<T>(x, bias ? (float)bias[i] : 0.f, lse, norm, dp, delta, a.scale, a.cap);
             if (bias_sums && at == 0) bias_sums[i] += pg.dx;
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[e] = fmaf(pg.da, k[e], acc[e]);
@@ -453,7 +455,7 @@ __device__ __forceinline__ void grad_kv_row(const AttentionArgs &a, uint32_t ran
             if (dst >= 0) {
                 const float b = a.bias ? (float)((const T *)a.bias)[(int64_t)h * t.s + i] : 0.f;
                 const float lse = a.lse[r * a.q_heads + h], norm = norm_of(a, r, h, lse);
-                const PairGradient pg = pair_gradient(x, b, lse, norm, dp, a.delta[r * a.q_heads + h], a.scale, a.cap);
+                const PairGradient pg = pair_gradient<T>(x, b, lse, norm, dp, a.delta[r * a.q_heads + h], a.scale, a.cap);
 #pragma unroll
                 for (int e = 0; e < E; ++e) dk[e] = fmaf(pg.da, q[e], dk[e]), dv[e] = fmaf(pg.p, g[e], dv[e]);
             }
@@ -524,7 +526,7 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
         dp = sum_over_lanes<E>(dp, L);
         if (src >= 0) {
             const float lse = a.lse[r * a.q_heads + h];
-            sum += pair_gradient(x, bias, lse, norm_of(a, r, h, lse), dp, a.delta[r * a.q_heads + h], a.scale, a.cap).dx;
+            sum += pair_gradient<T>(x, bias, lse, norm_of(a, r, h, lse), dp, a.delta[r * a.q_heads + h], a.scale, a.cap).dx;
         }
     }
     sum = sum_across_groups(sum, L);

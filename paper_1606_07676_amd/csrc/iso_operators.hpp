@@ -222,6 +222,7 @@ ISO_TILE_KERNEL(GradKVTileKernel, attention_grad_kv_tile_kernel)
 #undef ISO_TILE_KERNEL
 
 constexpr int kTileMaxHeadDim = 128;
+constexpr double kTileMaxDilution = 24;    // pairs in a tile's blocks for one that is a neighbour
 constexpr size_t kTileMaxLds = 64 << 10;
 inline int tile_head_dim(int head_dim) { return (head_dim + 31) / 32 * 32; }
 inline int tile_chunk_rows(int head_dim) { return tile_head_dim(head_dim) > 32 ? TileLds<64>::kRows : TileLds<32>::kRows; }
@@ -264,7 +265,9 @@ inline int backward_workspace(const Comm &c, int q_heads, int kv_heads, bool bia
     w.bytes = w.partials;
     if (bias) {
         if ((uint64_t)q_heads * c.s > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
-        const uint64_t parts = std::max<uint64_t>(bias_parts(c, q_heads), (uint64_t)tile_shape(c, tile_heads(q_heads / kv_heads)).n_tiles);
+        uint64_t parts = bias_parts(c, q_heads);
+        for (int heads = tile_heads(q_heads / kv_heads); heads; heads /= 2)
+            parts = std::max<uint64_t>(parts, (uint64_t)tile_shape(c, heads).n_tiles);
         w.bytes += parts * q_heads * c.s * 4;
     }
     return ISO_SUCCESS;
@@ -293,15 +296,13 @@ class AttentionBinder {
         Table table;
         table.add(kernel_offsets(c));
         choose_width();
-        const int group = t.q_heads / t.kv_heads, heads = tile_heads(group);
-        const size_t biases = (size_t)heads * (c.s + 1);
-        if (!g) {
-            forward_side.take(*this, table, heads, false, false, biases);
-        } else {
-            const bool sums = g->grad_bias && c.s;                 // dx of 32 rows and the slots, of every wavefront
-            forward_side.take(*this, table, heads, false, sums, biases + 3 + (sums ? kTileWaves * (kDxFloats + (size_t)heads * c.s + 1) : 0));
-            backward_side.take(*this, table, 1, true, false, (t.bias ? (size_t)group : 1) * (c.s + 1));
-        }
+        const int group = t.q_heads / t.kv_heads;
+        const bool sums = g && g->grad_bias && c.s;                // dx of 32 rows and the slots, of every wavefront
+        // fewer heads together where what they need does not fit in LDS
+        for (int heads = tile_heads(group); heads && !forward_side.tiles; heads /= 2)
+            forward_side.take(*this, table, heads, false, sums,
+                              (size_t)heads * (c.s + 1) + (sums ? 3 + kTileWaves * (kDxFloats + (size_t)heads * c.s + 1) : 0));
+        if (g) backward_side.take(*this, table, 1, true, false, (t.bias ? (size_t)group : 1) * (c.s + 1));
         ISO_TRY(upload_table(b, table.bytes.data(), table.bytes.size()));
         fill_args(workspace);
         return g ? backward() : forward();
@@ -391,7 +392,7 @@ class AttentionBinder {
             const int chunk = tile_chunk_rows(o.t.head_dim);
             chunks = (plan.rows + chunk - 1) / chunk;
             lds = tile_lds_bytes(o.t.head_dim, chunks, floats);
-            if (lds > kTileMaxLds || plan.blocks * 256.0 > 12.0 * kTileColumns * o.c.s) return;
+            if (lds > kTileMaxLds || plan.blocks * 256.0 > kTileMaxDilution * kTileColumns * o.c.s) return;
             columns = table.add(plan.column_at);
             rows = table.add(plan.row_at);
             active = table.add(plan.active);

@@ -17,7 +17,7 @@ namespace iso {
 constexpr int kTileWaves = 4;              // wavefronts of a workgroup, 16 columns (rank, head) each
 constexpr int kTileColumns = 16 * kTileWaves;
 constexpr int kChunkRows = 64;             // rows (keys) that a workgroup holds in LDS at a time
-constexpr int kTileMaxRows = 2048;         // rows of a tile
+constexpr int kTileMaxRows = 4096;         // rows of a tile
 
 struct TilePlan {
     int heads = 1;                         // columns of one rank: column c is rank c / heads, head c % heads
@@ -180,9 +180,18 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
             }
             taken[(int64_t)r << 32 | copies[row.copy]] = i;
         }
-    // order: boxes of a wavefront's shape, so that the rows of 16 that a wavefront has no neighbour in are many
-    std::vector<int> order(rows.size());
-    for (size_t u = 0; u < order.size(); ++u) order[u] = (int)u;
+    // Order: boxes of a wavefront's shape, so that the groups of 16 rows that a wavefront has no neighbour in are many.  Where
+    // neighbours are few and far apart, so that few rows serve more than one column, the rows of one wavefront after those of
+    // the other (as they were found) leave fewer blocks.
+    std::vector<int> order(rows.size()), found(rows.size());
+    for (size_t u = 0; u < order.size(); ++u) order[u] = found[u] = (int)u;
+    const auto blocks_of = [&](const std::vector<int> &o) {
+        std::vector<int> place(o.size());
+        for (size_t u = 0; u < o.size(); ++u) place[o[u]] = (int)u;
+        std::vector<uint8_t> hit((o.size() + 15) / 16 * kTileWaves, 0);
+        for (const auto &[pair, i] : taken) hit[place[(size_t)(pair & 0xFFFFFFFF)] / 16 * kTileWaves + (int)(pair >> 32) / per_wave] = 1;
+        return std::count(hit.begin(), hit.end(), 1);
+    };
     std::sort(order.begin(), order.end(), [&](int a, int b) {
         for (int pass = 0; pass < 2; ++pass)
             for (int j = 0; j < d; ++j) {
@@ -192,6 +201,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
             }
         return rows[a].copy < rows[b].copy;
     });
+    if (blocks_of(found) < blocks_of(order)) order = found;
     p.rows = (int)rows.size();
     p.chunks = (p.rows + kChunkRows - 1) / kChunkRows;
     p.row_at.assign((size_t)p.chunks * kChunkRows * width, 0);

@@ -171,6 +171,32 @@ def fused(shape, dtype, seed, head_major=False, shift=0):
     return x[:, :nq], x[:, nq:nq + nk], x[:, nq + nk:]
 
 
+# neighbourhoods whose tables are large for the heads of one rank together, and whose neighbours have few rows in common
+WIDE = {
+    "shared_heads_of_many_neighbours": ((9, 8, 10), None, gen.moore(3, 3) + here(3), 4, 1, 128),
+    "pairs_of_heads_of_many_neighbours": ((9, 8, 10), [False, True, False], gen.moore(3, 3) + here(3), 4, 2, 64),
+    "scattered": ((7, 6, 5, 4), None, gen.random_distinct(4, -3, 3, 60, 11), 2, 1, 128),
+    "scattered_mesh": ((7, 6, 9, 4), [False, False, True, True], gen.random_distinct(4, -3, 3, 60, 12), 2, 2, 64),
+}
+
+
+@pytest.mark.parametrize("options", [dict(), dict(bias=True, segments=True)], ids=lambda o: "-".join(o) or "plain")
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", WIDE)
+def test_wide_neighbourhoods(shape, dtype, options, monkeypatch):
+    monkeypatch.setitem(SHAPES, shape, WIDE[shape])
+    t = tensors(16, shape, dtype, options.get("bias", False), options.get("segments", False))
+    out, lse = forward(shape, t)
+    want = oracle(shape, t)
+    within(lse, want.lse, want.lse_bound(), "lse")
+    within(out, want.out, want.out_bound(out.dtype), "out")
+    grad_out = torch.randn(t["q"].shape, device=DEV, generator=torch.Generator(DEV).manual_seed(17)).to(out.dtype)
+    got = backward(shape, t, out, lse, grad_out)
+    for name, parts in want.backward(host(grad_out), host(out)).items():
+        if got[name] is not None:
+            within(got[name], parts[0], orc.gradient_bound(*parts, out.dtype), name)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shape", ["picture", "volume", "half_mesh"])
 @pytest.mark.parametrize("head_major,shift", [(False, 0), (True, 0), (False, 3), (False, 8), (True, 1)])

@@ -222,7 +222,6 @@ ISO_TILE_KERNEL(GradKVTileKernel, attention_grad_kv_tile_kernel)
 #undef ISO_TILE_KERNEL
 
 constexpr int kTileMaxHeadDim = 128;
-constexpr double kTileMaxDilution = 24;    // pairs in a tile's blocks for one that is a neighbour
 constexpr size_t kTileMaxLds = 64 << 10;
 inline int tile_head_dim(int head_dim) { return (head_dim + 31) / 32 * 32; }
 inline int tile_chunk_rows(int head_dim) { return tile_head_dim(head_dim) > 32 ? TileLds<64>::kRows : TileLds<32>::kRows; }
@@ -383,6 +382,20 @@ class AttentionBinder {
         size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots = 0, zeros = 0;
         int chunks = 0;
 
+        // Tiles or rows.  A tile takes its chunks one after the other, 512 tiles side by side: 0.53 us a chunk forward and 2.35 us
+        // in both backward kernels together, whatever the neighbours in it.  Rows take pairs * head_dim / 1.35e6 us and
+        // / 0.29e6, which is a 1300th of the same measure either way, and no less than one row alone: 0.04 us a neighbour and
+        // 0.36 us.  Measured with 8 heads of 64, tiles to rows in us: 40 neighbours scattered in 4 dimensions, 630 ranks,
+        // 29.8 to 13.8 forward and 113 to 59 backward (45 chunks), 4096 ranks 52 to 60 and 191 to 285 (69 chunks); 343 in a
+        // cube, 300 ranks with 2 heads 39 to 20 and 180 to 156, with 8 heads 40 to 57 and 182 to 206, 4096 ranks 28 to 301 and
+        // 116 to 1695.
+        bool tiles_pay(const AttentionBinder &o, int heads, bool back) const {
+            const double group = o.t.q_heads / o.t.kv_heads, turns = back ? group : 1;
+            const double side_by_side = (double)plan.n_tiles * o.t.kv_heads * (back ? 1 : group / heads);
+            const double pairs = (double)o.c.p * o.t.q_heads * o.c.s, alone = (o.g ? 80.0 : 40.0) * turns * o.c.s;
+            return chunks * turns * std::max(512.0, side_by_side) <= 2000 + std::max(pairs * o.t.head_dim / 1300, alone);
+        }
+
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
             if (o.t.rows || o.t.dtype == ISO_DTYPE_F32 || !o.is_wide || o.t.head_dim > kTileMaxHeadDim) return;
             if (!(std::fabs(o.t.scale) > 1e-20f && std::fabs(o.t.scale) < 1e20f)) return;      // the kernels divide by it
@@ -392,7 +405,7 @@ class AttentionBinder {
             const int chunk = tile_chunk_rows(o.t.head_dim);
             chunks = (plan.rows + chunk - 1) / chunk;
             lds = tile_lds_bytes(o.t.head_dim, chunks, floats);
-            if (lds > kTileMaxLds || plan.blocks * 256.0 > kTileMaxDilution * kTileColumns * o.c.s) return;
+            if (lds > kTileMaxLds || !tiles_pay(o, heads, back)) return;
             columns = table.add(plan.column_at);
             rows = table.add(plan.row_at);
             active = table.add(plan.active);

@@ -223,6 +223,7 @@ ISO_TILE_KERNEL(GradKVTileKernel, attention_grad_kv_tile_kernel)
 
 constexpr int kTileMaxHeadDim = 128;
 constexpr size_t kTileMaxLds = 64 << 10;
+constexpr uint64_t kSplitWaves = 4096;     // wavefronts up to which a row's neighbours are shared out
 inline int tile_head_dim(int head_dim) { return (head_dim + 31) / 32 * 32; }
 inline int tile_chunk_rows(int head_dim) { return tile_head_dim(head_dim) > 32 ? TileLds<64>::kRows : TileLds<32>::kRows; }
 inline size_t tile_lds_bytes(int head_dim, int chunks, size_t biases) {
@@ -242,7 +243,9 @@ inline const void *sum_parts_by_type(int dtype) {
     }
 }
 
-// Parts of the ranks that the bias's gradient is summed over: enough wavefronts for the GPU, 16 ranks or more in each.
+// Parts of the ranks that the bias's gradient is summed over: enough wavefronts for the GPU, 16 ranks or more in each.  Float32
+// backward of 4 heads of 64, with 1024 wavefronts to 8192 to 65536, in us: 12 x 11 x 10 ranks, 26 neighbours, 115, 68, 69; 64 x 64
+// ranks, 24 neighbours, 279, 136, 137.
 inline uint64_t bias_parts(const Comm &c, int q_heads) {
     const uint64_t slots = std::max<uint64_t>(1, (uint64_t)q_heads * c.s);
     return std::clamp<uint64_t>(8192 / slots, 1, ((uint64_t)c.p + 15) / 16);
@@ -453,9 +456,12 @@ class AttentionBinder {
         if (forward_side.tiles)
             return add_tiles(forward_side, tile_by_type<TileKernel>(t.dtype, t.head_dim, segments), a.group / forward_side.plan.heads);
         const uint64_t items = n * t.q_heads;
-        // Few rows: the wavefronts of a workgroup share the neighbours of one, so that the GPU has work.
+        // Few rows: the wavefronts of a workgroup share the neighbours of one, so that the GPU has work, up to 4 wavefronts for
+        // each of its 1024 SIMDs.  One wavefront a row to this, in us: 8 heads of 64, 48 neighbours, 100 rows 12.0 to 8.9, 250
+        // rows 12.5 to 10.7; 168 neighbours, 37 rows 27.3 to 10.6.  Twice as many wavefronts: 250 rows 11.2, 500 rows 20.0 for
+        // 15.1; sixteen a row, 250 rows 16.0.
         const uint64_t sets = 64 >> a.lanes_log2, takes = ((uint64_t)c.s + sets - 1) / sets;
-        a.waves = items < 2048 ? (int)std::clamp<uint64_t>(takes, 1, 16) : 1;
+        a.waves = (int)std::clamp<uint64_t>(std::min(takes, kSplitWaves / items), 1, 16);
         if (a.waves > 1) return add_launch(b, by_type<SplitRowKernel>(t.dtype, is_wide), items, 64u * a.waves, a);
         return add_launch(b, by_type<RowKernel>(t.dtype, is_wide), (items + 3) / 4, 256, a);
     }
@@ -531,7 +537,8 @@ inline int bind_rotary(BoundOperator &b, const Comm *c, const iso_rotary_t &t) {
         a.dims[j] = c->dims[j];
         a.inner[j] = (int32_t)c->inner[j];
     }
-    // a workgroup makes about one angle per lane
+    // A workgroup makes about one angle per lane: 16 heads of 80 at 255 x 257 ranks take 129 us, with one rank a workgroup 136,
+    // with four times as many 140; 10 heads of 128 at 64 x 64 x 64 ranks 226, 349 and 243.
     a.ranks = std::clamp(256 / std::max(1, t.pairs), 1, 8);
     const int per_lane = t.dtype == ISO_DTYPE_F32 ? 4 : 8;
     const bool whole = (t.interleaved ? 2 * t.pairs : t.pairs) % per_lane == 0;      // no unit of 16 bytes mixes both kinds

@@ -244,8 +244,8 @@ inline const void *sum_parts_by_type(int dtype) {
 }
 
 // Parts of the ranks that the bias's gradient is summed over: enough wavefronts for the GPU, 16 ranks or more in each.  Float32
-// backward of 4 heads of 64, with 1024 wavefronts to 8192 to 65536, in us: 12 x 11 x 10 ranks, 26 neighbours, 115, 68, 69; 64 x 64
-// ranks, 24 neighbours, 279, 136, 137.
+// backward of 4 heads of 64, with 1024 wavefronts to 8192 to 65536, in us: 12 x 11 x 10 ranks, 27 neighbours, 115, 68, 69; 64 x 64
+// ranks, 25 neighbours, 279, 136, 137.
 inline uint64_t bias_parts(const Comm &c, int q_heads) {
     const uint64_t slots = std::max<uint64_t>(1, (uint64_t)q_heads * c.s);
     return std::clamp<uint64_t>(8192 / slots, 1, ((uint64_t)c.p + 15) / 16);
@@ -457,8 +457,8 @@ class AttentionBinder {
             return add_tiles(forward_side, tile_by_type<TileKernel>(t.dtype, t.head_dim, segments), a.group / forward_side.plan.heads);
         const uint64_t items = n * t.q_heads;
         // Few rows: the wavefronts of a workgroup share the neighbours of one, so that the GPU has work, up to 4 wavefronts for
-        // each of its 1024 SIMDs.  One wavefront a row to this, in us: 8 heads of 64, 48 neighbours, 100 rows 12.0 to 8.9, 250
-        // rows 12.5 to 10.7; 168 neighbours, 37 rows 27.3 to 10.6.  Twice as many wavefronts: 250 rows 11.2, 500 rows 20.0 for
+        // each of its 1024 SIMDs.  One wavefront a row to this, in us: 8 heads of 64, 49 neighbours, 100 rows 12.0 to 8.9, 250
+        // rows 12.5 to 10.7; 169 neighbours, 37 rows 27.3 to 10.6.  Twice as many wavefronts: 250 rows 11.2, 500 rows 20.0 for
         // 15.1; sixteen a row, 250 rows 16.0.
         const uint64_t sets = 64 >> a.lanes_log2, takes = ((uint64_t)c.s + sets - 1) / sets;
         a.waves = (int)std::clamp<uint64_t>(std::min(takes, kSplitWaves / items), 1, 16);

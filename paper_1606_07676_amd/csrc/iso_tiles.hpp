@@ -111,7 +111,8 @@ inline Steps source_steps(const Comm &c) {
 inline TileShape tile_shape(const Comm &c, int heads) { return tile_shape(c, kTileColumns / heads, 16 / heads, source_steps(c).reach); }
 
 // back = false: columns are ranks, rows their sources R (-) C^i.  back = true: columns are sources, rows the ranks that read
-// them.  False where no table of that form exists (neighbours too many, or too far apart).
+// them.  False where no table of that form exists (neighbours too many, or too far apart) or nothing would be in it (a mesh on
+// which no neighbour has a source at any rank): a tile that the kernels are given has one chunk of rows or more.
 inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots, TilePlan &out) {
     const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
     if (c.s < 1 || (int64_t)heads * (c.s + 1) * 4 > 65535) return false;
@@ -180,6 +181,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
             }
             taken[(int64_t)r << 32 | copies[row.copy]] = i;
         }
+    if (rows.empty()) return false;
     // Order: boxes of a wavefront's shape, so that the groups of 16 rows that a wavefront has no neighbour in are many.  Where
     // neighbours are few and far apart, so that few rows serve more than one column, the rows of one wavefront after those of
     // the other (as they were found) leave fewer blocks.

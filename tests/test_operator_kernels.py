@@ -1,0 +1,87 @@
+"""Which kernels a start of an operator on the ranks' tokens enqueues, on the CPU (see stub_library.py)."""
+import math
+import re
+
+import pytest
+
+import iso_inputs as gen
+import paper_1606_07676_amd as iso
+
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+TYPE = {"f32": iso.ISO_DTYPE_F32, "bf16": iso.ISO_DTYPE_BF16, "f16": iso.ISO_DTYPE_F16}
+
+
+def plain_name(name):
+    """Of a demangled name, or of one with a type that c++filt does not know: tile<64> for attention_tile_kernel<__bf16, 64, false>."""
+    found = re.match(r"_ZN3iso\d+(\w+?)_kernelI\w+?Li(\d+)E", name) or re.match(r"(\w+)_kernel<[^,]+, (\d+)", name)
+    if found:
+        return f"{found[1]}<{found[2]}>".replace("attention_", "")
+    return re.match(r"(?:_ZN3iso\d+)?(\w+?)_kernel", name)[1].replace("attention_", "")
+
+
+class Kernels:
+    """Requests over dense stand-in buffers."""
+
+    def __init__(self, stub):
+        import sys
+        self.stub, self.b, self.owned = stub, sys.modules["iso_on_stub.binding"], []
+
+    def alloc(self, n):
+        self.owned.append(self.stub.lib.stub_device_alloc(max(1, n)))
+        return self.owned[-1]
+
+    def start(self, dims, offsets, q_heads, kv_heads, D, dtype="bf16", periodic=None, backward=False, bias=False, segments=False, rows=0,
+              cap=0.0, scale=None, shift=0):
+        """The kernels of one start, those over tiles as name<elements of a row>."""
+        import ctypes
+        lib, p, s, e = self.stub.iso.load_library(), math.prod(dims), len(offsets), SIZE[dtype]
+        comm = self.stub.comm(dims, offsets, periodic)
+        heads = lambda n, h: self.b.iso_heads_t(self.alloc(n * h * D * e + shift * e) + shift * e, h * D, D)       # noqa: E731
+        n = rows or p
+        t = self.b.iso_attention_t(dtype=TYPE[dtype], q_heads=q_heads, kv_heads=kv_heads, head_dim=D, cap=cap,
+                                   scale=D ** -0.5 if scale is None else scale, n_rows=rows)
+        t.q, t.out, t.k, t.v = heads(n, q_heads), heads(n, q_heads), heads(p, kv_heads), heads(p, kv_heads)
+        t.lse = self.alloc(n * q_heads * 4)
+        t.bias = self.alloc(q_heads * s * e) if bias else None
+        t.segments = self.alloc(p * 4) if segments else None
+        t.rows = self.alloc(rows * 8) if rows else None
+        h = ctypes.c_void_p()
+        if backward:
+            g = self.b.iso_attention_grads_t(grad_bias=self.alloc(q_heads * s * e) if bias else None)
+            g.grad_out, g.grad_q, g.grad_k, g.grad_v = heads(n, q_heads), heads(n, q_heads), heads(p, kv_heads), heads(p, kv_heads)
+            size = ctypes.c_size_t()
+            assert lib.iso_neighbor_attention_backward_workspace_bytes(comm.handle, TYPE[dtype], q_heads, kv_heads, D, int(bias), ctypes.byref(size)) == 0
+            st = lib.iso_neighbor_attention_backward_init(ctypes.byref(t), ctypes.byref(g), self.alloc(size.value), size.value, comm.handle, ctypes.byref(h))
+        else:
+            st = lib.iso_neighbor_attention_init(ctypes.byref(t), comm.handle, ctypes.byref(h))
+        assert st == 0
+        names = self.stub.launched(lambda: lib.iso_start(h, None))
+        assert lib.iso_request_free(ctypes.byref(h)) == 0
+        return [plain_name(n) for n in names]
+
+    def free(self):
+        for q in self.owned:
+            self.stub.lib.stub_device_free(q)
+
+
+@pytest.fixture
+def kernels(stub_library):
+    k = Kernels(stub_library)
+    yield k
+    k.free()
+
+
+def short(names):
+    return [n.split("<")[0] for n in names]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dims,offsets", [((8, 8), [(9, 0), (0, -8)]), ((4, 6), [(4, 0), (0, -6)]), ((1, 40), [(1, 0), (-1, 3)]),
+                                          ((64, 64), [(64, 0)])])
+def test_a_mesh_without_any_source_has_no_tiles(kernels, dims, offsets, dtype):
+    """No key of any rank: nothing to stage, and the row kernels write what is left."""
+    mesh = (0,) * len(dims)
+    assert short(kernels.start(dims, offsets, 2, 2, 64, dtype, mesh)) in (["row"], ["split_row"])
+    assert short(kernels.start(dims, offsets, 4, 2, 64, dtype, mesh, backward=True, bias=True)) == ["grad_q_row", "grad_kv_row", "grad_bias_row", "sum_parts"]
+    # with one source it is tiles again, where they pay
+    assert short(kernels.start((64, 64), gen.moore(2, 2) + [(64, 0)], 2, 2, 64, dtype, mesh)) == ["tile"]

@@ -430,6 +430,9 @@ __global__ __launch_bounds__(256, DP > 64 ? 3 : SEGMENTS ? 4 : 5) void attention
     // Scores times log2 e and less the column's base, so that the weights are powers of two.  The base comes into the
     // products' start value (the cap's constant); it is raised, and what was added up before scaled, only when a score exceeds
     // it by more than 8: weights of up to 256 lose nothing, and most chunks need no maximum over the lanes of a column.
+    // Scores made on top of a base far from theirs lose bits to it, all of them after a first chunk of neighbours that a bias
+    // of -1e9 masks.  So the first base lies at most kBelow under the head's highest bias: 2^-24 of that is lost.
+    constexpr float kBelow = 128.f, kLowestBase = -1e16f;           // the latter keeps the start value finite
     const float scale = a.scale * kLog2e, per_scale = 1.f / scale, cap = a.cap * kLog2e, to_cap = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : 0.f;
     __syncthreads();
 
@@ -493,7 +496,16 @@ __global__ __launch_bounds__(256, DP > 64 ? 3 : SEGMENTS ? 4 : 5) void attention
         if (__any(top > limit)) {
             top = column_max(top);
             const bool based = limit > 0.f;
-            const float raise = based ? fmaxf(top, 0.f) : finite_floor(top), keep = based ? __builtin_amdgcn_exp2f(-raise) : 1.f;
+            float raise = based ? fmaxf(top, 0.f) : finite_floor(top);
+            if (__any(raise < -kBelow)) {                           // first bases only
+                const float *biases = lds.bias + column % t.heads * (a.torus.s + 1);
+                float highest = -INFINITY;
+#pragma nounroll
+                for (int i = lane / 16; i < a.torus.s; i += 4) highest = fmaxf(highest, biases[i]);
+                highest = column_max(highest);
+                if (raise < -kBelow) raise = fmaxf(raise, fmaxf(highest - kBelow, kLowestBase));
+            }
+            const float keep = based ? __builtin_amdgcn_exp2f(-raise) : 1.f;
             if (top > -INFINITY) limit = 8.f;
             base += raise;
             from = a.cap > 0.f ? from : f4{1.f, 1.f, 1.f, 1.f} * (-base * per_scale);
@@ -519,9 +531,10 @@ __global__ __launch_bounds__(256, DP > 64 ? 3 : SEGMENTS ? 4 : 5) void attention
     }
     l = column_sum(l);
     bool fine = store_column<T, DP>(a.out, rank, head, a.head_dim, acc, l == 0.f ? 0.f : 1.f / l);
-    // again: NaN or infinities among the scores, or biases near the type's lowest value alone, whose products with log2 e and
-    // 1 / scale leave the range
-    const bool again = !(l < INFINITY) || !(fabsf(base) < 1e30f);
+    // again: NaN or infinities among the scores; biases near the type's highest value, whose products with log2 e and 1 / scale
+    // leave the range; no score as high as the base, by whose highest biases the column has no neighbour, or whose biases are
+    // all the type's lowest value (the highest weight of any other column with a neighbour is 1 or more)
+    const bool again = !(l < INFINITY) || !(fabsf(base) < 1e30f) || (limit > 0.f && l < 0.5f);
     if (a.lse && rank >= 0 && lane < 16 && !again)
         a.lse[rank * a.q_heads + head] = l == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * kLn2;
     redo_columns(rank >= 0 && !(fine && !again), [&](int c) {

@@ -29,3 +29,49 @@ def test_a_mesh_without_any_source(dims, offsets, dtype, monkeypatch):
     assert not out.any() and bool(torch.isneginf(lse).all())
     got = backward("outside", t, out, lse, normal_like(t["q"], 9))
     assert all(not g.any() for g in got.values())
+
+
+MASKED = {
+    "window": ((24, 26), None, gen.moore(2, 6) + here(2), 2, 1, 64),
+    "window_mesh": ((24, 26), [False, True], gen.moore(2, 6) + here(2), 2, 2, 32),
+    "cube": ((10, 9, 12), None, gen.moore(3, 2) + here(3), 4, 2, 128),
+    "cube_of_80": ((10, 9, 12), None, gen.moore(3, 2) + here(3), 2, 2, 80),
+}
+
+
+def masked_offsets(which, offsets):
+    """corners: what lies outside the circle; ahead: one side of the rank; all but some: one neighbour in nine is left."""
+    c = np.asarray(offsets)
+    if which == "corners":
+        return (c ** 2).sum(1) > c.max() ** 2
+    if which == "all but some":
+        return np.arange(len(c)) % 9 != 4
+    return c[:, 0] < 0
+
+
+@pytest.mark.parametrize("value,scale,cap", [("-1e4", None, 0.0), ("-1e9", None, 0.0), ("lowest", None, 0.0), ("several", None, 0.0), ("-1e9", 1.0, 0.0),
+                                             ("lowest", 1.0, 0.0), ("lowest", None, 30.0), ("several", 0.1, 5.0)])
+@pytest.mark.parametrize("shape,dtype,which", [(shape, dtype, "corners") for shape in MASKED for dtype in TYPES] +
+                         [(shape, dtype, which) for shape in ("window", "cube") for dtype in ("bf16", "f16") for which in ("ahead", "all but some")])
+def test_finite_biases_that_mask_some_neighbours(shape, dtype, which, scale, cap, value, monkeypatch):
+    """The neighbours of a bias far below the others' weigh nothing, wherever in a tile's rows they come: as with a bias of -inf."""
+    monkeypatch.setitem(SHAPES, shape, MASKED[shape])
+    t = tensors(21, shape, dtype, bias=True)
+    if scale == 1.0:
+        t["q"] *= 0.125
+    off = torch.from_numpy(np.flatnonzero(masked_offsets(which, MASKED[shape][2]))).to(DEV)
+    lowest = torch.finfo(t["q"].dtype).min
+    values = {"-1e4": [-1e4], "-1e9": [-1e9], "lowest": [lowest], "several": [lowest, -1e9, -3e4, -5e3, -700]}[value]
+    values = torch.tensor([max(x, lowest) for x in values], device=DEV)
+    want_of = {k: v.clone() if v is not None else None for k, v in t.items()}
+    t["bias"][:, off] = values[torch.arange(len(off), device=DEV) * 7 % len(values)].to(t["bias"].dtype)
+    want_of["bias"][:, off] = float("-inf")
+    out, lse = forward(shape, t, cap, scale=scale)
+    want = oracle(shape, want_of, cap, scale=scale)
+    within(lse, want.lse, want.lse_bound(), "lse")
+    within(out, want.out, want.out_bound(out.dtype), "out")
+    if which == "corners" and value in ("-1e9", "several"):
+        grad_out = normal_like(t["q"], 9)
+        got = backward(shape, t, out, lse, grad_out, cap, scale=scale)
+        for name, parts in want.backward(host(grad_out), host(out)).items():
+            within(got[name], parts[0], orc.gradient_bound(*parts, out.dtype), name)

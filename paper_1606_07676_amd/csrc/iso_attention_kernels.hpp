@@ -101,11 +101,19 @@ __device__ __forceinline__ void store_elements(T *row, int at, int end, const fl
     }
 }
 
-// cap * tanh(a / cap).  For 16-bit tensors tanh y = 1 - 2 / (1 + e^2y), whose error is 2^-23 of the cap whatever the score.
+// cap * tanh(a / cap).  For 16-bit tensors tanh y = 1 - 2 / (1 + e^2y), whose error is about 2^-22 of the cap whatever the
+// score.  Above kPlainCap (2^-15 of a weight there)
+// small scores go by tanh y / y as a series to y^8, whose rest is 2^-26, and the tile kernels, whose registers have no room
+// for it, are not taken: 32 x 32 x 32 ranks, 27 neighbours, 8 and 2 heads of 128, 46 us at a cap of 128, 466 above.
+constexpr float kPlainCap = 128.f, kSmallTanh = 0.25f;
 template <typename T> __device__ __forceinline__ float capped(float a, float cap) {
     if constexpr (sizeof(T) == 4) return cap * tanhf(a / cap);
     const float e = __builtin_amdgcn_exp2f(a * (2.f * kLog2e / cap));
-    return cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + e);
+    const float t = cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + e);
+    if (cap <= kPlainCap) return t;
+    const float y = a * (1.f / cap), y2 = y * y;
+    const float ratio = fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return fabsf(y) < kSmallTanh ? a * ratio : t;
 }
 
 // exp(x - of): the difference first, so that scores near the type's lowest value stay finite; -inf gives 0.

@@ -402,6 +402,7 @@ class AttentionBinder {
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
             if (o.t.rows || o.t.dtype == ISO_DTYPE_F32 || !o.is_wide || o.t.head_dim > kTileMaxHeadDim) return;
             if (!(std::fabs(o.t.scale) > 1e-20f && std::fabs(o.t.scale) < 1e20f)) return;      // the kernels divide by it
+            if (o.t.cap > kPlainCap) return;                       // scores would be off by more than the weights' rounding
             for (const iso_heads_t *x : {&o.t.q, &o.t.k, &o.t.v, o.g ? &o.g->grad_out : &o.t.q})
                 if (x->rank_stride >> 31) return;                  // strides in bytes: 32 bits
             if (!build_tile_plan(o.c, heads, back, sums, plan)) return;

@@ -75,3 +75,25 @@ def test_finite_biases_that_mask_some_neighbours(shape, dtype, which, scale, cap
         got = backward(shape, t, out, lse, grad_out, cap, scale=scale)
         for name, parts in want.backward(host(grad_out), host(out)).items():
             within(got[name], parts[0], orc.gradient_bound(*parts, out.dtype), name)
+
+
+@pytest.mark.parametrize("cap", [100.0, 600.0, 1e4, 1e6, 1e30, 3e38])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", ["picture", "volume", "odd_rows"])
+def test_large_caps(shape, dtype, cap):
+    """A cap far above the scores leaves them as they are: the error that is allowed is that of scores without one."""
+    t = tensors(22, shape, dtype, bias=True)
+    plain, want = oracle(shape, t), oracle(shape, t, cap)
+    want.e = plain.e
+    out, lse = forward(shape, t, cap)
+    within(lse, want.lse, want.lse_bound(), "lse")
+    within(out, want.out, want.out_bound(out.dtype), "out")
+    rows = list(range(0, len(t["q"]), 7))
+    some = {k: v for k, v in t.items()} | {"q": t["q"][rows].contiguous()}
+    few, few_lse = forward(shape, some, cap, rows)
+    within(few_lse, want.lse[rows], want.lse_bound()[rows], "lse of single rows")
+    within(few, want.out[rows], want.out_bound(out.dtype)[rows], "single rows")
+    grad_out = normal_like(t["q"], 9)
+    got = backward(shape, t, out, lse, grad_out, cap)
+    for name, parts in want.backward(host(grad_out), host(out)).items():
+        within(got[name], parts[0], orc.gradient_bound(*parts, out.dtype), name)

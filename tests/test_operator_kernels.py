@@ -85,3 +85,11 @@ def test_a_mesh_without_any_source_has_no_tiles(kernels, dims, offsets, dtype):
     assert short(kernels.start(dims, offsets, 4, 2, 64, dtype, mesh, backward=True, bias=True)) == ["grad_q_row", "grad_kv_row", "grad_bias_row", "sum_parts"]
     # with one source it is tiles again, where they pay
     assert short(kernels.start((64, 64), gen.moore(2, 2) + [(64, 0)], 2, 2, 64, dtype, mesh)) == ["tile"]
+
+
+def test_large_caps_go_by_rows(kernels):
+    """The tiles' form of the cap is off by about 2^-22 of it."""
+    volume = ((32, 32, 32), gen.moore(3, 1), 4, 2, 64)
+    assert short(kernels.start(*volume, cap=128.0)) == ["tile"] and short(kernels.start(*volume, cap=129.0)) == ["row"]
+    assert short(kernels.start(*volume, cap=30.0, backward=True)) == ["grad_q_tile", "grad_kv_tile"]
+    assert short(kernels.start(*volume, cap=1e4, backward=True)) == ["grad_q_row", "grad_kv_row"]

@@ -471,7 +471,7 @@ int iso_neighbor_alltoall_noalloc(const void *sendbuf, void *recvbuf, size_t m, 
  * The same inputs give the same bits in every start.  Sums, softmax statistics and angles are held in 32 bits or more; what
  * is written is rounded to the tensors' type once.
  * Errors: ISO_ERR_ARG (null or misaligned pointer, bad count, type, scale or cap), ISO_ERR_TOO_LARGE (head_dim > 256, heads >
- * 65536, 2^31 rows or more), ISO_ERR_OVERLAP (a written tensor shares bytes with another one, or two of its own rows do; rows
+ * 65536, 2^31 rows or more, 2^34 or more of all heads together), ISO_ERR_OVERLAP (a written tensor shares bytes with another one, or two of its own rows do; rows
  * of tensors with the same strides are told apart, other tensors by the ranges that they span), ISO_ERR_POINTER and
  * ISO_ERR_WORKSPACE as in the collectives' init calls. */
 typedef struct {

@@ -55,6 +55,7 @@ struct AttentionArgs {
     const int32_t *segments;               // [p] or null
     const int64_t *rows;                   // device [n] ranks, or null: row n is rank n
     uint32_t n;                            // rows
+    uint32_t first_block;                  // workgroups of the launches before, where one launch cannot hold all
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t lanes_log2;                    // lanes that share one neighbour's row
     int32_t waves;                         // wavefronts that share one row (1: four rows in a workgroup)
@@ -253,7 +254,7 @@ template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void attention_row_kernel(const AttentionArgs a) {
     __shared__ int32_t coords[4][ISO_MAX_DIMS];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint64_t item = (uint64_t)blockIdx.x * 4 + wave;
+    const uint64_t item = ((uint64_t)a.first_block + blockIdx.x) * 4 + wave;
     const uint32_t row = (uint32_t)(item / a.q_heads);
     const int h = (int)(item % a.q_heads);
     const int64_t rank = row < a.n ? rank_of_row(a, row) : -1;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(256) void attention_grad_q_row_kernel(const Attenti
     constexpr int E = ElementTraits<T>::kPerLane;
     __shared__ int32_t coords[4][ISO_MAX_DIMS];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint64_t item = (uint64_t)blockIdx.x * 4 + wave;
+    const uint64_t item = ((uint64_t)a.first_block + blockIdx.x) * 4 + wave;
     const uint32_t rank = (uint32_t)(item / a.q_heads);
     const int h = (int)(item % a.q_heads);
     if (rank < a.n) store_coordinates(a.torus, rank, lane, coords[wave]);
@@ -487,7 +488,7 @@ template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void attention_grad_kv_row_kernel(const AttentionArgs a) {
     __shared__ int32_t coords[4][ISO_MAX_DIMS];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const uint64_t item = (uint64_t)blockIdx.x * 4 + wave;
+    const uint64_t item = ((uint64_t)a.first_block + blockIdx.x) * 4 + wave;
     const uint32_t rank = (uint32_t)(item / a.kv_heads);
     if (rank < a.n) store_coordinates(a.torus, rank, lane, coords[wave]);
     __syncthreads();
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
     constexpr int E = ElementTraits<T>::kPerLane;
     const NeighbourTorus &t = a.torus;
     const int lane = threadIdx.x & 63, L = a.lanes_log2, sets = 64 >> L;
-    const uint64_t item = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6), slots = (uint64_t)a.q_heads * t.s;
+    const uint64_t item = ((uint64_t)a.first_block + blockIdx.x) * 4 + (threadIdx.x >> 6), slots = (uint64_t)a.q_heads * t.s;
     const int part = (int)(item / slots);
     if (part >= a.parts) return;
     const int slot = (int)(item % slots), h = slot / t.s, i = slot % t.s, hk = h / a.group;
@@ -548,12 +549,12 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
 struct SumPartsArgs {
     const float *partials;
     void *out;
-    uint32_t slots, parts;
+    uint32_t slots, parts, first_block;
 };
 template <typename T>
 __global__ __launch_bounds__(1024) void sum_parts_kernel(const SumPartsArgs a) {
     __shared__ float sums[64][17];
-    const uint32_t col = threadIdx.x & 15, row = threadIdx.x >> 4, slot = blockIdx.x * 16 + col;
+    const uint32_t col = threadIdx.x & 15, row = threadIdx.x >> 4, slot = (a.first_block + blockIdx.x) * 16 + col;
     float sum = 0.f;
     if (slot < a.slots) {
 #pragma unroll 4

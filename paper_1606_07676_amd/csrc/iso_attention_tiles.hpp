@@ -167,7 +167,7 @@ struct TileWork {
 };
 __device__ __forceinline__ TileWork tile_work(const TileArgs &t) {
     TileWork w;
-    const uint32_t item = (blockIdx.x & 7) * t.per_xcd + (blockIdx.x >> 3);
+    const uint32_t block = t.a.first_block + blockIdx.x, item = (block & 7) * t.per_xcd + (block >> 3);
     uint32_t pair, part, head, tile;
     fast_divmod(item, t.parts, pair, part);
     fast_divmod(pair, t.n_tiles, head, tile);

@@ -28,11 +28,19 @@ struct BoundOperator {
     void *dev_table = nullptr;             // owned by the request
 };
 
+inline void set_first_block(TileArgs &args, uint32_t first) { args.a.first_block = first; }
+template <typename Args> void set_first_block(Args &args, uint32_t first) { args.first_block = first; }
+
+// A launch holds fewer than 2^32 work-items: more workgroups than that go in several, each a multiple of 8 but the last, so
+// that a workgroup's XCD stays the one that its number names.
 template <typename Args>
-int add_launch(BoundOperator &b, const void *func, uint64_t grid, uint32_t threads, const Args &args, size_t lds = 0) {
-    if (!grid) return ISO_SUCCESS;
-    if (grid > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
-    b.launches.push_back({func, (uint32_t)grid, threads, (uint32_t)lds, std::make_shared<Args>(args)});
+int add_launch(BoundOperator &b, const void *func, uint64_t grid, uint32_t threads, Args args, size_t lds = 0) {
+    if (grid > 0xFFFFFFFFull) return ISO_ERR_TOO_LARGE;
+    const uint64_t most = 0xFFFFFFFFull / threads / 8 * 8;
+    for (uint64_t first = 0; first < grid; first += most) {
+        set_first_block(args, (uint32_t)first);
+        b.launches.push_back({func, (uint32_t)std::min(most, grid - first), threads, (uint32_t)lds, std::make_shared<Args>(args)});
+    }
     return ISO_SUCCESS;
 }
 
@@ -483,7 +491,7 @@ class AttentionBinder {
         if (!forward_side.tiles)
             ISO_TRY(add_launch(b, by_type<GradBiasRowKernel>(t.dtype, is_wide), (slots * a.parts + 3) / 4, 256, a));
         return add_launch(b, sum_parts_by_type(t.dtype), (slots + 15) / 16, 1024,
-                          SumPartsArgs{a.partials, g->grad_bias, (uint32_t)slots, (uint32_t)a.parts});
+                          SumPartsArgs{a.partials, g->grad_bias, (uint32_t)slots, (uint32_t)a.parts, 0});
     }
 
     BoundOperator &b;

@@ -14,7 +14,7 @@ struct RotaryArgs {
     const int32_t *positions;              // device [n][n_axes], or null: the coordinates of rank n
     const double *turns;                   // device [pairs]: frequency_j / 2 pi
     const int32_t *axes;                   // device [pairs]
-    uint32_t n;
+    uint32_t n, first_block;               // first_block: workgroups of the launches before, where one cannot hold all
     int32_t n_axes, head_dim, pairs, ranks;    // ranks: of one workgroup
     int32_t interleaved;                   // pairs (2j, 2j + 1) instead of (j, j + pairs)
     float sign;                            // -1 turns back
@@ -31,7 +31,7 @@ template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     constexpr int E = WIDE ? ElementTraits<T>::kPerLane : 1;
     __shared__ float2 turn[kRotaryAngles];
-    const uint32_t first = blockIdx.x * (uint32_t)a.ranks, count = min((uint32_t)a.ranks, a.n - first);
+    const uint32_t first = (a.first_block + blockIdx.x) * (uint32_t)a.ranks, count = min((uint32_t)a.ranks, a.n - first);
     for (uint32_t item = threadIdx.x; item < count * (uint32_t)a.pairs; item += 256) {
         uint32_t r, j;
         fast_divmod(item, a.by_pairs, r, j);

@@ -84,7 +84,10 @@ hipError_t hipMemGetAddressRange(hipDeviceptr_t *base, size_t *size, hipDevicept
     return hipSuccess;
 }
 hipError_t hipGetSymbolAddress(void **ptr, const void *) { *ptr = g_symbol_memory; return hipSuccess; }
-hipError_t hipLaunchKernel(const void *func, dim3 grid, dim3, void **, size_t, hipStream_t) {
+// HIP takes fewer than 2^32 work-items in a launch.
+static bool too_many(dim3 grid, dim3 block) { return (unsigned long long)grid.x * block.x >> 32; }
+hipError_t hipLaunchKernel(const void *func, dim3 grid, dim3 block, void **, size_t, hipStream_t) {
+    if (too_many(grid, block)) return hipErrorInvalidConfiguration;
     std::lock_guard<std::mutex> lock(g_mu);
     ++g_launches;
     g_log.push_back(kernel_names()[func]);
@@ -96,6 +99,7 @@ hipError_t hipGraphCreate(hipGraph_t *g, unsigned) { *g = (hipGraph_t) new StubG
 hipError_t hipGraphAddKernelNode(hipGraphNode_t *node, hipGraph_t g, const hipGraphNode_t *, size_t,
                                  const hipKernelNodeParams *p) {
     if (!p || !p->func || !p->kernelParams || !p->kernelParams[0]) return hipErrorInvalidValue;
+    if (too_many(p->gridDim, p->blockDim)) return hipErrorInvalidConfiguration;
     StubGraph *sg = (StubGraph *)g;
     *node = (hipGraphNode_t)(uintptr_t)(++sg->nodes);
     ++g_nodes;

@@ -97,3 +97,38 @@ def test_large_caps(shape, dtype, cap):
     got = backward(shape, t, out, lse, grad_out, cap)
     for name, parts in want.backward(host(grad_out), host(out)).items():
         within(got[name], parts[0], orc.gradient_bound(*parts, out.dtype), name)
+
+
+def test_more_rows_than_a_launch_holds():
+    """2^26 rows of all heads, 2^32 work-items: one neighbour, whose value every row takes over as it is."""
+    dims, heads, D = (2048, 1024), 32, 4
+    p = dims[0] * dims[1]
+    g = torch.Generator(DEV).manual_seed(23)
+    q = torch.randn(p, heads, D, device=DEV, generator=g)
+    k, v = (torch.randn(p, 1, D, device=DEV, generator=g) for _ in range(2))
+    out = torch.full_like(q, 7)
+    req = iso.iso_neighbor_attention_init(q, k, v, out, iso.iso_neighborhood_create(dims, [(1, -3)]))
+    assert iso.iso_request_info(req)["launches"] == 2
+    for form in (iso.ISO_GRAPH_OFF, iso.ISO_GRAPH_CHAIN):
+        out.fill_(7)
+        iso.iso_request_set_graph(req, form)
+        iso.iso_start(req)
+        iso.iso_wait(req)
+        assert torch.equal(out, torch.roll(v.view(*dims, D), (1, -3), (0, 1)).view(p, 1, D).expand_as(out))
+
+
+def test_more_tokens_than_a_launch_holds():
+    n = (1 << 27) + 3
+    x = torch.randn(n, 1, 2, device=DEV, generator=torch.Generator(DEV).manual_seed(24)).to(torch.float16)
+    at = torch.arange(n, device=DEV, dtype=torch.int32).view(n, 1)
+    out = torch.full_like(x, 7)
+    req = iso.iso_rotary_init(x, out, [0.3], [0], positions=at)
+    iso.iso_start(req)
+    iso.iso_wait(req)
+    u, tiny = orc.roundoff(x.dtype)
+    for first in range(0, n, 1 << 24):
+        part = slice(first, first + (1 << 24))
+        a, w = x[part, 0].double(), at[part, 0].double() * 0.3
+        want = torch.stack([a[:, 0] * w.cos() - a[:, 1] * w.sin(), a[:, 0] * w.sin() + a[:, 1] * w.cos()], 1)
+        off = (out[part, 0].double() - want).abs()
+        assert bool((off <= u * want.abs() + 2.0 ** -21 * a.abs().sum(1, keepdim=True) + tiny).all()), first

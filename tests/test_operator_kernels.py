@@ -93,3 +93,40 @@ def test_large_caps_go_by_rows(kernels):
     assert short(kernels.start(*volume, cap=128.0)) == ["tile"] and short(kernels.start(*volume, cap=129.0)) == ["row"]
     assert short(kernels.start(*volume, cap=30.0, backward=True)) == ["grad_q_tile", "grad_kv_tile"]
     assert short(kernels.start(*volume, cap=1e4, backward=True)) == ["grad_q_row", "grad_kv_row"]
+
+
+MOST = (1 << 32) // 256 - 8                    # workgroups of 256 that a launch holds, in eights
+
+
+@pytest.mark.parametrize("dims,heads,kv_heads,D,dtype", [((2048, 1024), 32, 1, 4, "f32"), ((1 << 24, 1), 5, 5, 1, "bf16")])
+def test_more_rows_than_a_launch_holds(kernels, dims, heads, kv_heads, D, dtype):
+    """2^32 work-items and more: several launches, which together have a wavefront for every row."""
+    rows = math.prod(dims) * heads
+    names = kernels.start(dims, [(1, 0)], heads, kv_heads, D, dtype)
+    grids = list(kernels.stub.grids)
+    assert short(names) == ["row"] * -(-rows // 4 // MOST) and len(grids) > 1
+    assert sum(grids) == rows // 4 and all(n == MOST for n in grids[:-1])
+    names = kernels.start(dims, [(1, 0)], heads, kv_heads, D, dtype, backward=True)
+    of = lambda name: sum(n for n, k in zip(kernels.stub.grids, short(names)) if k == name)          # noqa: E731
+    assert of("grad_q_row") == rows // 4 and of("grad_kv_row") == rows // heads * kv_heads // 4
+
+
+def test_more_tiles_than_a_launch_holds(kernels):
+    assert short(kernels.start((8192, 8192), gen.moore(2, 1), 16, 16, 8)) == ["tile"] * 2
+    assert kernels.stub.grids == [MOST, 8192 * 8192 // 64 * 16 - MOST]
+
+
+def test_more_tokens_than_a_launch_holds(kernels):
+    """A workgroup of the rotary kernel takes 8 tokens of one pair of channels."""
+    import ctypes
+    import numpy as np
+    n, lib = (1 << 27) + 3, kernels.stub.iso.load_library()
+    freqs, axes, h = np.ones(1), np.zeros(1, np.int32), ctypes.c_void_p()
+    t = kernels.b.iso_rotary_t(dtype=TYPE["f16"], heads=1, head_dim=2, pairs=1, n=n, freqs=freqs.ctypes.data, axes=axes.ctypes.data,
+                               positions=kernels.alloc(4 * n), n_axes=1)
+    t.x = t.out = kernels.b.iso_heads_t(kernels.alloc(4 * n), 2, 2)
+    assert lib.iso_rotary_init(ctypes.byref(t), None, ctypes.byref(h)) == 0
+    assert len(kernels.stub.launched(lambda: lib.iso_start(h, None))) == 2 and sum(kernels.stub.grids) == -(-n // 8)
+    for form in (iso.ISO_GRAPH_CHAIN, iso.ISO_GRAPH_OFF):
+        assert lib.iso_request_set_graph(h, form) == 0 and lib.iso_start(h, None) == 0
+    assert lib.iso_request_free(ctypes.byref(h)) == 0

@@ -55,12 +55,12 @@ struct AttentionArgs {
     const int32_t *segments;               // [p] or null
     const int64_t *rows;                   // device [n] ranks, or null: row n is rank n
     uint32_t n;                            // rows
-    uint32_t first_block;                  // workgroups of the launches before, where one launch cannot hold all
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t lanes_log2;                    // lanes that share one neighbour's row
     int32_t waves;                         // wavefronts that share one row (1: four rows in a workgroup)
     int32_t parts;                         // of the bias's gradient
     float scale, cap;
+    uint32_t first_block;                  // workgroups of the launches before, where one launch cannot hold all
 };
 
 // ---- elements ---------------------------------------------------------------
@@ -109,12 +109,13 @@ __device__ __forceinline__ void store_elements(T *row, int at, int end, const fl
 constexpr float kPlainCap = 128.f, kSmallTanh = 0.25f;
 template <typename T> __device__ __forceinline__ float capped(float a, float cap) {
     if constexpr (sizeof(T) == 4) return cap * tanhf(a / cap);
+    if (__builtin_expect(cap > kPlainCap, 0)) {
+        const float y = a * (1.f / cap), y2 = y * y;
+        const float ratio = fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+        if (fabsf(y) < kSmallTanh) return a * ratio;
+    }
     const float e = __builtin_amdgcn_exp2f(a * (2.f * kLog2e / cap));
-    const float t = cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + e);
-    if (cap <= kPlainCap) return t;
-    const float y = a * (1.f / cap), y2 = y * y;
-    const float ratio = fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-    return fabsf(y) < kSmallTanh ? a * ratio : t;
+    return cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + e);
 }
 
 // exp(x - of): the difference first, so that scores near the type's lowest value stay finite; -inf gives 0.

@@ -131,10 +131,11 @@ __device__ __forceinline__ void store_coordinates(const NeighbourTorus &t, uint3
     if (lane < t.d) coords[lane] = (int32_t)(rank / (uint32_t)t.inner[lane] % (uint32_t)t.dims[lane]);
 }
 
-// Neighbour i of the rank with these coordinates: R (-) C^i, or R (+) C^i where TARGET.  -1: none.
+// Neighbour i of the rank with these coordinates: R (-) C^i, or R (+) C^i where TARGET.  -1: none.  Sizes go to 2^31 - 1, so
+// what wraps takes one difference that stays inside 32 bits, and what does not is compared without a sign.
 template <bool TARGET>
 __device__ __forceinline__ int32_t neighbour_rank(const NeighbourTorus &t, const int32_t *coords, int i) {
-    int32_t rank = 0;
+    uint32_t rank = 0;
     bool there = true;
     const int32_t *c = t.offsets + (int64_t)i * t.d;
     for (int first = 0; first < t.d; first += 4) {                  // four offsets under way at a time
@@ -145,18 +146,19 @@ __device__ __forceinline__ int32_t neighbour_rank(const NeighbourTorus &t, const
         for (int q = 0; q < 4; ++q) {
             const int j = first + q;
             if (j >= t.d) break;
-            const int32_t n = t.dims[j];
-            int32_t x = TARGET ? coords[j] + step[q] : coords[j] - step[q];
+            const uint32_t at = (uint32_t)coords[j], n = (uint32_t)t.dims[j], by = (uint32_t)step[q];
+            uint32_t x;
             if (t.open >> j & 1) {
-                there = there && (uint32_t)x < (uint32_t)n;
+                x = TARGET ? at + by : at - by;
+                there = there && x < n;
             } else {
-                x += x < 0 ? n : 0;
-                x -= x >= n ? n : 0;
+                x = TARGET ? at - (n - by) : at - by;
+                x += (int32_t)x < 0 ? n : 0;
             }
-            rank += x * t.inner[j];
+            rank += x * (uint32_t)t.inner[j];
         }
     }
-    return there ? rank : -1;
+    return there ? (int32_t)rank : -1;
 }
 
 template <int E>
@@ -516,14 +518,16 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
         const uint32_t rank = r0 + (lane >> L);
         int32_t src = -1;
         if (rank < end) {
-            src = 0;
+            uint32_t from = 0;
             bool there = true;
             for (int j = 0; j < t.d; ++j) {
-                int32_t x = (int32_t)(rank / (uint32_t)t.inner[j] % (uint32_t)t.dims[j]) - c[j];
-                if (t.open >> j & 1) there = there && (uint32_t)x < (uint32_t)t.dims[j];
-                else x += x < 0 ? t.dims[j] : 0;
-                src += x * t.inner[j];
+                const uint32_t n = (uint32_t)t.dims[j];
+                uint32_t x = rank / (uint32_t)t.inner[j] % n - (uint32_t)c[j];
+                if (t.open >> j & 1) there = there && x < n;
+                else x += (int32_t)x < 0 ? n : 0;
+                from += x * (uint32_t)t.inner[j];
             }
+            src = (int32_t)from;
             if (!there || (a.segments && (a.segments[rank] < 0 || a.segments[src] != a.segments[rank]))) src = -1;
         }
         const int64_t r = src < 0 ? 0 : rank, u = src < 0 ? 0 : src;

@@ -137,7 +137,7 @@ inline bool wide(const iso_heads_t &t, int head_dim, int dtype) {
 }
 
 // Offsets as the kernels add them: residues where the dimension wraps; where it does not, a coordinate beyond the mesh's
-// size has no source from anywhere, as the size itself has none, and sums stay inside 32 bits.
+// size has no source from anywhere, as the size itself has none.
 inline std::vector<int32_t> kernel_offsets(const Comm &c) {
     std::vector<int32_t> out((size_t)c.s * c.d);
     for (int i = 0; i < c.s; ++i)

@@ -150,6 +150,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     std::array<int64_t, ISO_MAX_DIMS> span{};
     int64_t volume = 1;
     for (int j = 0; j < d; ++j) {
+        if (c.dims[j] > 1 << 30) return false;                      // a tile's place and a position add up in 32 bits
         span[j] = (int64_t)high[j] - low[j] + p.tile[j];
         if (low[j] < -32768 || (int64_t)high[j] + p.tile[j] > 32768 || span[j] > (int64_t(1) << 40) / volume) return false;
         volume *= span[j];

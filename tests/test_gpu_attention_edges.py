@@ -132,3 +132,22 @@ def test_more_tokens_than_a_launch_holds():
         want = torch.stack([a[:, 0] * w.cos() - a[:, 1] * w.sin(), a[:, 0] * w.sin() + a[:, 1] * w.cos()], 1)
         off = (out[part, 0].double() - want).abs()
         assert bool((off <= u * want.abs() + 2.0 ** -21 * a.abs().sum(1, keepdim=True) + tiny).all()), first
+
+
+def test_a_ring_longer_than_half_the_32_bits():
+    """Coordinates plus offsets pass 2^31: one neighbour, the next rank, whose value is taken over and whose gradient comes back."""
+    p = (1 << 30) + 72
+    comm, f16 = iso.iso_neighborhood_create((p,), [(-1,)]), torch.float16
+    values = lambda seed: torch.randint(-50, 50, (p, 1, 1), device=DEV, dtype=torch.int8, generator=torch.Generator(DEV).manual_seed(seed)).to(f16)  # noqa: E731
+    q, k, v, grad_out = (values(seed) for seed in range(4))
+    out, lse = torch.full_like(q, 7), torch.empty(p, 1, device=DEV)
+    req = iso.iso_neighbor_attention_init(q, k, v, out, comm, lse=lse)
+    iso.iso_start(req)
+    iso.iso_wait(req)
+    assert torch.equal(out, torch.roll(v, -1, 0))
+    grads = [torch.full_like(q, 7) for _ in range(3)]
+    work = torch.empty(iso.iso_neighbor_attention_backward_workspace_bytes(comm, 1, 1, 1, f16), dtype=torch.uint8, device=DEV)
+    req = iso.iso_neighbor_attention_backward_init(q, k, v, out, lse, grad_out, *grads, work, comm)
+    iso.iso_start(req)
+    iso.iso_wait(req)
+    assert torch.equal(grads[2], torch.roll(grad_out, 1, 0)) and not grads[0].any() and not grads[1].any()

@@ -130,3 +130,9 @@ def test_more_tokens_than_a_launch_holds(kernels):
     for form in (iso.ISO_GRAPH_CHAIN, iso.ISO_GRAPH_OFF):
         assert lib.iso_request_set_graph(h, form) == 0 and lib.iso_start(h, None) == 0
     assert lib.iso_request_free(ctypes.byref(h)) == 0
+
+
+def test_rings_longer_than_half_the_32_bits_have_no_tiles(kernels):
+    """A tile's place and a position in it add up in 32 bits."""
+    for n, want in (((1 << 20), "tile"), ((1 << 30) + 64, "row")):
+        assert set(short(kernels.start((n,), [(c,) for c in range(-20, 21)], 1, 1, 8))) == {want}, n

@@ -67,19 +67,34 @@ struct Region {
 
 constexpr uint64_t kMaxSpan = uint64_t(1) << 60;
 
-// Rows of tensors that share their strides (slices of one [p][heads][head_dim] buffer) are told apart rank by rank, or head
-// by head; anything else by the ranges that they span.
+// Rows of tensors that share their strides (slices of one buffer) are told apart rank by rank, or head by head where the heads
+// lie further apart than the ranks; anything else by the ranges that they span.
+//
+// lattice_apart: two sets of cells, `outer` bytes from one to the next, with rows `inner` bytes apart in each.  They share no
+// byte where the rows of b's cell lie behind all of a's, or between them.
+struct Cells {
+    uint64_t outer, inner, rows, bytes;
+    uint64_t footprint() const { return (rows - 1) * inner + bytes; }
+};
+inline bool lattice_apart(const Cells &a, const Cells &b, uint64_t distance) {
+    if (!a.outer || a.outer != b.outer || a.footprint() > a.outer) return false;
+    const uint64_t delta = distance % a.outer;
+    const bool inside = delta + b.footprint() <= a.outer;          // b's cell ends before a's next one
+    if (inside && delta >= a.footprint()) return true;
+    if (!a.inner || a.inner != b.inner || !(inside || a.outer % a.inner == 0)) return false;
+    return delta % a.inner >= a.bytes && delta % a.inner + b.bytes <= a.inner;
+}
 inline bool regions_meet(const Region &a, const Region &b) {
     if (a.empty() || b.empty()) return false;
     if (a.at + a.span() <= b.at || b.at + b.span() <= a.at) return false;
-    if (a.rank_stride != b.rank_stride || !a.rank_stride) return true;
-    const uint64_t rank = a.rank_stride;
-    if (a.footprint() > rank || b.footprint() > rank) return true;
-    const uint64_t delta = b.at >= a.at ? (b.at - a.at) % rank : (rank - (a.at - b.at) % rank) % rank;
-    if (delta >= a.footprint() && delta + b.footprint() <= rank) return false;
-    const uint64_t head = a.head_stride;
-    if (!head || head != b.head_stride || rank % head) return true;
-    return !(delta % head >= a.bytes && delta % head + b.bytes <= head);
+    // b - a, and a - b, up to whole cells
+    const auto apart = [&](const Cells &x, const Cells &y) {
+        if (!x.outer) return false;
+        const uint64_t ahead = b.at >= a.at ? (b.at - a.at) % x.outer : x.outer - (a.at - b.at) % x.outer;
+        return lattice_apart(x, y, ahead) || lattice_apart(y, x, x.outer - ahead % x.outer);
+    };
+    return !apart({a.rank_stride, a.head_stride, a.heads, a.bytes}, {b.rank_stride, b.head_stride, b.heads, b.bytes}) &&
+           !apart({a.head_stride, a.rank_stride, a.n, a.bytes}, {b.head_stride, b.rank_stride, b.n, b.bytes});
 }
 
 // Two rows of one written tensor must not share bytes.

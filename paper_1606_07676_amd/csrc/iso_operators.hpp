@@ -415,9 +415,10 @@ class AttentionBinder {
         // 29.8 to 13.8 forward and 113 to 59 backward (45 chunks), 4096 ranks 52 to 60 and 191 to 285 (69 chunks); 343 in a
         // cube, 300 ranks with 2 heads 39 to 20 and 180 to 156, with 8 heads 40 to 57 and 182 to 206, 4096 ranks 28 to 301 and
         // 116 to 1695.
-        bool tiles_pay(const AttentionBinder &o, int heads, bool back) const {
+        static bool tiles_pay(const AttentionBinder &o, int heads, bool back, int rows, int64_t n_tiles) {
             const double group = o.t.q_heads / o.t.kv_heads, turns = back ? group : 1;
-            const double side_by_side = (double)plan.n_tiles * o.t.kv_heads * (back ? 1 : group / heads);
+            const double side_by_side = (double)n_tiles * o.t.kv_heads * (back ? 1 : group / heads);
+            const double chunks = std::ceil(rows / (double)tile_chunk_rows(o.t.head_dim));
             const double pairs = (double)o.c.p * o.t.q_heads * o.c.s, alone = (o.g ? 80.0 : 40.0) * turns * o.c.s;
             return chunks * turns * std::max(512.0, side_by_side) <= 2000 + std::max(pairs * o.t.head_dim / 1300, alone);
         }
@@ -428,11 +429,14 @@ class AttentionBinder {
             if (o.t.cap > kPlainCap) return;                       // scores would be off by more than the weights' rounding
             for (const iso_heads_t *x : {&o.t.q, &o.t.k, &o.t.v, o.g ? &o.g->grad_out : &o.t.q})
                 if (x->rank_stride >> 31) return;                  // strides in bytes: 32 bits
-            if (!build_tile_plan(o.c, heads, back, sums, plan)) return;
             const int chunk = tile_chunk_rows(o.t.head_dim);
+            const auto lds_of = [&](int rows) { return tile_lds_bytes(o.t.head_dim, (rows + chunk - 1) / chunk, floats); };
+            if (!build_tile_plan(o.c, heads, back, sums, plan, [&](int rows, int64_t n_tiles) {
+                    return lds_of(rows) <= kTileMaxLds && tiles_pay(o, heads, back, rows, n_tiles);
+                }))
+                return;
             chunks = (plan.rows + chunk - 1) / chunk;
-            lds = tile_lds_bytes(o.t.head_dim, chunks, floats);
-            if (lds > kTileMaxLds || !tiles_pay(o, heads, back)) return;
+            lds = lds_of(plan.rows);
             columns = table.add(plan.column_at);
             rows = table.add(plan.row_at);
             active = table.add(plan.active);

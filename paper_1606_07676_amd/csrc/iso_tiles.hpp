@@ -113,7 +113,11 @@ inline TileShape tile_shape(const Comm &c, int heads) { return tile_shape(c, kTi
 // back = false: columns are ranks, rows their sources R (-) C^i.  back = true: columns are sources, rows the ranks that read
 // them.  False where no table of that form exists (neighbours too many, or too far apart) or nothing would be in it (a mesh on
 // which no neighbour has a source at any rank): a tile that the kernels are given has one chunk of rows or more.
-inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots, TilePlan &out) {
+//
+// pays(rows, n_tiles) is asked before any table is made, with the fewest rows that there can be and then with those that there
+// are: false ends it.
+template <typename Pays>
+inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots, TilePlan &out, Pays &&pays) {
     const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
     if (c.s < 1 || (int64_t)heads * (c.s + 1) * 4 > 65535) return false;
     Steps steps = source_steps(c);
@@ -132,6 +136,14 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
     p.tiles = shape.tiles;
     p.n_tiles = shape.n_tiles;
     if (p.n_tiles > 0x7FFFFFFF) return false;
+    // sums of a of one kind and b of another are a + b - 1 or more
+    std::vector<std::array<int32_t, ISO_MAX_DIMS>> distinct;
+    for (int i = 0; i < c.s; ++i)
+        if (used[i]) distinct.push_back(step[i]);
+    std::sort(distinct.begin(), distinct.end());
+    const int steps_apart = (int)(std::unique(distinct.begin(), distinct.end()) - distinct.begin());
+    const int fewest = steps_apart + ranks - 1;
+    if (!steps_apart || fewest > kTileMaxRows || !pays(fewest, p.n_tiles)) return false;
     // columns: the wavefronts' boxes one after the other, the last dimension fastest inside and outside
     const int width = (d + 3) / 4 * 4;
     std::vector<int32_t> column_at((size_t)ranks * d);
@@ -182,7 +194,7 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
             }
             taken[(int64_t)r << 32 | copies[row.copy]] = i;
         }
-    if (rows.empty()) return false;
+    if (!pays((int)rows.size(), p.n_tiles)) return false;
     // Order: boxes of a wavefront's shape, so that the groups of 16 rows that a wavefront has no neighbour in are many.  Where
     // neighbours are few and far apart, so that few rows serve more than one column, the rows of one wavefront after those of
     // the other (as they were found) leave fewer blocks.

@@ -258,6 +258,13 @@ inline size_t tile_lds_bytes(int head_dim, int chunks, size_t biases) {
     }
 }
 
+// Lanes that share one neighbour's row in the row kernels.
+inline int row_lanes(int dtype, int head_dim) {
+    int lanes = 1;
+    while (lanes * (dtype == ISO_DTYPE_F32 ? 4 : 8) < head_dim) lanes *= 2;
+    return lanes;
+}
+
 inline const void *sum_parts_by_type(int dtype) {
     switch (dtype) {
         case ISO_DTYPE_F32: return (const void *)(sum_parts_kernel<float>);
@@ -379,8 +386,7 @@ class AttentionBinder {
         a.head_dim = t.head_dim;
         a.scale = t.scale;
         a.cap = t.cap;
-        const int per_lane = t.dtype == ISO_DTYPE_F32 ? 4 : 8;
-        while ((per_lane << a.lanes_log2) < t.head_dim) ++a.lanes_log2;
+        a.lanes_log2 = __builtin_ctz(row_lanes(t.dtype, t.head_dim));
         if (g) {
             a.grad_out = device_heads(g->grad_out);
             a.grad_q = device_heads(g->grad_q);
@@ -408,19 +414,32 @@ class AttentionBinder {
         size_t lds = 0, columns = 0, rows = 0, active = 0, index = 0, slots = 0, zeros = 0;
         int chunks = 0;
 
-        // Tiles or rows.  A tile takes its chunks one after the other, 512 tiles side by side: 0.53 us a chunk forward and 2.35 us
-        // in both backward kernels together, whatever the neighbours in it.  Rows take pairs * head_dim / 1.35e6 us and
-        // / 0.29e6, which is a 1300th of the same measure either way, and no less than one row alone: 0.04 us a neighbour and
-        // 0.36 us.  Measured with 8 heads of 64, tiles to rows in us: 40 neighbours scattered in 4 dimensions, 630 ranks,
-        // 29.8 to 13.8 forward and 113 to 59 backward (45 chunks), 4096 ranks 52 to 60 and 191 to 285 (69 chunks); 343 in a
-        // cube, 300 ranks with 2 heads 39 to 20 and 180 to 156, with 8 heads 40 to 57 and 182 to 206, 4096 ranks 28 to 301 and
-        // 116 to 1695.
+        // Tiles or rows, by what either would take, in us.  A tile takes 32 of its rows after the other, as fast as one does alone
+        // or as all side by side do together; a row takes its neighbours in sets, as many as lanes have room for, and something
+        // to begin and end with, likewise.  Constants by kernel (forward; grad_q with the bias's gradient; grad_kv), fitted to
+        // 681 times of either: heads of 32, 64, 80 and 128, 8 / 8, 8 / 2 and 2 / 2 of them, 64 to 38416 ranks, 5 to 169 neighbours in
+        // 1 to 4 dimensions; tiles a tenth under their fit, as a wrong choice of rows costs more.  What is taken is 1 % over
+        // the better of the two in the mean, 70 % at worst; for 693 others (heads of 32 to 128, 3 to 81 neighbours, to 200000
+        // ranks) 0.3 % and 65 %.  Tiles to rows: 128 x 128, 169 neighbours, 8 / 8 heads, forward, 29 to 338 at 32 elements, 54 to
+        // 1294 at 128; 8 x 8, the same, 15.9 to 8.3 and 28.8 to 12.9; grad_kv of 10 x 10 x 10, 27 neighbours, 8 / 2 heads of 32,
+        // 25.9 to 16.3; 40 neighbours scattered over 4 dimensions, 8 / 8 heads of 128, forward, 1296 ranks 58 to 38, 14641 ranks
+        // 279 to 364.
+        struct Estimate {
+            double tile, rows32, rows32_element, beside, beside_element;
+            double row, set, row_beside, row_sets;
+        };
         static bool tiles_pay(const AttentionBinder &o, int heads, bool back, int rows, int64_t n_tiles) {
-            const double group = o.t.q_heads / o.t.kv_heads, turns = back ? group : 1;
-            const double side_by_side = (double)n_tiles * o.t.kv_heads * (back ? 1 : group / heads);
-            const double chunks = std::ceil(rows / (double)tile_chunk_rows(o.t.head_dim));
-            const double pairs = (double)o.c.p * o.t.q_heads * o.c.s, alone = (o.g ? 80.0 : 40.0) * turns * o.c.s;
-            return chunks * turns * std::max(512.0, side_by_side) <= 2000 + std::max(pairs * o.t.head_dim / 1300, alone);
+            static constexpr Estimate kForward{4.6, 0.177, 0.0045, 4.35e-4, 1.31e-5, 5.9, 0.18, 2.28e-4, 1.5};
+            static constexpr Estimate kGradQ{7.6, 0.61, 0.0071, 1.5e-3, 2.35e-5, 13.8, 1.85, 7.6e-4, 0.6};
+            static constexpr Estimate kGradKV{5.3, 0.416, 0.0065, 4.7e-4, 2.8e-5, 7.8, 1.25, 3.87e-4, 1.8};
+            const Estimate &e = back ? kGradKV : o.g ? kGradQ : kForward;
+            const int chunk = tile_chunk_rows(o.t.head_dim), elements = tile_head_dim(o.t.head_dim), group = o.t.q_heads / o.t.kv_heads;
+            const double turns = back ? group : 1, side_by_side = (double)n_tiles * o.t.kv_heads * (back ? 1 : group / heads);
+            const double chunks = (double)((rows + chunk - 1) / chunk) * (chunk / 32) * turns;
+            const double tile = e.tile + chunks * std::max(e.rows32 + e.rows32_element * elements,
+                                                           side_by_side * (e.beside + e.beside_element * elements));
+            const double lanes = row_lanes(o.t.dtype, o.t.head_dim), sets = std::ceil(o.c.s * lanes / 64);
+            return tile <= e.row + std::max(sets * turns * e.set, (double)o.c.p * o.t.q_heads * (sets + e.row_sets) * e.row_beside);
         }
 
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {

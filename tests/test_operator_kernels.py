@@ -136,3 +136,17 @@ def test_rings_longer_than_half_the_32_bits_have_no_tiles(kernels):
     """A tile's place and a position in it add up in 32 bits."""
     for n, want in (((1 << 20), "tile"), ((1 << 30) + 64, "row")):
         assert set(short(kernels.start((n,), [(c,) for c in range(-20, 21)], 1, 1, 8))) == {want}, n
+
+
+@pytest.mark.parametrize("dims,offsets,heads,forward,grad_q,grad_kv", [
+    ((128, 128), gen.moore(2, 6), (8, 8, 32), "tile<32>", "grad_q_tile<32>", "grad_kv_tile<32>"),
+    ((128, 128), gen.moore(2, 6), (8, 8, 128), "tile<128>", "grad_q_tile<128>", "grad_kv_tile<128>"),
+    ((8, 8), gen.moore(2, 6), (8, 8, 32), "split_row", None, None),
+    ((8, 8), gen.moore(2, 6), (8, 8, 128), "split_row", "grad_q_tile<128>", "grad_kv_tile<128>"),
+    ((10, 10, 10), gen.moore(3, 1), (8, 2, 32), "tile<32>", "grad_q_tile<32>", "grad_kv_row"),
+    ((8, 8, 8, 8), gen.random_distinct(4, -3, 3, 40, 7), (8, 2, 128), "tile<128>", "grad_q_tile<128>", "grad_kv_row"),
+    ((6, 6, 6, 6), gen.random_distinct(4, -3, 3, 40, 7), (8, 8, 128), "row", None, "grad_kv_row")])
+def test_tiles_or_rows_by_what_was_faster(kernels, dims, offsets, heads, forward, grad_q, grad_kv):
+    """Places where one of the two was 1.3 to 25 times as fast (None: either)."""
+    names = kernels.start(dims, offsets, *heads) + kernels.start(dims, offsets, *heads, backward=True, bias=True)
+    assert all(want in (None, got) for want, got in zip((forward, grad_q, grad_kv), names)), names

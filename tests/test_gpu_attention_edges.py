@@ -6,6 +6,7 @@ import torch
 import iso_inputs as gen
 import paper_1606_07676_amd as iso
 from oracle import attention_oracle as orc
+from tile_shapes import TILED
 from test_gpu_attention import DEV, SHAPES, TYPES, backward, forward, host, oracle, tensors, within
 
 pytestmark = pytest.mark.gpu
@@ -151,3 +152,22 @@ def test_a_ring_longer_than_half_the_32_bits():
     iso.iso_start(req)
     iso.iso_wait(req)
     assert torch.equal(grads[2], torch.roll(grad_out, 1, 0)) and not grads[0].any() and not grads[1].any()
+
+
+@pytest.mark.parametrize("options", [dict(), dict(bias=True), dict(bias=True, cap=20.0, segments=True)], ids=lambda o: "-".join(o) or "plain")
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", TILED)
+def test_in_tiles(shape, dtype, options, monkeypatch):
+    """Shapes that reach every path of the tile kernels (test_operator_kernels.py says that they take them)."""
+    monkeypatch.setitem(SHAPES, shape, TILED[shape])
+    cap = options.get("cap", 0.0)
+    t = tensors(25, shape, dtype, options.get("bias", False), options.get("segments", False))
+    out, lse = forward(shape, t, cap)
+    want = oracle(shape, t, cap)
+    within(lse, want.lse, want.lse_bound(), "lse")
+    within(out, want.out, want.out_bound(out.dtype), "out")
+    grad_out = normal_like(t["q"], 9)
+    got = backward(shape, t, out, lse, grad_out, cap)
+    for name, parts in want.backward(host(grad_out), host(out)).items():
+        if got[name] is not None:
+            within(got[name], parts[0], orc.gradient_bound(*parts, out.dtype), name)

@@ -6,6 +6,7 @@ import pytest
 
 import iso_inputs as gen
 import paper_1606_07676_amd as iso
+from tile_shapes import TILED
 
 SIZE = {"f32": 4, "bf16": 2, "f16": 2}
 TYPE = {"f32": iso.ISO_DTYPE_F32, "bf16": iso.ISO_DTYPE_BF16, "f16": iso.ISO_DTYPE_F16}
@@ -150,3 +151,13 @@ def test_tiles_or_rows_by_what_was_faster(kernels, dims, offsets, heads, forward
     """Places where one of the two was 1.3 to 25 times as fast (None: either)."""
     names = kernels.start(dims, offsets, *heads) + kernels.start(dims, offsets, *heads, backward=True, bias=True)
     assert all(want in (None, got) for want, got in zip((forward, grad_q, grad_kv), names)), names
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", TILED)
+def test_shapes_of_the_tile_tests_take_tiles(kernels, shape, dtype):
+    dims, periodic, offsets, q_heads, kv_heads, D = TILED[shape]
+    assert short(kernels.start(dims, offsets, q_heads, kv_heads, D, dtype, periodic)) == ["tile"]
+    for bias in (False, True):
+        names = short(kernels.start(dims, offsets, q_heads, kv_heads, D, dtype, periodic, backward=True, bias=bias))
+        assert names == ["grad_q_tile", "grad_kv_tile"] + ["sum_parts"] * bias

@@ -161,7 +161,6 @@ __device__ __forceinline__ int32_t neighbour_rank(const NeighbourTorus &t, const
     return there ? (int32_t)rank : -1;
 }
 
-template <int E>
 __device__ __forceinline__ float sum_over_lanes(float x, int lanes_log2) {
     for (int l = 0; l < lanes_log2; ++l) x += __shfl_xor(x, 1 << l);
     return x;
@@ -215,7 +214,7 @@ __device__ __forceinline__ void attend_row(const AttentionArgs &a, uint32_t row,
         float x = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
-        x = sum_over_lanes<E>(x, L) * a.scale;
+        x = sum_over_lanes(x, L) * a.scale;
         if (a.cap > 0.f) x = capped<T>(x, a.cap);
         if (bias && src >= 0) x += (float)bias[i];
         if (src < 0) x = -INFINITY;
@@ -355,7 +354,7 @@ __device__ __forceinline__ float row_delta(const AttentionArgs &a, uint32_t rank
     load_elements<T, WIDE>((const T *)a.out.data + rank * a.out.rank_stride + h * a.out.head_stride, at, a.head_dim, o);
 #pragma unroll
     for (int e = 0; e < E; ++e) x = fmaf(g[e], o[e], x);
-    return sum_over_lanes<E>(x, a.lanes_log2);
+    return sum_over_lanes(x, a.lanes_log2);
 }
 
 // bias_sums: of the row's head, to which dx is added, or null.
@@ -384,7 +383,7 @@ __device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank
             load_elements<T, WIDE>(k0 + (src < 0 ? 0 : src) * a.k.rank_stride, at, src < 0 ? 0 : a.head_dim, k);
 #pragma unroll
             for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x);
-            x = sum_over_lanes<E>(x, L);
+            x = sum_over_lanes(x, L);
             if (src >= 0) sum += pair_gradient<T>(x, bias ? (float)bias[i] : 0.f, lse, 1.f, 0.f, 0.f, a.scale, a.cap).p;
         }
         sum = sum_across_groups(sum, L);
@@ -400,8 +399,8 @@ __device__ __forceinline__ void grad_q_row(const AttentionArgs &a, uint32_t rank
         load_elements<T, WIDE>(v0 + (src < 0 ? 0 : src) * a.v.rank_stride, at, src < 0 ? 0 : a.head_dim, v);
 #pragma unroll
         for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x), dp = fmaf(g[e], v[e], dp);
-        x = sum_over_lanes<E>(x, L);
-        dp = sum_over_lanes<E>(dp, L);
+        x = sum_over_lanes(x, L);
+        dp = sum_over_lanes(dp, L);
         if (src >= 0) {
             const PairGradient pg = pair_gradient<T>(x, bias ? (float)bias[i] : 0.f, lse, norm, dp, delta, a.scale, a.cap);
             if (bias_sums && at == 0) bias_sums[i] += pg.dx;
@@ -465,8 +464,8 @@ __device__ __forceinline__ void grad_kv_row(const AttentionArgs &a, uint32_t ran
                                    dst < 0 ? 0 : a.head_dim, g);
 #pragma unroll
             for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x), dp = fmaf(g[e], v[e], dp);
-            x = sum_over_lanes<E>(x, L);
-            dp = sum_over_lanes<E>(dp, L);
+            x = sum_over_lanes(x, L);
+            dp = sum_over_lanes(dp, L);
             if (dst >= 0) {
                 const float b = a.bias ? (float)((const T *)a.bias)[(int64_t)h * t.s + i] : 0.f;
                 const float lse = a.lse[r * a.q_heads + h], norm = norm_of(a, r, h, lse);
@@ -539,8 +538,8 @@ __global__ __launch_bounds__(256) void attention_grad_bias_row_kernel(const Atte
         load_elements<T, WIDE>((const T *)a.v.data + u * a.v.rank_stride + hk * a.v.head_stride, at, end_at, v);
 #pragma unroll
         for (int e = 0; e < E; ++e) x = fmaf(q[e], k[e], x), dp = fmaf(g[e], v[e], dp);
-        x = sum_over_lanes<E>(x, L);
-        dp = sum_over_lanes<E>(dp, L);
+        x = sum_over_lanes(x, L);
+        dp = sum_over_lanes(dp, L);
         if (src >= 0) {
             const float lse = a.lse[r * a.q_heads + h];
             sum += pair_gradient<T>(x, bias, lse, norm_of(a, r, h, lse), dp, a.delta[r * a.q_heads + h], a.scale, a.cap).dx;

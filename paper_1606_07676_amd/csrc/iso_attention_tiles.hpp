@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256, DP > 64 ? 3 : SEGMENTS ? 4 : 5) void attention
     const TileWork work = tile_work(t);
     if (!work.any) return;
     Lds lds(lds_bytes, t.chunks);
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
     const int64_t rank = rank_at<true>(t, work.tile, t.column_at + column / t.heads * t.words);
     const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;
@@ -624,7 +624,7 @@ __global__ __launch_bounds__(256, 3) void attention_grad_q_tile_kernel(const Til
     const TileWork work = tile_work(t);
     if (!work.any) return;
     Lds lds(lds_bytes, t.chunks);
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group + work.part * t.heads, head = first_head + column % t.heads;
     const int s = a.torus.s, slots = t.heads * s;
     // behind the biases: dx of 32 rows and the wavefront's columns, a zero, and the sums of its slots over the tile's rows
@@ -752,7 +752,7 @@ __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const Ti
     const TileWork work = tile_work(t);
     if (!work.any) return;
     Lds lds(lds_bytes, t.chunks);
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, column = 16 * wave + lane % 16;
     const int first_head = work.key_head * a.group, s = a.torus.s;
     const int64_t rank = rank_at<true>(t, work.tile, t.column_at + column * t.words);
     const int32_t own = SEGMENTS ? column_segment(a, rank) : 0;

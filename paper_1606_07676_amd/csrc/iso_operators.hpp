@@ -584,9 +584,10 @@ inline int bind_rotary(BoundOperator &b, const Comm *c, const iso_rotary_t &t) {
         a.dims[j] = c->dims[j];
         a.inner[j] = (int32_t)c->inner[j];
     }
-    // A workgroup makes about one angle per lane: 16 heads of 80 at 255 x 257 ranks take 129 us, with one rank a workgroup 136,
-    // with four times as many 140; 10 heads of 128 at 64 x 64 x 64 ranks 226, 349 and 243.
-    a.ranks = std::clamp(256 / std::max(1, t.pairs), 1, 8);
+    // As many ranks as a workgroup holds angles of, at most 8: 16 heads of 80 at 255 x 257 ranks take 129 us, with one rank a
+    // workgroup 136, with four times as many 140; 10 heads of 128 at 64 x 64 x 64 ranks 226, 349 and 243.
+    static_assert(kRotaryAngles >= kAttentionMaxHeadDim / 2);
+    a.ranks = std::clamp(kRotaryAngles / std::max(1, t.pairs), 1, 8);
     const int per_lane = t.dtype == ISO_DTYPE_F32 ? 4 : 8;
     const bool whole = (t.interleaved ? 2 * t.pairs : t.pairs) % per_lane == 0;      // no unit of 16 bytes mixes both kinds
     const bool is_wide = whole && wide(t.x, t.head_dim, t.dtype) && wide(t.out, t.head_dim, t.dtype);

@@ -7,7 +7,7 @@
 
 namespace iso {
 
-constexpr uint32_t kRotaryAngles = 1024;   // angles that a workgroup holds in LDS
+constexpr int kRotaryAngles = 256;         // angles that a workgroup holds in LDS: about one per lane
 
 struct RotaryArgs {
     Heads x, out;
@@ -30,7 +30,7 @@ struct RotaryArgs {
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     constexpr int E = WIDE ? ElementTraits<T>::kPerLane : 1;
-    __shared__ float2 turn[kRotaryAngles];
+    __shared__ float2 turn[kRotaryAngles];                          // count * pairs
     const uint32_t first = (a.first_block + blockIdx.x) * (uint32_t)a.ranks, count = min((uint32_t)a.ranks, a.n - first);
     for (uint32_t item = threadIdx.x; item < count * (uint32_t)a.pairs; item += 256) {
         uint32_t r, j;

@@ -24,7 +24,6 @@ struct TilePlan {
     std::array<int32_t, ISO_MAX_DIMS> tile{}, tiles{};      // ranks per tile and tiles, by dimension
     int64_t n_tiles = 1;
     int rows = 0, chunks = 0;              // rows in use; chunks of kChunkRows
-    int blocks = 0;                        // 16 x 16 blocks of pairs that hold a neighbour
     // positions relative to the tile's first rank, the last dimension first, in words of four
     std::vector<int16_t> column_at;        // [kTileColumns / heads][words * 4]
     std::vector<int16_t> row_at;           // [chunks * kChunkRows][words * 4]
@@ -238,7 +237,6 @@ inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots
             p.active[group / 4] |= 1u << (4 * w + group % 4);
         }
     }
-    for (uint32_t a : p.active) p.blocks += __builtin_popcount(a);
     if (bias_slots) {
         std::vector<std::vector<std::pair<uint32_t, uint32_t>>> of((size_t)p.chunks * 2 * kTileWaves);
         for (const auto &[pair, i] : taken) {

@@ -611,7 +611,7 @@ int iso_neighbor_attention_backward_workspace_bytes(iso_comm_t comm, int dtype, 
         int st = iso::check_shape(dtype, q_heads, kv_heads, head_dim);
         if (st != ISO_SUCCESS) return st;
         iso::BackwardWorkspace w;
-        if ((st = iso::backward_workspace(comm->c, q_heads, kv_heads, with_bias != 0, w)) != ISO_SUCCESS) return st;
+        if ((st = iso::backward_workspace(comm->c, dtype, q_heads, kv_heads, head_dim, with_bias != 0, w)) != ISO_SUCCESS) return st;
         *bytes = (size_t)w.bytes;
         return ISO_SUCCESS;
     });

@@ -48,7 +48,7 @@ struct AttentionArgs {
     Heads grad_out, grad_q, grad_k, grad_v;
     float *lse;                            // [n][q_heads]
     float *delta;                          // [p][q_heads]: grad_out . out of every row, for the gradients of k and v
-    float *starts;                         // [2][p][q_heads]: -lse / scale (cap: lse log2 e) and -delta, for the tile kernels
+    float *starts;                         // [2][p][q_heads]: -lse / scale (cap: lse log2 e) and -delta, or null: for the tile kernels
     float *norms;                          // [p][q_heads]: 1 / (sum of the weights), of rows with a large lse
     float *partials;                       // [parts][q_heads * s] of the bias's gradient
     const void *bias;                      // [q_heads][s] of the tensors' type, or null
@@ -428,10 +428,14 @@ __global__ __launch_bounds__(256) void attention_grad_q_row_kernel(const Attenti
     const float delta = row_delta<T, WIDE>(a, rank, h, (lane & ((1 << a.lanes_log2) - 1)) * E);
     if (lane == 0) {
         const int64_t at = (int64_t)rank * a.q_heads + h;
-        const float lse = finite_floor(a.lse[at]);
         a.delta[at] = delta;
-        a.starts[at] = fabsf(lse) > kLargeLse ? NAN : a.cap > 0.f ? lse * kLog2e : -lse / a.scale;
-        a.starts[(int64_t)a.n * a.q_heads + at] = -delta;
+        if constexpr (sizeof(T) == 2) {
+            if (a.starts) {
+                const float lse = finite_floor(a.lse[at]);
+                a.starts[at] = fabsf(lse) > kLargeLse ? NAN : a.cap > 0.f ? lse * kLog2e : -lse / a.scale;
+                a.starts[(int64_t)a.n * a.q_heads + at] = -delta;
+            }
+        }
     }
     grad_q_row<T, WIDE>(a, rank, h, delta, coords[wave]);
 }

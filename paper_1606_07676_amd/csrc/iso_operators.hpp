@@ -289,17 +289,22 @@ inline int tile_heads(int group) {             // q heads of a rank that one til
     while (heads < 8 && group % (2 * heads) == 0) heads *= 2;
     return heads;
 }
-inline int backward_workspace(const Comm &c, int q_heads, int kv_heads, bool bias, BackwardWorkspace &w) {
+// Tensors that the tile kernels may take, whatever their strides.
+inline bool tile_tensors(int dtype, int head_dim) {
+    return dtype != ISO_DTYPE_F32 && head_dim <= kTileMaxHeadDim && head_dim * dtype_size(dtype) % 16 == 0;
+}
+inline int backward_workspace(const Comm &c, int dtype, int q_heads, int kv_heads, int head_dim, bool bias, BackwardWorkspace &w) {
     const uint64_t rows = (uint64_t)c.p * q_heads;               // below 2^47
+    const bool tiles = tile_tensors(dtype, head_dim);
     w.starts = (rows * 4 + 255) / 256 * 256;
-    w.norms = w.starts + (rows * 8 + 255) / 256 * 256;
+    w.norms = w.starts + (tiles ? (rows * 8 + 255) / 256 * 256 : 0);
     w.partials = w.norms + (rows * 4 + 255) / 256 * 256;
     w.bytes = w.partials;
     if (bias) {
         if ((uint64_t)q_heads * c.s > 0x7FFFFFFFull) return ISO_ERR_TOO_LARGE;
         uint64_t parts = bias_parts(c, q_heads);
-        for (int heads = tile_heads(q_heads / kv_heads); heads; heads /= 2)
-            parts = std::max<uint64_t>(parts, (uint64_t)tile_shape(c, heads).n_tiles);
+        for (int heads = tiles ? tile_heads(q_heads / kv_heads) : 0; heads; heads /= 2)
+            if (tile_table_holds(heads, c.s)) parts = std::max<uint64_t>(parts, (uint64_t)tile_shape(c, heads).n_tiles);
         w.bytes += parts * q_heads * c.s * 4;
     }
     return ISO_SUCCESS;
@@ -361,7 +366,7 @@ class AttentionBinder {
             ISO_TRY(r.heads(g->grad_v, n, nk, D, dt, true));
             if (g->grad_bias && !t.bias && c.s) return ISO_ERR_ARG;
             if (g->grad_bias) ISO_TRY(r.array(g->grad_bias, slots * size, size, true));
-            ISO_TRY(backward_workspace(c, nq, nk, g->grad_bias != nullptr, work));
+            ISO_TRY(backward_workspace(c, dt, nq, nk, D, g->grad_bias != nullptr, work));
             if (!workspace || workspace_bytes < work.bytes) return ISO_ERR_WORKSPACE;
             ISO_TRY(r.array(workspace, work.bytes, 4, true));
         }
@@ -393,7 +398,7 @@ class AttentionBinder {
             a.grad_k = device_heads(g->grad_k);
             a.grad_v = device_heads(g->grad_v);
             a.delta = (float *)((char *)workspace + work.delta);
-            a.starts = (float *)((char *)workspace + work.starts);
+            a.starts = work.norms > work.starts ? (float *)((char *)workspace + work.starts) : nullptr;
             a.norms = (float *)((char *)workspace + work.norms);
             a.partials = (float *)((char *)workspace + work.partials);
         }
@@ -443,7 +448,7 @@ class AttentionBinder {
         }
 
         void take(const AttentionBinder &o, Table &table, int heads, bool back, bool sums, size_t floats) {
-            if (o.t.rows || o.t.dtype == ISO_DTYPE_F32 || !o.is_wide || o.t.head_dim > kTileMaxHeadDim) return;
+            if (o.t.rows || !o.is_wide || !tile_tensors(o.t.dtype, o.t.head_dim)) return;
             if (!(std::fabs(o.t.scale) > 1e-20f && std::fabs(o.t.scale) < 1e20f)) return;      // the kernels divide by it
             if (o.t.cap > kPlainCap) return;                       // scores would be off by more than the weights' rounding
             for (const iso_heads_t *x : {&o.t.q, &o.t.k, &o.t.v, o.g ? &o.g->grad_out : &o.t.q})

@@ -109,6 +109,9 @@ inline Steps source_steps(const Comm &c) {
 }
 inline TileShape tile_shape(const Comm &c, int heads) { return tile_shape(c, kTileColumns / heads, 16 / heads, source_steps(c).reach); }
 
+// The index holds byte offsets of biases in 16 bits.
+inline bool tile_table_holds(int heads, int s) { return (int64_t)heads * (s + 1) * 4 <= 65535; }
+
 // back = false: columns are ranks, rows their sources R (-) C^i.  back = true: columns are sources, rows the ranks that read
 // them.  False where no table of that form exists (neighbours too many, or too far apart) or nothing would be in it (a mesh on
 // which no neighbour has a source at any rank): a tile that the kernels are given has one chunk of rows or more.
@@ -118,7 +121,7 @@ inline TileShape tile_shape(const Comm &c, int heads) { return tile_shape(c, kTi
 template <typename Pays>
 inline bool build_tile_plan(const Comm &c, int heads, bool back, bool bias_slots, TilePlan &out, Pays &&pays) {
     const int d = c.d, ranks = kTileColumns / heads, per_wave = 16 / heads;
-    if (c.s < 1 || (int64_t)heads * (c.s + 1) * 4 > 65535) return false;
+    if (c.s < 1 || !tile_table_holds(heads, c.s)) return false;
     Steps steps = source_steps(c);
     if (back)                              // from a source to its readers
         for (int i = 0; i < c.s; ++i)

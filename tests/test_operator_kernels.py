@@ -161,3 +161,22 @@ def test_shapes_of_the_tile_tests_take_tiles(kernels, shape, dtype):
     for bias in (False, True):
         names = short(kernels.start(dims, offsets, q_heads, kv_heads, D, dtype, periodic, backward=True, bias=bias))
         assert names == ["grad_q_tile", "grad_kv_tile"] + ["sum_parts"] * bias
+
+
+def test_the_workspace_holds_what_the_kernels_use(kernels):
+    """Partial sums by the tile only where tiles are possible: not for float32, odd rows, or more neighbours than their tables hold."""
+    import ctypes
+    lib = kernels.stub.iso.load_library()
+
+    def size(dims, offsets, q_heads, kv_heads, D, dtype, bias=True):
+        out = ctypes.c_size_t()
+        assert lib.iso_neighbor_attention_backward_workspace_bytes(kernels.stub.comm(dims, offsets).handle, TYPE[dtype], q_heads, kv_heads, D,
+                                                                   int(bias), ctypes.byref(out)) == 0
+        return out.value
+    window, rows = gen.moore(2, 6), 256 * 256 * 8
+    for dtype, D, by_row in (("f32", 64, 8), ("bf16", 63, 8), ("f16", 136, 8), ("bf16", 64, 16)):
+        assert size((256, 256), window, 8, 8, D, dtype, False) == by_row * rows
+        parts = (size((256, 256), window, 8, 8, D, dtype) - by_row * rows) / (8 * len(window) * 4)
+        assert parts == (1024 if by_row == 16 else 8192 // (8 * len(window)))
+    many = gen.moore(2, 64)                                        # 16640 neighbours
+    assert size((1000, 1000), many, 8, 8, 64, "bf16") == 16 * 8 * 10 ** 6 + 8 * len(many) * 4

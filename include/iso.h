@@ -468,12 +468,16 @@ int iso_neighbor_alltoall_noalloc(const void *sendbuf, void *recvbuf, size_t m, 
  * The calls return requests as the collectives' do: buffers are bound once, iso_start enqueues the kernels on a stream (on
  * one that is being captured as well) and returns, iso_wait and iso_request_free work as everywhere.  iso_start_range counts
  * the operator's kernels, iso_request_set_graph makes a chain of them in both forms, and iso_request_plan is ISO_ERR_ARG.
- * The same inputs give the same bits in every start.  Sums, softmax statistics and angles are held in 32 bits or more; what
- * is written is rounded to the tensors' type once.
+ * The same inputs give the same bits in every start.
+ * Rounding: scores, softmax statistics, angles and all sums are held in 32 bits or more, and results are rounded to the
+ * tensors' type once.  With 16-bit tensors the products of weights and rows (exp(x_i - lse) with v_i; in the backward pass
+ * those weights with grad_out, and the scores' gradients with q and k) may take the weights rounded to the tensors' type, as
+ * the matrix units do: half a unit in the last place of each.  A cap is off by about 2^-22 of itself up to 128, and by 2^-20 of
+ * the score above (16 bits).
  * Errors: ISO_ERR_ARG (null or misaligned pointer, bad count, type, scale or cap), ISO_ERR_TOO_LARGE (head_dim > 256, heads >
- * 65536, 2^31 rows or more, 2^34 or more of all heads together), ISO_ERR_OVERLAP (a written tensor shares bytes with another one, or two of its own rows do; rows
- * of tensors with the same strides are told apart, other tensors by the ranges that they span), ISO_ERR_POINTER and
- * ISO_ERR_WORKSPACE as in the collectives' init calls. */
+ * 65536, 2^31 rows or more, 2^34 or more of all heads together), ISO_ERR_OVERLAP (a written tensor shares bytes with another
+ * one, or two of its own rows do; rows of tensors with the same strides are told apart, other tensors by the ranges that they
+ * span), ISO_ERR_POINTER and ISO_ERR_WORKSPACE as in the collectives' init calls. */
 typedef struct {
     void *data;
     int64_t rank_stride, head_stride;
@@ -485,8 +489,9 @@ typedef struct {
  *     lse = log sum_i exp x_i    out = sum_i exp(x_i - lse) v_i
  * A neighbour does not count where it has no source (mesh), or where segments are given and its segment is not the rank's; a
  * negative segment holds no token.  Keys, values and biases of neighbours that do not count may hold anything, infinities and
- * NaN included.  A row without neighbours gets out = 0 and lse = -inf, and no gradient.  A bias of -inf takes its neighbour
- * out; where every bias of a row is -inf, the row is one without neighbours. */
+ * NaN included.  A row without neighbours gets out = 0 and lse = -inf, and no gradient.  A bias of -inf gives its neighbour
+ * no weight, if its key and value are finite (0 times a NaN stays one); where every bias of a row is -inf, the row is one
+ * without neighbours.  A finite bias far below the others' (-1e9, the type's lowest value) masks as well. */
 typedef struct {
     int32_t dtype;               /* enum iso_dtype: of q, k, v, out, bias and the gradients */
     int32_t q_heads, kv_heads;   /* kv_heads divides q_heads: head h reads key head h / (q_heads / kv_heads) */

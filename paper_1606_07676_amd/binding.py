@@ -556,7 +556,7 @@ def _attention(q, k, v, out, lse, bias, segments, scale, cap, rows, comm):
     if rows is None and n != p:
         raise ValueError(f"q must hold the rows of all {p} ranks, or `rows` say whose rows it holds")
     t = iso_attention_t(dtype=_dtype(q.dtype), q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, cap=cap,
-                        scale=head_dim ** -0.5 if scale is None else scale,
+                        scale=max(head_dim, 1) ** -0.5 if scale is None else scale,
                         n_rows=0 if rows is None else n)
     t.q, t.out = _heads(q, q.shape, q.dtype, "q"), _heads(out, q.shape, q.dtype, "out")
     t.k, t.v = (_heads(x, (p, kv_heads, head_dim), q.dtype, name) for x, name in ((k, "k"), (v, "v")))

@@ -238,3 +238,12 @@ def test_requests_of_operators(ops, stub_library):
         assert ops.raw.iso_request_set_graph(h, form) == 0 and ops.raw.iso_start(h, None) == 0 and ops.raw.iso_wait(h) == 0
     assert ops.raw.iso_request_free(ctypes.byref(h)) == 0
     assert ops.raw.iso_plan_create(ops.comm.handle, iso.ISO_OP_ATTENTION, 0, ctypes.byref(plan)) == iso.ISO_ERR_ARG
+
+
+def test_rows_without_elements_are_refused_from_python_too(ops):
+    """head_dim 0 has no default scale; the library says what is wrong."""
+    import torch
+    x = torch.empty(P, 2, 0)
+    with pytest.raises(ops.iso.IsoError) as e:
+        ops.iso.iso_neighbor_attention_init(x, x, x, torch.empty_like(x), ops.comm)
+    assert e.value.status == ops.iso.ISO_ERR_ARG

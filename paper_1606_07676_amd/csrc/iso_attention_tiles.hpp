@@ -403,9 +403,9 @@ template <typename F> __device__ __forceinline__ void redo_columns(bool bad, F &
     }
 }
 
-// Measured: 256 x 256 ranks, 169 neighbours, 8 heads of 64: 121 us of 41 for the bytes once (the row kernel 2.7 ms);
+// Measured: 256 x 256 ranks, 169 neighbours, 8 heads of 64: 120 us of 41 for the bytes once (the row kernel 2.7 ms);
 // 32 x 32 x 32, 27 neighbours, 8 query and 2 key heads of 128: 52 us of 26 (533).  What is left is waiting: finding the tile's
-// rows and storing the result take 40 us of the 121, in which no product can run.
+// rows and storing the result take 40 us of the 120, in which no product can run.
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256, DP > 64 ? 3 : SEGMENTS ? 4 : 5) void attention_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
@@ -612,7 +612,7 @@ struct SlotRound {
 
 // Two products for the scores and their gradients, one for grad_q, and the bias's gradient summed by slots, as a score's dx has
 // to be added to the others of its neighbour and no matrix product does that.  256 x 256 ranks, 49 neighbours, 8 heads of 64:
-// 210 us, vector units busy for 47 % of them; 32 x 32 x 32, 27 neighbours, 8 and 2 heads of 128: 106 us.
+// 213 us, vector units busy for 46 % of them; 32 x 32 x 32, 27 neighbours, 8 and 2 heads of 128: 105 us.
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256, 3) void attention_grad_q_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;
@@ -739,7 +739,7 @@ __global__ __launch_bounds__(256, 3) void attention_grad_q_tile_kernel(const Til
 }
 
 // Four products, with accumulators for two results: 200 registers at 128 elements, so that two workgroups share a CU, and the
-// wavefronts wait for 57 % of the time.  180 us and 132 us in the places of the above.
+// wavefronts wait for 56 % of the time.  179 us and 130 us in the places of the above.
 template <typename T, int DP, bool SEGMENTS>
 __global__ __launch_bounds__(256, 2) void attention_grad_kv_tile_kernel(const TileArgs t) {
     typedef typename Matrix<T>::f4 f4;

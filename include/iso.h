@@ -53,7 +53,12 @@ enum iso_op {
     /* in iso_request_info only: the operators on the ranks' tokens, which have no plan */
     ISO_OP_ATTENTION          = 2,
     ISO_OP_ATTENTION_BACKWARD = 3,
-    ISO_OP_ROTARY             = 4
+    ISO_OP_ROTARY             = 4,
+    ISO_OP_LAYER_NORM          = 5,
+    ISO_OP_LAYER_NORM_BACKWARD = 6,
+    ISO_OP_DROPOUT             = 7,
+    ISO_OP_GATED               = 8,
+    ISO_OP_GATED_BACKWARD      = 9
 };
 
 enum iso_dtype {                 /* element type of the operators' tensors      */
@@ -543,6 +548,85 @@ typedef struct {
     int32_t n_axes;              /* of positions */
 } iso_rotary_t;
 int iso_rotary_init(const iso_rotary_t *rotary, iso_comm_t comm, iso_request_t *req);      /* comm: NULL with positions */
+
+/* ---- operators on each token by itself --------------------------------------------
+ * What a layer does besides attention: rows are tokens, of all ranks or of a few, and no neighbourhood is needed.  Requests,
+ * rounding and errors are those of the operators above: sums, statistics and products are held in 32 bits or more and results
+ * rounded once, the same inputs give the same bits in every start, and nothing is enqueued for no tokens but the zeros of
+ * gradients that sum over them.  Requests that use one workspace must not overlap in time. */
+typedef struct {                 /* [n] rows of consecutive elements                  */
+    void *data;
+    int64_t stride;              /* elements between rows, >= 0; 0 repeats a row of an input */
+} iso_rows_t;
+
+/* Layer norm of every head's row by itself (heads = 1: of the token's row; heads > 1: of queries or keys where they lie).
+ *     h = (x - mean) rstd    out = weight h + bias    rstd = 1 / sqrt(var + eps), var = sum (x - mean)^2 / channels
+ * out may be x (same strides).
+ * ISO_ERR_TOO_LARGE: channels > 16384, heads > 65536, n * heads of 2^32 or more. */
+typedef struct {
+    int32_t dtype;               /* enum iso_dtype: of x, out, weight, bias and the gradients */
+    int32_t heads, channels;
+    int64_t n;
+    iso_heads_t x, out;          /* [n] rows of `heads` heads of `channels` elements */
+    const void *weight, *bias;   /* device [channels], the same for all heads, or NULL: 1 and 0 */
+    float eps;                   /* >= 0 */
+    float *mean, *rstd;          /* device [n][heads]; may be NULL in the forward pass */
+} iso_layer_norm_t;
+/* All are overwritten; grad_weight and grad_bias, of the tensors' type, add up all rows.  grad_x may be grad_out (same strides). */
+typedef struct {
+    iso_heads_t grad_out, grad_x;
+    void *grad_weight, *grad_bias;     /* device [channels], or NULL; grad_weight only with a weight */
+} iso_layer_norm_grads_t;
+int iso_layer_norm_init(const iso_layer_norm_t *norm, iso_request_t *req);
+/* norm->mean and ->rstd are what the forward pass wrote of the same x; its out, bias and eps are not read. */
+int iso_layer_norm_backward_init(const iso_layer_norm_t *norm, const iso_layer_norm_grads_t *grads,
+                                 void *workspace, size_t workspace_bytes, iso_request_t *req);
+int iso_layer_norm_backward_workspace_bytes(int64_t n, int heads, int channels, int dtype, size_t *bytes);
+
+/* Dropout from a counter-based generator: no mask is stored, and the gradient is the same call on grad_out, without a
+ * residual, while the seed is the same.
+ *     out = residual + x * 65536 / (65536 - t) where the element's number is t or more, residual elsewhere    t = rate * 65536, rounded
+ * (rate = 1: residual everywhere).  What is dropped may hold anything.  Element e of [n][channels] in row-major order takes 16
+ * bits, the (e % 8)th half word, low halves first, of the block of Philox4x32-10 with the counter (e / 8, seed[1]) and the key
+ * seed[0], low words first.  out may be x or residual (same stride).
+ * ISO_ERR_TOO_LARGE: n * channels of 2^35 or more. */
+typedef struct {
+    int32_t dtype, channels;
+    int64_t n;
+    iso_rows_t x, out;
+    iso_rows_t residual;         /* data NULL: none */
+    const uint64_t *seed;        /* device [2], read when the request is started */
+    float rate;                  /* 0 to 1 */
+} iso_dropout_t;
+int iso_dropout_init(const iso_dropout_t *dropout, iso_request_t *req);
+
+/* The gated projections of a feed-forward block:
+ *     out = f(x . gate) * (x . up)    f(g) = g / (1 + exp(-g))  or  g * (1 + erf(g / sqrt 2)) / 2
+ * The backward pass makes x . gate and x . up again, and keeps the gradients of both, rounded to the tensors' type, in its
+ * workspace: grad_x and the weights' gradients are products of those.
+ * ISO_ERR_TOO_LARGE: channels or hidden > 2^20, n of 2^31 or more. */
+enum iso_activation {
+    ISO_ACTIVATION_SILU = 0,
+    ISO_ACTIVATION_GELU = 1
+};
+typedef struct {
+    int32_t dtype, activation;
+    int32_t channels, hidden;
+    int64_t n;
+    iso_rows_t x;                /* [n] rows of `channels` */
+    iso_rows_t gate, up;         /* [hidden] rows of `channels` */
+    iso_rows_t out;              /* [n] rows of `hidden`; not read by the backward pass */
+} iso_gated_t;
+typedef struct {
+    iso_rows_t grad_out;         /* [n] rows of `hidden` */
+    iso_rows_t grad_x;           /* [n] rows of `channels` */
+    iso_rows_t grad_gate, grad_up;     /* [hidden] rows of `channels` */
+} iso_gated_grads_t;
+int iso_gated_init(const iso_gated_t *gated, iso_request_t *req);
+/* workspace: on a 16-byte boundary. */
+int iso_gated_backward_init(const iso_gated_t *gated, const iso_gated_grads_t *grads,
+                            void *workspace, size_t workspace_bytes, iso_request_t *req);
+int iso_gated_backward_workspace_bytes(int64_t n, int channels, int hidden, int dtype, size_t *bytes);
 
 /* ---- diagnostics ----------------------------------------------------------- */
 const char *iso_error_string(int status);

@@ -7,6 +7,8 @@ arguments.  PyTorch is used by callers for device memory and streams.
 from .binding import (  # noqa: F401
     IsoError, load_library, library_path,
     ISO_OP_ALLTOALL, ISO_OP_ALLGATHER, ISO_OP_ATTENTION, ISO_OP_ATTENTION_BACKWARD, ISO_OP_ROTARY,
+    ISO_OP_LAYER_NORM, ISO_OP_LAYER_NORM_BACKWARD, ISO_OP_DROPOUT, ISO_OP_GATED, ISO_OP_GATED_BACKWARD,
+    ISO_ACTIVATION_SILU, ISO_ACTIVATION_GELU,
     ISO_DTYPE_F32, ISO_DTYPE_BF16, ISO_DTYPE_F16,
     ISO_ALG_COMBINED, ISO_ALG_COMBINED_BYDIM, ISO_ALG_SX_ROUNDS, ISO_ALG_SX_FUSED, ISO_ALG_ONEHOP,
     ISO_ALG_COMBINED_STAGED,
@@ -28,6 +30,8 @@ from .binding import (  # noqa: F401
     iso_neighbor_alltoallv_init_layout, iso_neighbor_allgatherv_init_layout,
     iso_neighbor_attention_init, iso_neighbor_attention_backward_init, iso_neighbor_attention_backward_workspace_bytes,
     iso_rotary_init,
+    iso_layer_norm_init, iso_layer_norm_backward_init, iso_layer_norm_backward_workspace_bytes, iso_dropout_init,
+    iso_gated_init, iso_gated_backward_init, iso_gated_backward_workspace_bytes,
     iso_start, iso_start_range, iso_request_set_graph, iso_wait, iso_request_info, iso_request_start_info,
     iso_request_plan, iso_request_free,
     iso_error_string, iso_last_hip_error, iso_copy_reference,

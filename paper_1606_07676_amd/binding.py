@@ -16,6 +16,8 @@ ISO_MAX_DIMS = 16
 ISO_NOALLOC_SCRATCH_BYTES, ISO_NOALLOC_TABLE_BYTES = 32 << 20, 256 << 10
 ISO_OP_ALLTOALL, ISO_OP_ALLGATHER = 0, 1
 ISO_OP_ATTENTION, ISO_OP_ATTENTION_BACKWARD, ISO_OP_ROTARY = 2, 3, 4
+ISO_OP_LAYER_NORM, ISO_OP_LAYER_NORM_BACKWARD, ISO_OP_DROPOUT, ISO_OP_GATED, ISO_OP_GATED_BACKWARD = 5, 6, 7, 8, 9
+ISO_ACTIVATION_SILU, ISO_ACTIVATION_GELU = 0, 1
 ISO_DTYPE_F32, ISO_DTYPE_BF16, ISO_DTYPE_F16 = 0, 1, 2
 ISO_ALG_COMBINED, ISO_ALG_COMBINED_BYDIM, ISO_ALG_SX_ROUNDS, ISO_ALG_SX_FUSED, ISO_ALG_ONEHOP = 0, 1, 2, 3, 4
 ISO_ALG_COMBINED_STAGED = 5
@@ -101,6 +103,34 @@ class iso_rotary_t(ctypes.Structure):
                 ("axes", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n_axes", ctypes.c_int32)]
 
 
+class iso_rows_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class iso_layer_norm_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("channels", ctypes.c_int32), ("n", ctypes.c_int64),
+                ("x", iso_heads_t), ("out", iso_heads_t), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p)]
+
+
+class iso_layer_norm_grads_t(ctypes.Structure):
+    _fields_ = [("grad_out", iso_heads_t), ("grad_x", iso_heads_t), ("grad_weight", ctypes.c_void_p), ("grad_bias", ctypes.c_void_p)]
+
+
+class iso_dropout_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("channels", ctypes.c_int32), ("n", ctypes.c_int64), ("x", iso_rows_t), ("out", iso_rows_t),
+                ("residual", iso_rows_t), ("seed", ctypes.c_void_p), ("rate", ctypes.c_float)]
+
+
+class iso_gated_t(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("channels", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("n", ctypes.c_int64), ("x", iso_rows_t), ("gate", iso_rows_t), ("up", iso_rows_t), ("out", iso_rows_t)]
+
+
+class iso_gated_grads_t(ctypes.Structure):
+    _fields_ = [("grad_out", iso_rows_t), ("grad_x", iso_rows_t), ("grad_gate", iso_rows_t), ("grad_up", iso_rows_t)]
+
+
 def _struct_dict(st):
     out = {}
     for name, _ in st._fields_:
@@ -152,6 +182,14 @@ _PROTOTYPES = {
                                               _VP, _SZ, _VP, ctypes.POINTER(_VP)], _I),
     "iso_neighbor_attention_backward_workspace_bytes": ([_VP, _I, _I, _I, _I, _I, ctypes.POINTER(_SZ)], _I),
     "iso_rotary_init": ([ctypes.POINTER(iso_rotary_t), _VP, ctypes.POINTER(_VP)], _I),
+    "iso_layer_norm_init": ([ctypes.POINTER(iso_layer_norm_t), ctypes.POINTER(_VP)], _I),
+    "iso_layer_norm_backward_init": ([ctypes.POINTER(iso_layer_norm_t), ctypes.POINTER(iso_layer_norm_grads_t), _VP, _SZ,
+                                      ctypes.POINTER(_VP)], _I),
+    "iso_layer_norm_backward_workspace_bytes": ([ctypes.c_int64, _I, _I, _I, ctypes.POINTER(_SZ)], _I),
+    "iso_dropout_init": ([ctypes.POINTER(iso_dropout_t), ctypes.POINTER(_VP)], _I),
+    "iso_gated_init": ([ctypes.POINTER(iso_gated_t), ctypes.POINTER(_VP)], _I),
+    "iso_gated_backward_init": ([ctypes.POINTER(iso_gated_t), ctypes.POINTER(iso_gated_grads_t), _VP, _SZ, ctypes.POINTER(_VP)], _I),
+    "iso_gated_backward_workspace_bytes": ([ctypes.c_int64, _I, _I, _I, ctypes.POINTER(_SZ)], _I),
     "iso_start": ([_VP, _VP], _I),
     "iso_start_range": ([_VP, _I, _I, _VP], _I),
     "iso_request_set_graph": ([_VP, _I], _I),
@@ -624,6 +662,120 @@ def iso_rotary_init(x, out, freqs, axes, comm=None, *, positions=None, interleav
     _check(load_library().iso_rotary_init(ctypes.byref(t), comm.handle if comm is not None else None, ctypes.byref(h)),
            "iso_rotary_init")
     return Request(h.value, (x, out, positions))
+
+
+def _rows(x, shape, dtype, name):
+    """A [rows][elements] tensor with any stride but of its elements, as iso_rows_t."""
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}, not {tuple(x.shape)} of {x.dtype}")
+    if x.numel() and x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be consecutive")
+    return iso_rows_t(x.data_ptr() or None, x.stride(0))
+
+
+def _head_rows(x, like, name):
+    """[n][heads][channels], or [n][channels] as one head."""
+    if tuple(x.shape) != tuple(like.shape):
+        raise ValueError(f"{name} must be {tuple(like.shape)}, not {tuple(x.shape)}")
+    x = x if x.dim() == 3 else x.unsqueeze(1)
+    return _heads(x, x.shape, like.dtype, name)
+
+
+def _layer_norm(x, mean, rstd, weight):
+    import torch
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [tokens][channels] or [tokens][heads][channels]")
+    t = iso_layer_norm_t(dtype=_dtype(x.dtype), heads=x.shape[1] if x.dim() == 3 else 1, channels=x.shape[-1], n=x.shape[0])
+    t.x = _head_rows(x, x, "x")
+    t.mean, t.rstd = (_array(s, x.shape[:-1], torch.float32, name) for s, name in ((mean, "mean"), (rstd, "rstd")))
+    t.weight = _array(weight, x.shape[-1:], x.dtype, "weight")
+    return t
+
+
+def iso_layer_norm_init(x, out, *, weight=None, bias=None, eps=1e-5, mean=None, rstd=None):
+    """x, out: [tokens][channels], or [tokens][heads][channels] where every head's row is normalised by itself; any strides with
+    consecutive elements in a row; out may be x.  weight, bias: [channels].  mean, rstd: float32, x's shape without the channels."""
+    t = _layer_norm(x, mean, rstd, weight)
+    t.out, t.bias, t.eps = _head_rows(out, x, "out"), _array(bias, x.shape[-1:], x.dtype, "bias"), eps
+    h = ctypes.c_void_p()
+    _check(load_library().iso_layer_norm_init(ctypes.byref(t), ctypes.byref(h)), "iso_layer_norm_init")
+    return Request(h.value, (x, out, weight, bias, mean, rstd))
+
+
+def iso_layer_norm_backward_workspace_bytes(tokens, heads, channels, dtype):
+    """dtype: of the tensors (torch).  Only gradients of weight and bias need a workspace."""
+    out = ctypes.c_size_t()
+    _check(load_library().iso_layer_norm_backward_workspace_bytes(tokens, heads, channels, _dtype(dtype), ctypes.byref(out)),
+           "iso_layer_norm_backward_workspace_bytes")
+    return out.value
+
+
+def iso_layer_norm_backward_init(x, mean, rstd, grad_out, grad_x, workspace, *, weight=None, grad_weight=None, grad_bias=None,
+                                 workspace_bytes=None):
+    """mean, rstd: as the forward pass left them; grad_out, grad_x: shaped as x, any strides, grad_x may be grad_out.  workspace
+    may be None where neither grad_weight nor grad_bias is asked for."""
+    t = _layer_norm(x, mean, rstd, weight)
+    g = iso_layer_norm_grads_t(grad_out=_head_rows(grad_out, x, "grad_out"), grad_x=_head_rows(grad_x, x, "grad_x"))
+    g.grad_weight, g.grad_bias = (_array(s, x.shape[-1:], x.dtype, name) for s, name in ((grad_weight, "grad_weight"), (grad_bias, "grad_bias")))
+    h = ctypes.c_void_p()
+    _check(load_library().iso_layer_norm_backward_init(ctypes.byref(t), ctypes.byref(g), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                                       ctypes.byref(h)), "iso_layer_norm_backward_init")
+    return Request(h.value, (x, mean, rstd, grad_out, grad_x, workspace, weight, grad_weight, grad_bias))
+
+
+def iso_dropout_init(x, out, seed, rate, *, residual=None):
+    """x, out, residual: [tokens][channels], any stride between rows; out may be x or residual.  seed: two 64-bit integers on the
+    device, read at every start: give each start of a training step another second one, and its backward pass the same."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be [tokens][channels]")
+    t = iso_dropout_t(dtype=_dtype(x.dtype), channels=x.shape[1], n=x.shape[0], rate=rate, seed=_array(seed, (2,), torch.int64, "seed"))
+    t.x, t.out = _rows(x, x.shape, x.dtype, "x"), _rows(out, x.shape, x.dtype, "out")
+    if residual is not None:
+        t.residual = _rows(residual, x.shape, x.dtype, "residual")
+    h = ctypes.c_void_p()
+    _check(load_library().iso_dropout_init(ctypes.byref(t), ctypes.byref(h)), "iso_dropout_init")
+    return Request(h.value, (x, out, seed, residual))
+
+
+def _gated(x, gate, up, activation):
+    known = {"silu": ISO_ACTIVATION_SILU, "gelu": ISO_ACTIVATION_GELU}
+    if x.dim() != 2 or gate.dim() != 2:
+        raise ValueError("x must be [tokens][channels], gate and up [hidden][channels]")
+    if activation not in known:
+        raise ValueError('activation must be "silu" or "gelu"')
+    t = iso_gated_t(dtype=_dtype(x.dtype), activation=known[activation], channels=x.shape[1], hidden=gate.shape[0], n=x.shape[0])
+    t.x = _rows(x, x.shape, x.dtype, "x")
+    t.gate, t.up = (_rows(w, (gate.shape[0], x.shape[1]), x.dtype, name) for w, name in ((gate, "gate"), (up, "up")))
+    return t
+
+
+def iso_gated_init(x, gate, up, out, *, activation="silu"):
+    """x: [tokens][channels]; gate, up: [hidden][channels]; out: [tokens][hidden]; any strides between rows."""
+    t = _gated(x, gate, up, activation)
+    t.out = _rows(out, (x.shape[0], gate.shape[0]), x.dtype, "out")
+    h = ctypes.c_void_p()
+    _check(load_library().iso_gated_init(ctypes.byref(t), ctypes.byref(h)), "iso_gated_init")
+    return Request(h.value, (x, gate, up, out))
+
+
+def iso_gated_backward_workspace_bytes(tokens, channels, hidden, dtype):
+    """dtype: of the tensors (torch)."""
+    out = ctypes.c_size_t()
+    _check(load_library().iso_gated_backward_workspace_bytes(tokens, channels, hidden, _dtype(dtype), ctypes.byref(out)),
+           "iso_gated_backward_workspace_bytes")
+    return out.value
+
+
+def iso_gated_backward_init(x, gate, up, grad_out, grad_x, grad_gate, grad_up, workspace, *, activation="silu", workspace_bytes=None):
+    """grad_*: shaped as what they belong to, any strides between rows."""
+    t = _gated(x, gate, up, activation)
+    g = iso_gated_grads_t(_rows(grad_out, (x.shape[0], gate.shape[0]), x.dtype, "grad_out"), _rows(grad_x, x.shape, x.dtype, "grad_x"),
+                          _rows(grad_gate, gate.shape, x.dtype, "grad_gate"), _rows(grad_up, gate.shape, x.dtype, "grad_up"))
+    h = ctypes.c_void_p()
+    _check(load_library().iso_gated_backward_init(ctypes.byref(t), ctypes.byref(g), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                                  ctypes.byref(h)), "iso_gated_backward_init")
+    return Request(h.value, (x, gate, up, grad_out, grad_x, grad_gate, grad_up, workspace))
 
 
 def iso_start(req, stream=None):

@@ -15,6 +15,7 @@
 #include "iso_bind.hpp"
 #include "iso_kernels.hpp"
 #include "iso_operators.hpp"
+#include "iso_token_operators.hpp"
 #include "iso_plan.hpp"
 
 namespace iso {
@@ -624,6 +625,76 @@ int iso_rotary_init(const iso_rotary_t *rotary, iso_comm_t comm, iso_request_t *
         return make_operator_request(ISO_OP_ROTARY, comm ? &comm->c : nullptr, 0, req, [&](iso::BoundOperator &op) {
             return iso::bind_rotary(op, comm ? &comm->c : nullptr, *rotary);
         });
+    });
+}
+
+int iso_layer_norm_init(const iso_layer_norm_t *norm, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!norm) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_LAYER_NORM, nullptr, 0, req, [&](iso::BoundOperator &op) {
+            return iso::bind_layer_norm(op, *norm, nullptr, nullptr, 0);
+        });
+    });
+}
+
+int iso_layer_norm_backward_init(const iso_layer_norm_t *norm, const iso_layer_norm_grads_t *grads, void *workspace,
+                                 size_t workspace_bytes, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!norm || !grads) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_LAYER_NORM_BACKWARD, nullptr, workspace_bytes, req, [&](iso::BoundOperator &op) {
+            return iso::bind_layer_norm(op, *norm, grads, workspace, workspace_bytes);
+        });
+    });
+}
+
+int iso_layer_norm_backward_workspace_bytes(int64_t n, int heads, int channels, int dtype, size_t *bytes) {
+    return guarded([&]() -> int {
+        if (!bytes) return ISO_ERR_ARG;
+        const int st = iso::check_norm(n, heads, channels, dtype);
+        if (st != ISO_SUCCESS) return st;
+        *bytes = (size_t)iso::norm_workspace(n, heads, channels, dtype);
+        return ISO_SUCCESS;
+    });
+}
+
+int iso_dropout_init(const iso_dropout_t *dropout, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!dropout) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_DROPOUT, nullptr, 0, req, [&](iso::BoundOperator &op) { return iso::bind_dropout(op, *dropout); });
+    });
+}
+
+int iso_gated_init(const iso_gated_t *gated, iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!gated) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_GATED, nullptr, 0, req, [&](iso::BoundOperator &op) {
+            return iso::GatedBinder(op, *gated, nullptr).bind(nullptr, 0);
+        });
+    });
+}
+
+int iso_gated_backward_init(const iso_gated_t *gated, const iso_gated_grads_t *grads, void *workspace, size_t workspace_bytes,
+                            iso_request_t *req) {
+    return guarded([&]() -> int {
+        if (req) *req = nullptr;
+        if (!gated || !grads) return ISO_ERR_ARG;
+        return make_operator_request(ISO_OP_GATED_BACKWARD, nullptr, workspace_bytes, req, [&](iso::BoundOperator &op) {
+            return iso::GatedBinder(op, *gated, grads).bind(workspace, workspace_bytes);
+        });
+    });
+}
+
+int iso_gated_backward_workspace_bytes(int64_t n, int channels, int hidden, int dtype, size_t *bytes) {
+    return guarded([&]() -> int {
+        if (!bytes) return ISO_ERR_ARG;
+        const int st = iso::check_gated(n, channels, hidden, dtype);
+        if (st != ISO_SUCCESS) return st;
+        *bytes = (size_t)iso::gated_workspace(n, channels, hidden, dtype).bytes;
+        return ISO_SUCCESS;
     });
 }
 

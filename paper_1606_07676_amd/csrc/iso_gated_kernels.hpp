@@ -1,0 +1,522 @@
+// gfx950 kernels for the gated projections of a feed-forward block, and their gradients.
+//
+//     g = x . gate,  u = x . up,  out = f(g) u                          (rows of x: tokens; rows of gate and up: hidden units)
+//     d_up = grad_out f(g),  d_gate = grad_out u f'(g)
+//     grad_x = d_gate gate + d_up up,  grad_gate = d_gate^T x,  grad_up = d_up^T x
+//
+// All of it is matrix products, four kinds of them over one main loop (ProductKind); the activation, the product and its
+// derivatives happen on the accumulators of the first, so g and u are never stored: the backward pass makes them again (a third
+// of its products) and keeps d_gate and d_up in the tensors' type in its workspace.  All sums are 32-bit.
+//
+// The main loop: a workgroup takes a tile of the result, TileP elements along a row by TileQ rows.  Operands come in steps of
+// 128 bytes of the summed axis, 64 elements of 16 bits or 32 of 32, into one of two stages in LDS, one step ahead.  An operand
+// whose summed axis is its rows' (DOWN below) is read back transposed, so none is ever laid out anew in memory.
+#pragma once
+
+#include "iso_attention_kernels.hpp"
+#include "iso_attention_tiles.hpp"
+#include "iso_fastdiv.hpp"
+
+namespace iso {
+
+enum Activation { kSilu = ISO_ACTIVATION_SILU, kGelu = ISO_ACTIVATION_GELU };
+
+struct Rows {                              // element stride
+    const void *data;
+    int64_t stride;
+};
+
+enum class ProductKind {
+    kForward,                              // P: gate and up, half a tile each   Q: x             sum over channels
+    kGates,                                // the same, up to d_gate and d_up
+    kGradX,                                // P: gate, then up, down their rows  Q: d_gate, d_up  sum over hidden units, twice
+    kGradWeights                           // P: x, down its rows                Q: d_gate or d_up, down its rows    sum over tokens
+};
+
+struct ProductArgs {
+    Rows p[2], q[2], out[2];
+    Rows grad_out;                         // kGates
+    float *partials;                       // [splits][halves][rows of the result][elements of a row], where splits > 1
+    int32_t np, nq, nk;                    // elements of a result's row, its rows, length of the summed axis
+    int32_t steps, split_steps;            // of the whole summed axis, and of one split of it
+    int32_t splits;
+    uint32_t p_tiles, q_tiles;
+    FastDiv tiles, band_items;             // tiles of all halves; of a full band of kBand rows of tiles
+    uint32_t halves;                       // results of a kind: 2 for kGradWeights
+    uint32_t items, per_xcd, first_block;
+    int32_t activation;
+};
+
+constexpr int kBand = 8;
+constexpr int kStepBytes = 128;
+
+static __device__ const u4 kZeroUnit = {0, 0, 0, 0};
+
+// ---- activations -------------------------------------------------------------
+
+// f(g) = g s and f'(g).  In 16 bits the exponential and the reciprocal are the hardware's, off by 2^-22 or so.
+template <typename T> __device__ __forceinline__ void activate(int activation, float g, float &f, float &slope) {
+    if (activation == kSilu) {
+        float s;
+        if constexpr (sizeof(T) == 4) s = 1.f / (1.f + expf(-g));
+        else s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * g));
+        f = g * s;
+        slope = fmaf(f, 1.f - s, s);
+    } else {
+        const float c = 0.5f * erfcf(-0.70710678118654752440f * g);
+        f = g * c;
+        slope = fmaf(g * 0.39894228040143267794f, expf(-0.5f * g * g), c);
+    }
+}
+
+// ---- operands in LDS -----------------------------------------------------------
+
+// An operand's tile for one step.  !DOWN: N rows of 128 bytes, the summed axis along the row.  DOWN: one row of N elements for
+// each of the step's places on the summed axis.  16-byte units of a row are permuted by the row (turn), so that lanes that read
+// together find different banks.
+template <typename T, int N, bool DOWN, int THREADS> struct Operand {
+    static constexpr int E = 16 / sizeof(T), kStep = kStepBytes / sizeof(T), kBytes = N * kStepBytes;
+    static constexpr int kLoads = N * 8 / THREADS, kUnits = DOWN ? N / E : 8;       // loads of a lane, units of a row
+    static_assert(N * 8 % THREADS == 0);
+    const T *at[kLoads];
+
+    static __device__ __forceinline__ int turn(int row) {
+        if (!DOWN) return row & 7;
+        if (sizeof(T) == 2) return ((row & 3) << 1 | (row >> 3 & 1) << 3) & (kUnits - 1);
+        return (row >> 2 & 3) << 2;
+    }
+    static __device__ __forceinline__ int row_of(int i) { return (threadIdx.x + THREADS * i) / kUnits; }
+    static __device__ __forceinline__ int unit_of(int i) { return (threadIdx.x + THREADS * i) % kUnits ^ turn(row_of(i)); }
+
+    // row_at(r): row r of the tile, clamped to one that is there.  Its summed axis begins at k.
+    template <typename F> __device__ __forceinline__ void begin_rows(int k, F &&row_at) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) at[i] = (const T *)row_at(row_of(i)) + k + unit_of(i) * E;
+    }
+    // Elements from `first` on of rows k, k + 1, ..., of which there are `end`.
+    template <bool WHOLE_UNITS> __device__ __forceinline__ void begin_down(const Rows &x, int k, int first, int end) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int e = first + unit_of(i) * E;
+            if (WHOLE_UNITS) e = min(e, end - E);
+            at[i] = (const T *)x.data + (int64_t)(k + row_of(i)) * x.stride + e;
+        }
+    }
+    __device__ __forceinline__ void advance(int64_t stride) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) at[i] += DOWN ? kStep * stride : kStep;
+    }
+    // places: how many of the step's places on the summed axis there are; the others become zeros.
+    __device__ __forceinline__ void start(unsigned char *stage, int places) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const void *from = at[i];
+            if (places < kStep && (DOWN ? row_of(i) : unit_of(i) * E) >= places) from = &kZeroUnit;
+            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)stage +
+                                __builtin_amdgcn_readfirstlane((threadIdx.x & ~63u) * 16 + THREADS * 16 * i);
+            // straight into LDS, 16 bytes a lane, one lane's after the other's; waited for by wait_for_stage.  In assembly, as the
+            // compiler would wait for the whole stage before each transposing read of the other one.
+            uint32_t m0;
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                         : "=&s"(m0) : "s"(to), "v"(from) : "memory");
+        }
+    }
+
+    // The same through registers, for rows at any alignment and of any length.  end: elements of a row that are there, from the
+    // tile's first on (DOWN).
+    __device__ __forceinline__ void fetch(u4 (&held)[kLoads], int places, int end) const {
+        typedef T vec_t __attribute__((ext_vector_type(E)));
+        typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int along = unit_of(i) * E, left = DOWN ? (row_of(i) < places ? end - along : 0) : places - along;
+            vec_t v = {};
+            if (left >= E) {
+                v = *(const loose_t *)at[i];
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e < left) v[e] = at[i][e];
+            }
+            held[i] = __builtin_bit_cast(u4, v);
+        }
+    }
+    __device__ __forceinline__ void keep(const u4 (&held)[kLoads], unsigned char *stage) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) *(u4 *)(stage + (threadIdx.x + THREADS * i) * 16) = held[i];
+    }
+
+    // Where a lane reads: row or element lane % 16 of a group of 16, a quarter of the step's places by lane / 16.
+    static __device__ __forceinline__ uint32_t lane_base() {
+        const int lane = threadIdx.x & 63, quarter = lane / 16, within = lane % 16;
+        if (!DOWN) return within * kStepBytes + (quarter ^ (within & 7)) * 16;
+        if (sizeof(T) == 2) {
+            const int row = 8 * quarter + within / 4;
+            return row * N * 2 + (turn(row) ^ (within % 4 / 2)) * 16 + within % 2 * 8;
+        }
+        return 4 * quarter * N * 4 + ((quarter << 2) ^ (within / 4)) * 16 + within % 4 * 4;
+    }
+    // Group g of 16 rows or elements, half `h` of the step: 8 elements of 16 bits, or 4 of 32, of the summed axis.
+    static __device__ __forceinline__ u4 read(const unsigned char *stage, uint32_t base, int g, int h) {
+        if constexpr (!DOWN) {
+            return *(const u4 *)(stage + ((base + g * 16 * kStepBytes) ^ (h * 64)));
+        } else if constexpr (sizeof(T) == 2) {
+            constexpr int kGroups = kUnits / 2 < 8 ? kUnits / 2 : 8;       // groups of 16 that the permutation mixes
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4 *lds_t;
+            const unsigned char *from = stage + (base ^ (g % kGroups * 32)) + g / kGroups * kGroups * 32 + h * 32 * N * 2;
+            const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)from));
+            const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(from + 4 * N * 2)));
+            return u4{a.x, a.y, b.x, b.y};
+        } else {
+            const unsigned char *from = stage + (base ^ (g % 4 * 64)) + g / 4 * 256 + h * 16 * N * 4;
+            u4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *(const uint32_t *)(from + i * N * 4);
+            return v;
+        }
+    }
+};
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+template <typename T> __device__ __forceinline__ f4 multiply_units(u4 p, u4 q, f4 acc) {
+    if constexpr (sizeof(T) == 2) {
+        typedef typename Matrix<T>::x8 x8;
+        return Matrix<T>::multiply(__builtin_bit_cast(x8, p), __builtin_bit_cast(x8, q), acc);
+    } else {
+        const f4 x = __builtin_bit_cast(f4, p), y = __builtin_bit_cast(f4, q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], acc, 0, 0, 0);
+        return acc;
+    }
+}
+
+// ---- tiles ---------------------------------------------------------------------
+
+// WP x WQ wavefronts, each GP x GQ groups of 16 x 16.
+template <int WP_, int WQ_, int GP_, int GQ_> struct ProductTile {
+    static constexpr int WP = WP_, WQ = WQ_, GP = GP_, GQ = GQ_;
+    static constexpr int P = WP * GP * 16, Q = WQ * GQ * 16, kThreads = WP * WQ * 64;
+    static constexpr int kLds = 2 * (P + Q) * kStepBytes;
+};
+
+// Which tile a workgroup takes.  Workgroups go to the 8 XCDs in turn; each XCD takes a run of tiles, in bands of kBand rows of
+// tiles, so that those it has at a time share their operands in its L2.
+struct ProductWork {
+    int p, q, half, split;
+    bool any;
+};
+__device__ __forceinline__ ProductWork product_work(const ProductArgs &a) {
+    const uint32_t block = a.first_block + blockIdx.x, item = (block & 7) * a.per_xcd + (block >> 3);
+    ProductWork w{};
+    w.any = item < a.items;
+    uint32_t tile, split, half, band, within;
+    fast_divmod(item, a.tiles, split, tile);
+    half = tile >= a.p_tiles * a.q_tiles;
+    tile -= half ? a.p_tiles * a.q_tiles : 0;
+    fast_divmod(tile, a.band_items, band, within);
+    const uint32_t left = min(a.q_tiles - band * kBand, (uint32_t)kBand);         // rows of tiles of this band
+    w.p = left == kBand ? within / kBand : within / left;
+    w.q = band * kBand + (left == kBand ? within % kBand : within % left);
+    w.half = half;
+    w.split = split;
+    return w;
+}
+
+// What was started is in LDS, and all wavefronts have done with the stage before.
+__device__ __forceinline__ void wait_for_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <typename T> struct Quad { typedef T type __attribute__((ext_vector_type(4))); };
+
+// Four consecutive elements of a row, of which `left` are there, at any alignment.
+template <typename T> __device__ __forceinline__ void store_four(T *to, f4 v, int left) {
+    typedef typename Quad<T>::type vec_t;
+    typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+    vec_t y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = (T)v[r];
+    if (left >= 4) {
+        *(loose_t *)to = y;
+    } else {
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
+            if (r < left) to[r] = y[r];
+    }
+}
+template <typename T> __device__ __forceinline__ f4 load_four(const T *from, int left) {
+    typedef typename Quad<T>::type vec_t;
+    typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+    vec_t y = {};
+    if (left >= 4) {
+        y = *(const loose_t *)from;
+    } else {
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
+            if (r < left) y[r] = from[r];
+    }
+    return f4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+}
+
+// What becomes of four neighbouring hidden units of a token, h to h + 3, from their g and u.
+template <typename T, bool BACKWARD>
+__device__ __forceinline__ void gated_epilogue(const ProductArgs &a, int token, int h, f4 g, f4 u) {
+    f4 first, second;
+    if constexpr (BACKWARD) {
+        // rows of the workspace are whole units of 16 bytes; what is behind the last hidden unit stays out of all sums
+        const f4 dy = load_four((const T *)a.grad_out.data + (int64_t)token * a.grad_out.stride + h, a.np - h);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float f, slope;
+            activate<T>(a.activation, g[r], f, slope);
+            first[r] = h + r < a.np ? dy[r] * u[r] * slope : 0.f;
+            second[r] = h + r < a.np ? dy[r] * f : 0.f;
+        }
+        const int left = (int)a.out[0].stride - h;
+        store_four((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h, first, left);
+        store_four((T *)a.out[1].data + (int64_t)token * a.out[1].stride + h, second, left);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float f, slope;
+            activate<T>(a.activation, g[r], f, slope);
+            first[r] = f * u[r];
+        }
+        store_four((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h, first, a.np - h);
+    }
+}
+
+// DIRECT: operands lie on 16-byte boundaries in whole units and go straight to LDS.
+template <typename T, ProductKind KIND, typename Tile, bool DIRECT>
+__global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductArgs a) {
+    constexpr bool kPair = KIND == ProductKind::kForward || KIND == ProductKind::kGates;
+    constexpr int GP = Tile::GP, GQ = Tile::GQ;
+    typedef Operand<T, Tile::P, !kPair, Tile::kThreads> OperandP;
+    typedef Operand<T, Tile::Q, KIND == ProductKind::kGradWeights, Tile::kThreads> OperandQ;
+    constexpr int kStep = OperandP::kStep, kStage = OperandP::kBytes + OperandQ::kBytes;
+    __shared__ __align__(256) unsigned char stages[Tile::kLds];
+    const ProductWork work = product_work(a);
+    if (!work.any) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wp = wave % Tile::WP, wq = wave / Tile::WP;
+    // a pair's tile holds P / 2 units of either weight
+    const int p0 = work.p * (kPair ? Tile::P / 2 : Tile::P), q0 = work.q * Tile::Q;
+    const int first = work.split * a.split_steps, last = min(first + a.split_steps, a.steps);
+    const int part_steps = KIND == ProductKind::kGradX ? a.steps / 2 : a.steps;      // kGradX goes through both halves
+
+    OperandP p;
+    OperandQ q;
+    const auto begin = [&](int step) {
+        const int part = KIND == ProductKind::kGradX && step >= part_steps, k = (step - part * part_steps) * kStep;
+        const int half = KIND == ProductKind::kGradX ? part : work.half;
+        if constexpr (kPair) {
+            p.begin_rows(k, [&](int r) {
+                const int h = min(p0 + r % (Tile::P / 2), a.np - 1);
+                const Rows &w = r < Tile::P / 2 ? a.p[0] : a.p[1];
+                return (const T *)w.data + h * w.stride;
+            });
+        } else {
+            const Rows &w = KIND == ProductKind::kGradX ? a.p[part] : a.p[0];
+            p.template begin_down<DIRECT>(w, k, p0, a.np);
+        }
+        const Rows &y = kPair ? a.q[0] : a.q[half];
+        if constexpr (KIND == ProductKind::kGradWeights)
+            q.template begin_down<DIRECT>(y, k, q0, DIRECT ? (int)y.stride : a.nq);
+        else
+            q.begin_rows(k, [&](int r) { return (const T *)y.data + (int64_t)min(q0 + r, a.nq - 1) * y.stride; });
+    };
+    const auto advance = [&](int step) {                   // to `step`
+        if (KIND == ProductKind::kGradX && step == part_steps) {
+            begin(step);
+            return;
+        }
+        p.advance(KIND == ProductKind::kGradX && step > part_steps ? a.p[1].stride : a.p[0].stride);
+        q.advance(a.q[0].stride);
+    };
+    const auto places_of = [&](int step) {
+        return a.nk - (KIND == ProductKind::kGradX && step >= part_steps ? step - part_steps : step) * kStep;
+    };
+
+    f4 acc[GP][GQ] = {};
+    const uint32_t base_p = OperandP::lane_base(), base_q = OperandQ::lane_base();
+    const auto multiply = [&](const unsigned char *stage) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u4 ps[GP], qs[GQ];
+#pragma unroll
+            for (int i = 0; i < GP; ++i) {
+                // a pair's wavefront takes the same units of either weight
+                const int g = kPair ? wp * (GP / 2) + i % (GP / 2) + i / (GP / 2) * (Tile::P / 32) : wp * GP + i;
+                ps[i] = OperandP::read(stage, base_p, g, h);
+            }
+#pragma unroll
+            for (int j = 0; j < GQ; ++j) qs[j] = OperandQ::read(stage + OperandP::kBytes, base_q, wq * GQ + j, h);
+#pragma unroll
+            for (int i = 0; i < GP; ++i)
+#pragma unroll
+                for (int j = 0; j < GQ; ++j) acc[i][j] = multiply_units<T>(ps[i], qs[j], acc[i][j]);
+        }
+    };
+
+    if (first < last) {
+        begin(first);
+        if constexpr (DIRECT) {
+            p.start(stages, places_of(first));
+            q.start(stages + OperandP::kBytes, places_of(first));
+            for (int step = first; step < last; ++step) {
+                const int stage = (step - first) & 1;
+                wait_for_stage();
+                if (step + 1 < last) {
+                    advance(step + 1);
+                    p.start(stages + (stage ^ 1) * kStage, places_of(step + 1));
+                    q.start(stages + (stage ^ 1) * kStage + OperandP::kBytes, places_of(step + 1));
+                }
+                multiply(stages + stage * kStage);
+            }
+        } else {
+            u4 held_p[OperandP::kLoads], held_q[OperandQ::kLoads];
+            const auto fetch = [&](int step) {
+                const int places = min(places_of(step), kStep);
+                p.fetch(held_p, places, a.np - p0);
+                q.fetch(held_q, places, KIND == ProductKind::kGradWeights ? (int)a.q[0].stride - q0 : a.nq);
+            };
+            fetch(first);
+            p.keep(held_p, stages);
+            q.keep(held_q, stages + OperandP::kBytes);
+            for (int step = first; step < last; ++step) {
+                const int stage = (step - first) & 1;
+                __syncthreads();
+                if (step + 1 < last) {
+                    advance(step + 1);
+                    fetch(step + 1);
+                }
+                multiply(stages + stage * kStage);
+                if (step + 1 < last) {
+                    p.keep(held_p, stages + (stage ^ 1) * kStage);
+                    q.keep(held_q, stages + (stage ^ 1) * kStage + OperandP::kBytes);
+                }
+            }
+        }
+    }
+
+    // lane: row lane % 16 and elements 4 (lane / 16) + 0..3 of each group
+#pragma unroll
+    for (int j = 0; j < GQ; ++j) {
+        const int row = q0 + (wq * GQ + j) * 16 + lane % 16;
+        if (row >= a.nq) continue;
+        if constexpr (kPair) {
+            const int end = KIND == ProductKind::kGates ? (int)a.out[0].stride : a.np;
+#pragma unroll
+            for (int i = 0; i < GP / 2; ++i) {
+                const int h = p0 + (wp * (GP / 2) + i) * 16 + lane / 16 * 4;
+                if (h < end) gated_epilogue<T, KIND == ProductKind::kGates>(a, row, h, acc[i][j], acc[i + GP / 2][j]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < GP; ++i) {
+                const int e = p0 + (wp * GP + i) * 16 + lane / 16 * 4;
+                if (e >= a.np) continue;
+                if (a.splits > 1) {
+                    float *to = a.partials + (((uint64_t)work.split * a.halves + work.half) * a.nq + row) * a.np + e;
+                    store_four(to, acc[i][j], a.np - e);
+                } else {
+                    const Rows &y = a.out[work.half];
+                    store_four((T *)y.data + (int64_t)row * y.stride + e, acc[i][j], a.np - e);
+                }
+            }
+        }
+    }
+}
+
+struct ProductSumArgs {
+    const float *partials;                 // [splits][halves][rows][channels]
+    Rows out[2];
+    uint64_t slots;                        // halves * rows * channels
+    uint32_t rows, channels, splits;
+    uint32_t first_block;
+};
+
+// The splits of a sum, in their order.
+template <typename T> __global__ __launch_bounds__(256) void product_sum_kernel(const ProductSumArgs a) {
+    const uint64_t slot = ((uint64_t)a.first_block + blockIdx.x) * 1024 + threadIdx.x * 4;
+    if (slot >= a.slots) return;
+    const int there = (int)min(a.slots - slot, (uint64_t)4);
+    f4 sum = {};
+    for (uint32_t s = 0; s < a.splits; ++s) sum += load_four(a.partials + s * a.slots + slot, there);
+    uint64_t row = slot / a.channels;
+    uint32_t e = (uint32_t)(slot - row * a.channels);
+    for (int i = 0; i < there; ++i) {
+        const Rows &y = a.out[row >= a.rows];
+        ((T *)y.data)[(int64_t)(row >= a.rows ? row - a.rows : row) * y.stride + e] = (T)sum[i];
+        if (++e == a.channels) {
+            e = 0;
+            ++row;
+        }
+    }
+}
+
+// ---- few tokens ------------------------------------------------------------------
+
+// 16 hidden units of both weights to a workgroup, for up to 16 NT tokens: the weights' bytes bound it, so they go from memory to
+// the matrix units' registers once, with no stage between, and the wavefronts share the channels and join their sums in LDS.
+template <typename T, int NT, bool BACKWARD, bool DIRECT>
+__global__ __launch_bounds__(512) void gated_few_kernel(const ProductArgs a) {
+    constexpr int E = 16 / sizeof(T), kStep = 4 * E;       // channels of one product: 32 of 16 bits, 16 of 32
+    extern __shared__ __align__(16) unsigned char lds[];
+    typedef T vec_t __attribute__((ext_vector_type(E)));
+    typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    const int h0 = (int)(a.first_block + blockIdx.x) * 16, h = min(h0 + lane % 16, a.np - 1);
+    const T *gate = (const T *)a.p[0].data + h * a.p[0].stride, *up = (const T *)a.p[1].data + h * a.p[1].stride;
+    const T *x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x[t] = (const T *)a.q[0].data + (int64_t)min(t * 16 + lane % 16, a.nq - 1) * a.q[0].stride;
+    const auto load = [&](const T *row, int k) -> u4 {
+        vec_t v = {};
+        if (k + E <= a.nk) {
+            if (DIRECT) v = *(const vec_t *)(row + k);
+            else v = *(const loose_t *)(row + k);
+        } else if (!DIRECT) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (k + e < a.nk) v[e] = row[k + e];
+        }
+        return __builtin_bit_cast(u4, v);
+    };
+    f4 g[NT] = {}, u[NT] = {};
+    constexpr int kAtOnce = NT > 2 ? 2 : 4;                // products whose loads are under way together
+    for (int k0 = wave * kAtOnce * kStep; k0 < a.nk; k0 += waves * kAtOnce * kStep) {
+        u4 gs[kAtOnce], us[kAtOnce], xs[kAtOnce][NT];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int k = k0 + i * kStep + lane / 16 * E;
+            gs[i] = load(gate, k);
+            us[i] = load(up, k);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) xs[i][t] = load(x[t], k);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                g[t] = multiply_units<T>(gs[i], xs[i][t], g[t]);
+                u[t] = multiply_units<T>(us[i], xs[i][t], u[t]);
+            }
+    }
+    f4 *sums = (f4 *)lds;                                  // [wavefronts][NT][2][64]
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        sums[((wave * NT + t) * 2 + 0) * 64 + lane] = g[t];
+        sums[((wave * NT + t) * 2 + 1) * 64 + lane] = u[t];
+    }
+    __syncthreads();
+    for (int t = wave; t < NT; t += waves) {
+        f4 gs = {}, us = {};
+        for (int w = 0; w < waves; ++w) {
+            gs += sums[((w * NT + t) * 2 + 0) * 64 + lane];
+            us += sums[((w * NT + t) * 2 + 1) * 64 + lane];
+        }
+        const int token = t * 16 + lane % 16, at = h0 + lane / 16 * 4, end = BACKWARD ? (int)a.out[0].stride : a.np;
+        if (token < a.nq && at < end) gated_epilogue<T, BACKWARD>(a, token, at, gs, us);
+    }
+}
+
+}  // namespace iso

@@ -1,0 +1,404 @@
+// Host side of the operators on each token by itself (layer norm, dropout, gated projections): argument checks, the choice of
+// kernels and the launches of a request.
+#pragma once
+
+#include "iso_dropout_kernels.hpp"
+#include "iso_gated_kernels.hpp"
+#include "iso_norm_kernels.hpp"
+#include "iso_operators.hpp"
+
+namespace iso {
+
+inline int check_dtype(int dtype) {
+    return dtype == ISO_DTYPE_F32 || dtype == ISO_DTYPE_BF16 || dtype == ISO_DTYPE_F16 ? ISO_SUCCESS : ISO_ERR_ARG;
+}
+inline bool same_rows(const iso_heads_t &a, const iso_heads_t &b) {
+    return a.data == b.data && a.rank_stride == b.rank_stride && a.head_stride == b.head_stride;
+}
+inline bool same_rows(const iso_rows_t &a, const iso_rows_t &b) { return a.data == b.data && a.stride == b.stride; }
+inline iso_heads_t one_head(const iso_rows_t &t) { return iso_heads_t{t.data, t.stride, 0}; }
+inline bool wide(const iso_rows_t &t, int elements, int dtype) { return wide(one_head(t), elements, dtype); }
+
+// ---- layer norm --------------------------------------------------------------------
+
+// How lanes share a row: as few units a lane as let a wavefront hold it, else as many as a lane may hold.
+struct NormShape {
+    int units, per_lane, lanes;            // units of a row, of a lane (1, 2 or 4), lanes of a row
+    bool whole;                            // a row takes a workgroup
+    uint64_t groups() const { return whole ? 1 : 256 / lanes; }        // rows of a workgroup at a time
+    uint32_t threads() const { return whole ? (uint32_t)lanes : 256u; }
+};
+inline NormShape norm_shape(int channels, int dtype) {
+    const int E = dtype == ISO_DTYPE_F32 ? 4 : 8, most = kNormLaneElements / E;
+    NormShape s{(channels + E - 1) / E, 1, 1, false};
+    while (s.per_lane < most && (s.units + s.per_lane - 1) / s.per_lane > 64) s.per_lane *= 2;
+    while (s.lanes * s.per_lane < s.units) s.lanes *= 2;
+    s.whole = s.lanes > 64;
+    return s;
+}
+inline uint64_t norm_workgroups(const NormShape &s, uint64_t rows, uint64_t most) {
+    return std::clamp<uint64_t>((rows + s.groups() - 1) / s.groups(), 1, std::max<uint64_t>(1, most * 256 / s.threads()));
+}
+constexpr uint64_t kNormWorkgroups = 2048, kNormParts = 1024;          // of 256 threads
+
+inline int check_norm(int64_t n, int heads, int channels, int dtype) {
+    ISO_TRY(check_dtype(dtype));
+    if (n < 0 || heads < 1 || channels < 1) return ISO_ERR_ARG;
+    if (channels > kNormMaxChannels || heads > 65536 || n > 0xFFFFFFFFll / heads) return ISO_ERR_TOO_LARGE;
+    return ISO_SUCCESS;
+}
+inline uint64_t norm_workspace(int64_t n, int heads, int channels, int dtype) {
+    return norm_workgroups(norm_shape(channels, dtype), (uint64_t)n * heads, kNormParts) * 2 * channels * 4;
+}
+
+template <typename T, bool WIDE, int U> const void *norm_kernel(bool whole, bool backward, bool sums) {
+    if (!backward) return whole ? (const void *)(layer_norm_kernel<T, WIDE, U, true>) : (const void *)(layer_norm_kernel<T, WIDE, U, false>);
+    if (sums) return whole ? (const void *)(layer_norm_backward_kernel<T, WIDE, U, true, true>) : (const void *)(layer_norm_backward_kernel<T, WIDE, U, false, true>);
+    return whole ? (const void *)(layer_norm_backward_kernel<T, WIDE, U, true, false>) : (const void *)(layer_norm_backward_kernel<T, WIDE, U, false, false>);
+}
+template <typename T, bool WIDE> const void *norm_kernel(const NormShape &s, bool backward, bool sums) {
+    if (s.per_lane == 1) return norm_kernel<T, WIDE, 1>(s.whole, backward, sums);
+    if constexpr (sizeof(T) == 4)
+        if (s.per_lane == 4) return norm_kernel<T, WIDE, 4>(s.whole, backward, sums);
+    return norm_kernel<T, WIDE, 2>(s.whole, backward, sums);
+}
+inline const void *norm_kernel(int dtype, bool is_wide, const NormShape &s, bool backward, bool sums) {
+    switch (dtype) {
+        case ISO_DTYPE_F32: return is_wide ? norm_kernel<float, true>(s, backward, sums) : norm_kernel<float, false>(s, backward, sums);
+        case ISO_DTYPE_BF16: return is_wide ? norm_kernel<__bf16, true>(s, backward, sums) : norm_kernel<__bf16, false>(s, backward, sums);
+        default: return is_wide ? norm_kernel<_Float16, true>(s, backward, sums) : norm_kernel<_Float16, false>(s, backward, sums);
+    }
+}
+
+inline int bind_layer_norm(BoundOperator &b, const iso_layer_norm_t &t, const iso_layer_norm_grads_t *g, void *workspace,
+                           size_t workspace_bytes) {
+    ISO_TRY(check_norm(t.n, t.heads, t.channels, t.dtype));
+    if (!g && !(t.eps >= 0.f && t.eps <= 3.4e38f)) return ISO_ERR_ARG;
+    if (g && t.n && (!t.mean || !t.rstd)) return ISO_ERR_ARG;
+    if (g && g->grad_weight && !t.weight) return ISO_ERR_ARG;
+    const uint64_t n = (uint64_t)t.n, rows = n * t.heads, size = dtype_size(t.dtype), row_bytes = t.channels * size;
+    const bool sums = g && (g->grad_weight || g->grad_bias);
+    const uint64_t work = sums ? norm_workspace(t.n, t.heads, t.channels, t.dtype) : 0;
+    const iso_heads_t &in = g ? g->grad_out : t.x, &out = g ? g->grad_x : t.out;       // may be the same rows
+    Regions r;
+    ISO_TRY(r.heads(out, n, t.heads, t.channels, t.dtype, true));
+    if (g || !same_rows(in, out)) ISO_TRY(r.heads(t.x, n, t.heads, t.channels, t.dtype, false));
+    if (g && !same_rows(in, out)) ISO_TRY(r.heads(in, n, t.heads, t.channels, t.dtype, false));
+    if (t.weight) ISO_TRY(r.array(t.weight, row_bytes, size, false));
+    if (t.bias && !g) ISO_TRY(r.array(t.bias, row_bytes, size, false));
+    if (t.mean) ISO_TRY(r.array(t.mean, rows * 4, 4, !g));
+    if (t.rstd) ISO_TRY(r.array(t.rstd, rows * 4, 4, !g));
+    if (sums) {
+        if (g->grad_weight) ISO_TRY(r.array(g->grad_weight, row_bytes, size, true));
+        if (g->grad_bias) ISO_TRY(r.array(g->grad_bias, row_bytes, size, true));
+        if (!workspace || workspace_bytes < work) return ISO_ERR_WORKSPACE;
+        ISO_TRY(r.array(workspace, work, 4, true));
+    }
+    ISO_TRY(r.disjoint());
+    if (!rows && !sums) return ISO_SUCCESS;
+
+    const NormShape s = norm_shape(t.channels, t.dtype);
+    NormArgs a{};
+    a.x = device_heads(t.x);
+    a.out = device_heads(out);
+    if (g) a.grad_out = device_heads(in);
+    a.weight = t.weight;
+    a.bias = t.bias;
+    a.mean = t.mean;
+    a.rstd = t.rstd;
+    a.partials = (float *)workspace;
+    a.rows = rows;
+    a.heads = make_fastdiv((uint32_t)t.heads);
+    a.channels = t.channels;
+    a.units = s.units;
+    a.lanes = s.lanes;
+    a.eps = t.eps;
+    a.inverse = 1.f / (float)t.channels;
+    const auto at_16 = [](const void *p) { return ((uintptr_t)p & 15) == 0; };
+    const bool is_wide = wide(t.x, t.channels, t.dtype) && wide(out, t.channels, t.dtype) && wide(in, t.channels, t.dtype) && at_16(t.weight) &&
+                         (g || at_16(t.bias));
+    const void *func = norm_kernel(t.dtype, is_wide, s, g != nullptr, sums);
+    const uint64_t workgroups = norm_workgroups(s, rows, sums ? kNormParts : kNormWorkgroups);
+    ISO_TRY(add_launch(b, func, workgroups, s.threads(), a, sums && !s.whole ? 4 * 2 * (size_t)t.channels * 4 : 0));
+    if (!sums) return ISO_SUCCESS;
+    NormSumArgs sum{};
+    sum.partials = a.partials;
+    sum.out[0] = g->grad_weight;
+    sum.out[1] = g->grad_bias;
+    sum.parts = (int32_t)workgroups;
+    sum.channels = t.channels;
+    const void *sum_func = t.dtype == ISO_DTYPE_F32 ? (const void *)(layer_norm_sum_kernel<float>)
+                           : t.dtype == ISO_DTYPE_BF16 ? (const void *)(layer_norm_sum_kernel<__bf16>)
+                                                       : (const void *)(layer_norm_sum_kernel<_Float16>);
+    return add_launch(b, sum_func, (2 * (uint64_t)t.channels + 15) / 16, 1024, sum);
+}
+
+// ---- dropout -----------------------------------------------------------------------
+
+template <typename T, bool WIDE> struct DropoutKernel {
+    static const void *func() { return (const void *)(dropout_kernel<T, WIDE>); }
+};
+
+inline int bind_dropout(BoundOperator &b, const iso_dropout_t &t) {
+    ISO_TRY(check_dtype(t.dtype));
+    if (t.n < 0 || t.channels < 1 || !(t.rate >= 0.f && t.rate <= 1.f)) return ISO_ERR_ARG;
+    if (t.n > (int64_t(1) << 35) / t.channels) return ISO_ERR_TOO_LARGE;
+    const uint64_t n = (uint64_t)t.n, elements = n * t.channels;
+    if (elements >> 35) return ISO_ERR_TOO_LARGE;
+    const bool residual = t.residual.data != nullptr;
+    Regions r;
+    ISO_TRY(r.heads(one_head(t.out), n, 1, t.channels, t.dtype, true));
+    if (!same_rows(t.x, t.out)) ISO_TRY(r.heads(one_head(t.x), n, 1, t.channels, t.dtype, false));
+    if (residual && !same_rows(t.residual, t.out)) ISO_TRY(r.heads(one_head(t.residual), n, 1, t.channels, t.dtype, false));
+    if (n) ISO_TRY(r.array(t.seed, 16, 8, false));
+    ISO_TRY(r.disjoint());
+    if (!n) return ISO_SUCCESS;
+
+    DropoutArgs a{};
+    a.x = t.x.data;
+    a.out = t.out.data;
+    a.residual = t.residual.data;
+    a.x_stride = t.x.stride;
+    a.out_stride = t.out.stride;
+    a.residual_stride = t.residual.stride;
+    a.seed = t.seed;
+    a.elements = elements;
+    a.blocks = (uint32_t)((elements + 7) / 8);
+    a.channels = (uint32_t)t.channels;
+    a.row_blocks = make_fastdiv((uint32_t)std::max(1, t.channels / 8));
+    const auto all = [&](auto &&ok) { return ok(t.x) && ok(t.out) && (!residual || ok(t.residual)); };
+    a.flat = n == 1 || all([&](const iso_rows_t &x) { return x.stride == t.channels; });
+    const bool is_wide = a.flat ? all([](const iso_rows_t &x) { return ((uintptr_t)x.data & 15) == 0; })
+                                : t.channels % 8 == 0 && all([&](const iso_rows_t &x) { return wide(x, t.channels, t.dtype); });
+    a.threshold = (uint32_t)std::floor((double)t.rate * 65536 + 0.5);
+    a.scale = a.threshold < 65536 ? 65536.f / (float)(65536 - a.threshold) : 0.f;
+    return add_launch(b, by_type<DropoutKernel>(t.dtype, is_wide), ((uint64_t)a.blocks + 255) / 256, 256, a);
+}
+
+// ---- gated projections ----------------------------------------------------------------
+
+constexpr int kGatedMaxWidth = 1 << 20;
+constexpr int kFewTokens = 64;
+
+typedef ProductTile<4, 2, 4, 8> LargeTile;         // 256 x 256, 8 wavefronts
+typedef ProductTile<2, 2, 4, 4> MiddleTile;        // 128 x 128, 4
+typedef ProductTile<2, 2, 2, 2> SmallTile;         // 64 x 64, 4
+
+// How a product is cut up.
+struct ProductPlan {
+    int tile;                              // 0 large, 1 middle, 2 small
+    int size;                              // of the tile
+    uint64_t p_tiles, q_tiles;
+    int steps, splits, split_steps;
+};
+
+// np: elements of a result's row (of a pair: hidden units of one weight), nq: its rows, nk: the summed axis.
+inline ProductPlan plan_product(ProductKind kind, int dtype, bool direct, uint64_t np, uint64_t nq, uint64_t nk) {
+    static constexpr int kSize[3] = {256, 128, 64};
+    const bool pair = kind == ProductKind::kForward || kind == ProductKind::kGates;
+    const uint64_t halves = kind == ProductKind::kGradWeights ? 2 : 1;
+    const int step = kStepBytes / (int)dtype_size(dtype);
+    ProductPlan plan{};
+    for (plan.tile = dtype == ISO_DTYPE_F32 || !direct ? 1 : 0;; ++plan.tile) {
+        plan.size = kSize[plan.tile];
+        const uint64_t width = pair ? plan.size / 2 : plan.size;
+        plan.p_tiles = (np + width - 1) / width;
+        plan.q_tiles = (nq + plan.size - 1) / plan.size;
+        if (plan.tile == 2 || plan.p_tiles * plan.q_tiles * halves >= 192) break;
+    }
+    plan.steps = (int)((nk + step - 1) / step) * (kind == ProductKind::kGradX ? 2 : 1);
+    plan.splits = 1;
+    const uint64_t tiles = plan.p_tiles * plan.q_tiles * halves;
+    if (!pair && tiles < 256) plan.splits = (int)std::clamp<uint64_t>(512 / std::max<uint64_t>(1, tiles), 1, std::max(1, plan.steps / 8));
+    plan.split_steps = std::max(1, (plan.steps + plan.splits - 1) / plan.splits);
+    plan.splits = std::max(1, (plan.steps + plan.split_steps - 1) / plan.split_steps);
+    return plan;
+}
+
+template <typename T, ProductKind KIND> const void *product_func(int tile, bool direct) {
+    if constexpr (sizeof(T) == 2)
+        if (tile == 0) return (const void *)(product_kernel<T, KIND, LargeTile, true>);
+    if (tile <= 1) return direct ? (const void *)(product_kernel<T, KIND, MiddleTile, true>) : (const void *)(product_kernel<T, KIND, MiddleTile, false>);
+    return direct ? (const void *)(product_kernel<T, KIND, SmallTile, true>) : (const void *)(product_kernel<T, KIND, SmallTile, false>);
+}
+template <ProductKind KIND> const void *product_func(int dtype, int tile, bool direct) {
+    switch (dtype) {
+        case ISO_DTYPE_F32: return product_func<float, KIND>(tile, direct);
+        case ISO_DTYPE_BF16: return product_func<__bf16, KIND>(tile, direct);
+        default: return product_func<_Float16, KIND>(tile, direct);
+    }
+}
+template <typename T, bool BACKWARD> const void *few_func(int groups, bool direct) {
+    if (groups == 1) return direct ? (const void *)(gated_few_kernel<T, 1, BACKWARD, true>) : (const void *)(gated_few_kernel<T, 1, BACKWARD, false>);
+    if (groups == 2) return direct ? (const void *)(gated_few_kernel<T, 2, BACKWARD, true>) : (const void *)(gated_few_kernel<T, 2, BACKWARD, false>);
+    return direct ? (const void *)(gated_few_kernel<T, 4, BACKWARD, true>) : (const void *)(gated_few_kernel<T, 4, BACKWARD, false>);
+}
+template <bool BACKWARD> const void *few_func(int dtype, int groups, bool direct) {
+    switch (dtype) {
+        case ISO_DTYPE_F32: return few_func<float, BACKWARD>(groups, direct);
+        case ISO_DTYPE_BF16: return few_func<__bf16, BACKWARD>(groups, direct);
+        default: return few_func<_Float16, BACKWARD>(groups, direct);
+    }
+}
+
+inline int64_t gated_padded(int hidden) { return (hidden + 7) / 8 * 8; }
+
+struct GatedWorkspace {
+    uint64_t half = 0, partials = 0, bytes = 0;    // bytes of d_gate; offset of the sums of splits
+};
+inline GatedWorkspace gated_workspace(int64_t n, int channels, int hidden, int dtype) {
+    GatedWorkspace w;
+    w.half = ((uint64_t)n * gated_padded(hidden) * dtype_size(dtype) + 255) / 256 * 256;
+    w.partials = 2 * w.half;
+    uint64_t most = 0;
+    for (bool direct : {false, true}) {
+        const ProductPlan x = plan_product(ProductKind::kGradX, dtype, direct, channels, n, hidden);
+        const ProductPlan weights = plan_product(ProductKind::kGradWeights, dtype, direct, channels, hidden, n);
+        if (x.splits > 1) most = std::max(most, (uint64_t)x.splits * n * channels * 4);
+        if (weights.splits > 1) most = std::max(most, (uint64_t)weights.splits * 2 * hidden * channels * 4);
+    }
+    w.bytes = w.partials + most;
+    return w;
+}
+inline int check_gated(int64_t n, int channels, int hidden, int dtype) {
+    ISO_TRY(check_dtype(dtype));
+    if (n < 0 || channels < 1 || hidden < 1) return ISO_ERR_ARG;
+    if (channels > kGatedMaxWidth || hidden > kGatedMaxWidth || n > 0x7FFFFFFF) return ISO_ERR_TOO_LARGE;
+    return ISO_SUCCESS;
+}
+
+class GatedBinder {
+  public:
+    GatedBinder(BoundOperator &out, const iso_gated_t &gated, const iso_gated_grads_t *grads) : b(out), t(gated), g(grads) {}
+
+    int bind(void *workspace, size_t workspace_bytes) {
+        ISO_TRY(check_gated(t.n, t.channels, t.hidden, t.dtype));
+        if (t.activation != ISO_ACTIVATION_SILU && t.activation != ISO_ACTIVATION_GELU) return ISO_ERR_ARG;
+        ISO_TRY(check_buffers(workspace, workspace_bytes));
+        return g ? backward((char *)workspace) : forward();
+    }
+
+  private:
+    int check_buffers(void *workspace, size_t workspace_bytes) {
+        Regions r;
+        const uint64_t n = (uint64_t)t.n, hidden = (uint64_t)t.hidden;
+        const auto rows = [&](const iso_rows_t &x, uint64_t count, int width, bool written) {
+            return r.heads(one_head(x), count, 1, width, t.dtype, written);
+        };
+        ISO_TRY(rows(t.x, n, t.channels, false));
+        ISO_TRY(rows(t.gate, n ? hidden : 0, t.channels, false));
+        ISO_TRY(rows(t.up, n ? hidden : 0, t.channels, false));
+        if (!g) {
+            ISO_TRY(rows(t.out, n, t.hidden, true));
+            return r.disjoint();
+        }
+        ISO_TRY(rows(g->grad_out, n, t.hidden, false));
+        ISO_TRY(rows(g->grad_x, n, t.channels, true));
+        ISO_TRY(rows(g->grad_gate, hidden, t.channels, true));
+        ISO_TRY(rows(g->grad_up, hidden, t.channels, true));
+        work = gated_workspace(t.n, t.channels, t.hidden, t.dtype);
+        if (work.bytes && (!workspace || workspace_bytes < work.bytes)) return ISO_ERR_WORKSPACE;
+        ISO_TRY(r.array(workspace, work.bytes, 16, true));
+        return r.disjoint();
+    }
+
+    static Rows device_rows(const iso_rows_t &x) { return Rows{x.data, x.stride}; }
+
+    int add_product(ProductKind kind, const void *func(int, int, bool), bool direct, ProductArgs a, void *partials) {
+        const ProductPlan plan = plan_product(kind, t.dtype, direct, a.np, a.nq, a.nk);
+        a.halves = kind == ProductKind::kGradWeights ? 2 : 1;
+        a.steps = plan.steps;
+        a.splits = plan.splits;
+        a.split_steps = plan.split_steps;
+        a.p_tiles = (uint32_t)plan.p_tiles;
+        a.q_tiles = (uint32_t)plan.q_tiles;
+        const uint64_t tiles = plan.p_tiles * plan.q_tiles * a.halves, items = tiles * plan.splits;
+        if (items > 0x7FFFFFF0ull) return ISO_ERR_TOO_LARGE;
+        a.tiles = make_fastdiv((uint32_t)tiles);
+        a.band_items = make_fastdiv((uint32_t)plan.p_tiles * kBand);
+        a.items = (uint32_t)items;
+        a.per_xcd = (uint32_t)((items + 7) / 8);
+        a.partials = (float *)partials;
+        a.activation = t.activation;
+        ISO_TRY(add_launch(b, func(t.dtype, plan.tile, direct), (uint64_t)a.per_xcd * 8, plan.tile == 0 ? LargeTile::kThreads : 256, a));
+        if (plan.splits == 1) return ISO_SUCCESS;
+        ProductSumArgs s{};
+        s.partials = a.partials;
+        s.out[0] = a.out[0];
+        s.out[1] = a.out[1];
+        s.slots = (uint64_t)a.halves * a.nq * a.np;
+        s.rows = (uint32_t)a.nq;
+        s.channels = (uint32_t)a.np;
+        s.splits = (uint32_t)plan.splits;
+        const void *sum_func = t.dtype == ISO_DTYPE_F32 ? (const void *)(product_sum_kernel<float>)
+                               : t.dtype == ISO_DTYPE_BF16 ? (const void *)(product_sum_kernel<__bf16>)
+                                                           : (const void *)(product_sum_kernel<_Float16>);
+        return add_launch(b, sum_func, (s.slots + 1023) / 1024, 256, s);
+    }
+
+    // g and u of all tokens, up to out or to d_gate and d_up.
+    template <bool BACKWARD> int add_projections(ProductArgs a) {
+        a.p[0] = device_rows(t.gate);
+        a.p[1] = device_rows(t.up);
+        a.q[0] = device_rows(t.x);
+        a.np = t.hidden;
+        a.nq = (int32_t)t.n;
+        a.nk = t.channels;
+        const bool direct = wide(t.gate, t.channels, t.dtype) && wide(t.up, t.channels, t.dtype) && wide(t.x, t.channels, t.dtype);
+        if (t.n <= kFewTokens) {
+            const int groups = t.n <= 16 ? 1 : t.n <= 32 ? 2 : 4;
+            a.activation = t.activation;
+            return add_launch(b, few_func<BACKWARD>(t.dtype, groups, direct), ((uint64_t)t.hidden + 15) / 16, 512, a, (size_t)groups << 14);
+        }
+        constexpr ProductKind kind = BACKWARD ? ProductKind::kGates : ProductKind::kForward;
+        return add_product(kind, product_func<kind>, direct, a, nullptr);
+    }
+
+    int forward() {
+        if (!t.n) return ISO_SUCCESS;
+        ProductArgs a{};
+        a.out[0] = device_rows(t.out);
+        return add_projections<false>(a);
+    }
+
+    int backward(char *workspace) {
+        const int64_t padded = gated_padded(t.hidden);
+        const Rows d_gate{workspace, padded}, d_up{workspace + work.half, padded};
+        void *partials = workspace + work.partials;
+        if (t.n) {
+            ProductArgs a{};
+            a.out[0] = d_gate;
+            a.out[1] = d_up;
+            a.grad_out = device_rows(g->grad_out);
+            ISO_TRY(add_projections<true>(a));
+            a = ProductArgs{};
+            a.p[0] = device_rows(t.gate);
+            a.p[1] = device_rows(t.up);
+            a.q[0] = d_gate;
+            a.q[1] = d_up;
+            a.out[0] = device_rows(g->grad_x);
+            a.np = t.channels;
+            a.nq = (int32_t)t.n;
+            a.nk = t.hidden;
+            ISO_TRY(add_product(ProductKind::kGradX, product_func<ProductKind::kGradX>,
+                                wide(t.gate, t.channels, t.dtype) && wide(t.up, t.channels, t.dtype), a, partials));
+        }
+        ProductArgs a{};
+        a.p[0] = device_rows(t.x);
+        a.q[0] = d_gate;
+        a.q[1] = d_up;
+        a.out[0] = device_rows(g->grad_gate);
+        a.out[1] = device_rows(g->grad_up);
+        a.np = t.channels;
+        a.nq = t.hidden;
+        a.nk = (int32_t)t.n;
+        return add_product(ProductKind::kGradWeights, product_func<ProductKind::kGradWeights>, wide(t.x, t.channels, t.dtype), a, partials);
+    }
+
+    BoundOperator &b;
+    const iso_gated_t &t;
+    const iso_gated_grads_t *g;
+    GatedWorkspace work;
+};
+
+}  // namespace iso

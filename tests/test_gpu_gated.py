@@ -1,0 +1,176 @@
+"""Gated projections and their gradients against the 64-bit oracle, element by element inside the error that rounding allows."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1606_07676_amd as iso
+from oracle import token_oracle as orc
+from token_rows import DEV, TYPES, U, host, inside_rows, untouched_around, within
+
+pytestmark = pytest.mark.gpu
+
+# tokens, channels, hidden
+FEW = [(1, 1, 1), (1, 64, 16), (1, 136, 40), (5, 33, 17), (16, 256, 48), (17, 100, 31), (32, 512, 24), (37, 520, 90), (64, 1040, 33), (63, 72, 130)]
+TILED = [(65, 8, 8), (65, 1, 3), (70, 64, 64), (129, 130, 65), (100, 200, 300), (200, 72, 132), (333, 65, 127), (257, 264, 72), (65, 700, 513)]
+# enough tiles for the larger ones, with rows and elements left over
+LARGE = [(1500, 136, 1100), (2100, 72, 1928), (3333, 24, 1672)]
+
+
+def tensors(n, C, F, dtype, seed=0):
+    g = torch.Generator(DEV).manual_seed(seed)
+    normal = lambda *size: torch.randn(*size, device=DEV, generator=g)  # noqa: E731
+    return {"x": normal(n, C).to(TYPES[dtype]), "gate": (2 * normal(F, C) * C ** -0.5).to(TYPES[dtype]),
+            "up": (normal(F, C) * C ** -0.5).to(TYPES[dtype]), "dy": normal(n, F).to(TYPES[dtype])}
+
+
+def forward(t, activation, out=None, stream=None):
+    out = torch.full_like(t["dy"], 7) if out is None else out
+    req = iso.iso_gated_init(t["x"], t["gate"], t["up"], out, activation=activation)
+    iso.iso_start(req, stream)
+    iso.iso_wait(req)
+    return out
+
+
+def backward(t, activation, into=None):
+    (n, C), F = t["x"].shape, t["gate"].shape[0]
+    grads = into or {k: torch.full_like(t[k], 7) for k in ("x", "gate", "up")}
+    size = iso.iso_gated_backward_workspace_bytes(n, C, F, t["x"].dtype)
+    work = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device=DEV)
+    req = iso.iso_gated_backward_init(t["x"], t["gate"], t["up"], t["dy"], grads["x"], grads["gate"], grads["up"], work,
+                                      activation=activation, workspace_bytes=size)
+    iso.iso_start(req)
+    iso.iso_wait(req)
+    assert bool((work[size:] == 0xA5).all()), "written behind the workspace"
+    return grads
+
+
+def near(got, want, error, u, what):
+    """Inside the bound element by element; and, as roundings are independent, far inside it together: the roundings of a result
+    and of what it is a sum of are each at most u of a value, u / sqrt 3 on average, together u sqrt(2 / 3) of the values' size;
+    three times that, and what is off in 32 bits."""
+    within(host(got), want, orc.rounded(want, error, u), what)
+    size = np.sqrt(np.mean(want ** 2))
+    if got.numel() >= 256 and size:
+        assert np.sqrt(np.mean((host(got) - want) ** 2)) <= (3 * u * (2 / 3) ** 0.5 + 64 * orc.EPS) * size, what
+
+
+def check(t, dtype, activation, out, grads=None):
+    u = U[dtype]
+    o = orc.Gated(*(host(t[k]) for k in ("x", "gate", "up")), activation, dtype != "f32")
+    within(host(out), o.out, o.out_bound(u), "out")
+    if grads is None:
+        return
+    o.backward(host(t["dy"]), u)
+    near(grads["x"], o.grad_x, o.grad_x_error, u, "grad_x")
+    near(grads["gate"], o.grad_gate, o.grad_gate_error, u, "grad_gate")
+    near(grads["up"], o.grad_up, o.grad_up_error, u, "grad_up")
+
+
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", FEW + TILED, ids=str)
+def test_projections_and_gradients(shape, dtype, activation):
+    t = tensors(*shape, dtype)
+    check(t, dtype, activation, forward(t, activation), backward(t, activation))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+def test_many_tiles(shape, dtype):
+    t = tensors(*shape, dtype, seed=1)
+    out, grads = forward(t, "silu"), backward(t, "silu")
+    check(t, dtype, "silu", out, grads)
+    assert torch.equal(forward(t, "silu"), out)
+    for name, value in backward(t, "silu").items():
+        assert torch.equal(value, grads[name]), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_tokens_in_the_sum(dtype):
+    """The weights' gradient sums over tokens in parts."""
+    t = tensors(20000, 40, 56, dtype, seed=2)
+    check(t, dtype, "gelu", forward(t, "gelu"), backward(t, "gelu"))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(9, 64, 48), (150, 64, 72)], ids=str)
+@pytest.mark.parametrize("gap,shift", [(8, 0), (1, 0), (8, 3)])
+def test_rows_inside_larger_buffers(gap, shift, shape, dtype):
+    """Any strides and addresses; what lies around the rows stays as it was."""
+    t = tensors(*shape, dtype, seed=3)
+    views = {k: inside_rows(tuple(v.shape), v.dtype, gap, shift) for k, v in t.items()}
+    for k, v in t.items():
+        views[k].copy_(v)
+    out = inside_rows(tuple(t["dy"].shape), t["dy"].dtype, gap, shift)
+    into = {k: inside_rows(tuple(t[k].shape), t[k].dtype, gap, shift) for k in ("x", "gate", "up")}
+    check(t, dtype, "silu", forward(views, "silu", out), backward(views, "silu", into))
+    for view in [out, *into.values()]:
+        untouched_around(view)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [30, 100])
+def test_weights_in_one_buffer_and_one_row_for_all(n, dtype):
+    t = tensors(n, 48, 40, dtype, seed=4)
+    both = torch.cat([t["gate"], t["up"]])
+    t["gate"], t["up"] = both[:40], both[40:]
+    t["x"] = t["x"][:1].expand(n, 48)
+    grads = {k: torch.empty(t[k].shape, device=DEV, dtype=t[k].dtype) for k in ("x", "gate", "up")}
+    check(t, dtype, "silu", forward(t, "silu"), backward(t, "silu", grads))
+    t["up"] = t["gate"]
+    check(t, dtype, "gelu", forward(t, "gelu"), backward(t, "gelu", grads))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+@pytest.mark.parametrize("n", [4, 90])
+def test_far_ends_of_the_activations(n, activation, dtype):
+    """Hidden units far below and above zero give 0 and g itself, with slopes 0 and 1, and no infinity on the way."""
+    t = tensors(n, 16, 32, dtype, seed=5)
+    t["x"][:, 0] = 1
+    t["gate"][:, 1:] = 0
+    t["gate"][:, 0] = torch.linspace(-300, 300, 32, device=DEV).to(TYPES[dtype])
+    check(t, dtype, activation, forward(t, activation), backward(t, activation))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [20, 200])
+def test_a_token_that_is_not_a_number_stays_by_itself(n, dtype):
+    """Also at the ends of tiles, next to rows and elements that are not there."""
+    t = tensors(n, 72, 41, dtype, seed=6)
+    clean, grads = forward(t, "silu"), backward(t, "silu")
+    bad = [0, 7, n - 1]
+    good = torch.ones(n, dtype=torch.bool, device=DEV)
+    good[bad] = False
+    t["x"][0], t["x"][7, 3], t["x"][n - 1, 71] = float("nan"), float("inf"), float("-inf")
+    out, again = forward(t, "silu"), backward(t, "silu")
+    assert torch.equal(out[good], clean[good]) and torch.equal(again["x"][good], grads["x"][good])
+    assert out[0].isnan().all() and again["gate"].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_tokens(dtype):
+    t = tensors(0, 40, 24, dtype)
+    assert forward(t, "silu").shape == (0, 24)
+    grads = backward(t, "silu")
+    assert not grads["gate"].any() and not grads["up"].any()
+
+
+def test_another_stream():
+    t = tensors(300, 128, 256, "bf16", seed=7)
+    want, other = forward(t, "gelu"), torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        assert torch.equal(forward(t, "gelu", stream=other), want)
+
+
+@pytest.mark.parametrize("n", [6, 80])
+def test_gradient_against_differences(n):
+    t = tensors(n, 20, 24, "f32", seed=8)
+    grads, dy = backward(t, "gelu"), host(t["dy"])
+    for name in ("x", "gate", "up"):
+        direction = np.random.default_rng(9).normal(size=t[name].shape)
+        value = lambda s: float((orc.Gated(*(host(t[k]) + (s * direction if k == name else 0) for k in ("x", "gate", "up")),  # noqa: E731
+                                           "gelu", False).out * dy).sum())
+        change = (value(1e-6) - value(-1e-6)) / 2e-6
+        assert abs(change - float((host(grads[name]) * direction).sum())) < 1e-5 * np.abs(host(grads[name]) * direction).sum() + 1e-6, name

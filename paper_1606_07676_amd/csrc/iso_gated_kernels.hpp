@@ -38,6 +38,7 @@ struct ProductArgs {
     Rows grad_out;                         // kGates
     float *partials;                       // [splits][halves][rows of the result][elements of a row], where splits > 1
     int32_t np, nq, nk;                    // elements of a result's row, its rows, length of the summed axis
+    int32_t p_units;                       // elements of a row of P in whole units of 16 bytes, where P is gone through down its rows
     int32_t steps, split_steps;            // of the whole summed axis, and of one split of it
     int32_t splits;
     uint32_t p_tiles, q_tiles;
@@ -93,14 +94,11 @@ template <typename T, int N, bool DOWN, int THREADS> struct Operand {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) at[i] = (const T *)row_at(row_of(i)) + k + unit_of(i) * E;
     }
-    // Elements from `first` on of rows k, k + 1, ..., of which there are `end`.
-    template <bool WHOLE_UNITS> __device__ __forceinline__ void begin_down(const Rows &x, int k, int first, int end) {
+    // Elements from `first` on of rows k, k + 1, ..., which hold `end`, a multiple of E.
+    __device__ __forceinline__ void begin_down(const Rows &x, int k, int first, int end) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            int e = first + unit_of(i) * E;
-            if (WHOLE_UNITS) e = min(e, end - E);
-            at[i] = (const T *)x.data + (int64_t)(k + row_of(i)) * x.stride + e;
-        }
+        for (int i = 0; i < kLoads; ++i)
+            at[i] = (const T *)x.data + (int64_t)(k + row_of(i)) * x.stride + min(first + unit_of(i) * E, end - E);
     }
     __device__ __forceinline__ void advance(int64_t stride) {
 #pragma unroll
@@ -122,14 +120,13 @@ template <typename T, int N, bool DOWN, int THREADS> struct Operand {
         }
     }
 
-    // The same through registers, for rows at any alignment and of any length.  end: elements of a row that are there, from the
-    // tile's first on (DOWN).
-    __device__ __forceinline__ void fetch(u4 (&held)[kLoads], int places, int end) const {
+    // The same through registers, for rows at any alignment and of any length (!DOWN).
+    __device__ __forceinline__ void fetch(u4 (&held)[kLoads], int places) const {
         typedef T vec_t __attribute__((ext_vector_type(E)));
         typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int along = unit_of(i) * E, left = DOWN ? (row_of(i) < places ? end - along : 0) : places - along;
+            const int left = places - unit_of(i) * E;
             vec_t v = {};
             if (left >= E) {
                 v = *(const loose_t *)at[i];
@@ -285,10 +282,12 @@ __device__ __forceinline__ void gated_epilogue(const ProductArgs &a, int token, 
     }
 }
 
-// DIRECT: operands lie on 16-byte boundaries in whole units and go straight to LDS.
+// DIRECT: operands lie on 16-byte boundaries in whole units and go straight to LDS.  The backward pass sees to that, with copies
+// in its workspace where need be; the forward pass, which has none, takes other rows through registers.
 template <typename T, ProductKind KIND, typename Tile, bool DIRECT>
 __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductArgs a) {
     constexpr bool kPair = KIND == ProductKind::kForward || KIND == ProductKind::kGates;
+    static_assert(DIRECT || KIND == ProductKind::kForward);
     constexpr int GP = Tile::GP, GQ = Tile::GQ;
     typedef Operand<T, Tile::P, !kPair, Tile::kThreads> OperandP;
     typedef Operand<T, Tile::Q, KIND == ProductKind::kGradWeights, Tile::kThreads> OperandQ;
@@ -315,11 +314,11 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
             });
         } else {
             const Rows &w = KIND == ProductKind::kGradX ? a.p[part] : a.p[0];
-            p.template begin_down<DIRECT>(w, k, p0, a.np);
+            p.begin_down(w, k, p0, a.p_units);
         }
         const Rows &y = kPair ? a.q[0] : a.q[half];
         if constexpr (KIND == ProductKind::kGradWeights)
-            q.template begin_down<DIRECT>(y, k, q0, DIRECT ? (int)y.stride : a.nq);
+            q.begin_down(y, k, q0, (int)y.stride);
         else
             q.begin_rows(k, [&](int r) { return (const T *)y.data + (int64_t)min(q0 + r, a.nq - 1) * y.stride; });
     };
@@ -374,9 +373,8 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
         } else {
             u4 held_p[OperandP::kLoads], held_q[OperandQ::kLoads];
             const auto fetch = [&](int step) {
-                const int places = min(places_of(step), kStep);
-                p.fetch(held_p, places, a.np - p0);
-                q.fetch(held_q, places, KIND == ProductKind::kGradWeights ? (int)a.q[0].stride - q0 : a.nq);
+                p.fetch(held_p, places_of(step));
+                q.fetch(held_q, places_of(step));
             };
             fetch(first);
             p.keep(held_p, stages);
@@ -424,6 +422,37 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
             }
         }
     }
+}
+
+struct AlignArgs {
+    Rows from[3], to[3];                   // to: rows of whole units
+    uint64_t rows[3], first_unit[4];       // first_unit: units of the tensors before
+    int32_t channels, units;               // units of a row
+    uint32_t first_block;
+};
+
+// Rows at any alignment and of any length into rows of whole 16-byte units, zeros behind their end.
+template <typename T> __global__ __launch_bounds__(256) void align_rows_kernel(const AlignArgs a) {
+    constexpr int E = 16 / sizeof(T);
+    typedef T vec_t __attribute__((ext_vector_type(E)));
+    typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+    uint64_t unit = ((uint64_t)a.first_block + blockIdx.x) * 256 + threadIdx.x;
+    if (unit >= a.first_unit[3]) return;
+    const int which = unit >= a.first_unit[2] ? 2 : unit >= a.first_unit[1] ? 1 : 0;
+    unit -= a.first_unit[which];
+    const uint64_t row = unit / a.units;
+    const int at = (int)(unit - row * a.units) * E;
+    const Rows &x = a.from[which], &y = a.to[which];
+    const T *from = (const T *)x.data + (int64_t)row * x.stride;
+    vec_t v = {};
+    if (at + E <= a.channels) {
+        v = *(const loose_t *)(from + at);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (at + e < a.channels) v[e] = from[at + e];
+    }
+    *(vec_t *)((T *)y.data + (int64_t)row * y.stride + at) = v;
 }
 
 struct ProductSumArgs {

@@ -193,13 +193,13 @@ struct ProductPlan {
 };
 
 // np: elements of a result's row (of a pair: hidden units of one weight), nq: its rows, nk: the summed axis.
-inline ProductPlan plan_product(ProductKind kind, int dtype, bool direct, uint64_t np, uint64_t nq, uint64_t nk) {
+inline ProductPlan plan_product(ProductKind kind, int dtype, uint64_t np, uint64_t nq, uint64_t nk) {
     static constexpr int kSize[3] = {256, 128, 64};
     const bool pair = kind == ProductKind::kForward || kind == ProductKind::kGates;
     const uint64_t halves = kind == ProductKind::kGradWeights ? 2 : 1;
     const int step = kStepBytes / (int)dtype_size(dtype);
     ProductPlan plan{};
-    for (plan.tile = dtype == ISO_DTYPE_F32 || !direct ? 1 : 0;; ++plan.tile) {
+    for (plan.tile = dtype == ISO_DTYPE_F32 ? 1 : 0;; ++plan.tile) {
         plan.size = kSize[plan.tile];
         const uint64_t width = pair ? plan.size / 2 : plan.size;
         plan.p_tiles = (np + width - 1) / width;
@@ -216,10 +216,15 @@ inline ProductPlan plan_product(ProductKind kind, int dtype, bool direct, uint64
 }
 
 template <typename T, ProductKind KIND> const void *product_func(int tile, bool direct) {
+    if constexpr (KIND == ProductKind::kForward)
+        if (!direct) {
+            if constexpr (sizeof(T) == 2)
+                if (tile == 0) return (const void *)(product_kernel<T, KIND, LargeTile, false>);
+            return tile <= 1 ? (const void *)(product_kernel<T, KIND, MiddleTile, false>) : (const void *)(product_kernel<T, KIND, SmallTile, false>);
+        }
     if constexpr (sizeof(T) == 2)
         if (tile == 0) return (const void *)(product_kernel<T, KIND, LargeTile, true>);
-    if (tile <= 1) return direct ? (const void *)(product_kernel<T, KIND, MiddleTile, true>) : (const void *)(product_kernel<T, KIND, MiddleTile, false>);
-    return direct ? (const void *)(product_kernel<T, KIND, SmallTile, true>) : (const void *)(product_kernel<T, KIND, SmallTile, false>);
+    return tile <= 1 ? (const void *)(product_kernel<T, KIND, MiddleTile, true>) : (const void *)(product_kernel<T, KIND, SmallTile, true>);
 }
 template <ProductKind KIND> const void *product_func(int dtype, int tile, bool direct) {
     switch (dtype) {
@@ -241,23 +246,30 @@ template <bool BACKWARD> const void *few_func(int dtype, int groups, bool direct
     }
 }
 
-inline int64_t gated_padded(int hidden) { return (hidden + 7) / 8 * 8; }
+inline int64_t whole_units(int elements) { return (elements + 7) / 8 * 8; }
 
+// Offsets, each a multiple of 256 bytes: d_gate and d_up of all tokens, copies of x, gate and up with aligned rows where theirs are
+// not, the sums of splits.
 struct GatedWorkspace {
-    uint64_t half = 0, partials = 0, bytes = 0;    // bytes of d_gate; offset of the sums of splits
+    uint64_t d_gate = 0, d_up = 0, copies[3] = {}, partials = 0, bytes = 0;
 };
 inline GatedWorkspace gated_workspace(int64_t n, int channels, int hidden, int dtype) {
     GatedWorkspace w;
-    w.half = ((uint64_t)n * gated_padded(hidden) * dtype_size(dtype) + 255) / 256 * 256;
-    w.partials = 2 * w.half;
-    uint64_t most = 0;
-    for (bool direct : {false, true}) {
-        const ProductPlan x = plan_product(ProductKind::kGradX, dtype, direct, channels, n, hidden);
-        const ProductPlan weights = plan_product(ProductKind::kGradWeights, dtype, direct, channels, hidden, n);
-        if (x.splits > 1) most = std::max(most, (uint64_t)x.splits * n * channels * 4);
-        if (weights.splits > 1) most = std::max(most, (uint64_t)weights.splits * 2 * hidden * channels * 4);
-    }
-    w.bytes = w.partials + most;
+    const auto take = [&](uint64_t rows, int width) {
+        const uint64_t at = w.bytes;
+        w.bytes += (rows * whole_units(width) * dtype_size(dtype) + 255) / 256 * 256;
+        return at;
+    };
+    w.d_gate = take(n, hidden);
+    w.d_up = take(n, hidden);
+    w.copies[0] = take(n, channels);
+    w.copies[1] = take(n ? hidden : 0, channels);
+    w.copies[2] = take(n ? hidden : 0, channels);
+    w.partials = w.bytes;
+    const ProductPlan x = plan_product(ProductKind::kGradX, dtype, channels, n, hidden);
+    const ProductPlan weights = plan_product(ProductKind::kGradWeights, dtype, channels, hidden, n);
+    if (x.splits > 1) w.bytes += (uint64_t)x.splits * n * channels * 4;
+    if (weights.splits > 1) w.bytes = std::max(w.bytes, w.partials + (uint64_t)weights.splits * 2 * hidden * channels * 4);
     return w;
 }
 inline int check_gated(int64_t n, int channels, int hidden, int dtype) {
@@ -305,7 +317,7 @@ class GatedBinder {
     static Rows device_rows(const iso_rows_t &x) { return Rows{x.data, x.stride}; }
 
     int add_product(ProductKind kind, const void *func(int, int, bool), bool direct, ProductArgs a, void *partials) {
-        const ProductPlan plan = plan_product(kind, t.dtype, direct, a.np, a.nq, a.nk);
+        const ProductPlan plan = plan_product(kind, t.dtype, a.np, a.nq, a.nk);
         a.halves = kind == ProductKind::kGradWeights ? 2 : 1;
         a.steps = plan.steps;
         a.splits = plan.splits;
@@ -336,69 +348,109 @@ class GatedBinder {
         return add_launch(b, sum_func, (s.slots + 1023) / 1024, 256, s);
     }
 
+    int32_t units_end() const {                // of a row's elements, in whole units
+        const int E = 16 / (int)dtype_size(t.dtype);
+        return (t.channels + E - 1) / E * E;
+    }
+    bool direct(const iso_rows_t &x) const { return wide(x, t.channels, t.dtype); }
+
     // g and u of all tokens, up to out or to d_gate and d_up.
     template <bool BACKWARD> int add_projections(ProductArgs a) {
-        a.p[0] = device_rows(t.gate);
-        a.p[1] = device_rows(t.up);
-        a.q[0] = device_rows(t.x);
         a.np = t.hidden;
         a.nq = (int32_t)t.n;
         a.nk = t.channels;
-        const bool direct = wide(t.gate, t.channels, t.dtype) && wide(t.up, t.channels, t.dtype) && wide(t.x, t.channels, t.dtype);
         if (t.n <= kFewTokens) {
+            const bool aligned = direct(t.gate) && direct(t.up) && direct(t.x);
             const int groups = t.n <= 16 ? 1 : t.n <= 32 ? 2 : 4;
+            a.p[0] = device_rows(t.gate);
+            a.p[1] = device_rows(t.up);
+            a.q[0] = device_rows(t.x);
             a.activation = t.activation;
-            return add_launch(b, few_func<BACKWARD>(t.dtype, groups, direct), ((uint64_t)t.hidden + 15) / 16, 512, a, (size_t)groups << 14);
+            return add_launch(b, few_func<BACKWARD>(t.dtype, groups, aligned), ((uint64_t)t.hidden + 15) / 16, 512, a, (size_t)groups << 14);
         }
+        a.p[0] = gate;
+        a.p[1] = up;
+        a.q[0] = x;
         constexpr ProductKind kind = BACKWARD ? ProductKind::kGates : ProductKind::kForward;
-        return add_product(kind, product_func<kind>, direct, a, nullptr);
+        return add_product(kind, product_func<kind>, BACKWARD || (direct(t.gate) && direct(t.up) && direct(t.x)), a, nullptr);
     }
 
     int forward() {
         if (!t.n) return ISO_SUCCESS;
         ProductArgs a{};
+        x = device_rows(t.x);
+        gate = device_rows(t.gate);
+        up = device_rows(t.up);
         a.out[0] = device_rows(t.out);
         return add_projections<false>(a);
     }
 
+    // The backward pass's products need rows on 16-byte boundaries in whole units: others are copied first.  2000 tokens, 2685
+    // channels, 8192 hidden units, bfloat16: 0.65 ms in place of 2.2 with products that take such rows through registers.
+    int align_rows(char *workspace) {
+        AlignArgs a{};
+        a.channels = t.channels;
+        const int width = (int)whole_units(t.channels);
+        a.units = width / (16 / (int)dtype_size(t.dtype));
+        const iso_rows_t *const from[3] = {&t.x, &t.gate, &t.up};
+        Rows *const to[3] = {&x, &gate, &up};
+        for (int i = 0; i < 3; ++i) {
+            *to[i] = device_rows(*from[i]);
+            if (!direct(*from[i])) {
+                a.from[i] = *to[i];
+                a.to[i] = *to[i] = Rows{workspace + work.copies[i], width};
+                a.rows[i] = i ? (uint64_t)t.hidden : (uint64_t)t.n;
+            }
+            a.first_unit[i + 1] = a.first_unit[i] + a.rows[i] * a.units;
+        }
+        if (!a.first_unit[3]) return ISO_SUCCESS;
+        const void *func = t.dtype == ISO_DTYPE_F32 ? (const void *)(align_rows_kernel<float>)
+                           : t.dtype == ISO_DTYPE_BF16 ? (const void *)(align_rows_kernel<__bf16>)
+                                                       : (const void *)(align_rows_kernel<_Float16>);
+        return add_launch(b, func, (a.first_unit[3] + 255) / 256, 256, a);
+    }
+
     int backward(char *workspace) {
-        const int64_t padded = gated_padded(t.hidden);
-        const Rows d_gate{workspace, padded}, d_up{workspace + work.half, padded};
+        const int64_t padded = whole_units(t.hidden);
+        const Rows d_gate{workspace + work.d_gate, padded}, d_up{workspace + work.d_up, padded};
         void *partials = workspace + work.partials;
         if (t.n) {
+            ISO_TRY(align_rows(workspace));
             ProductArgs a{};
             a.out[0] = d_gate;
             a.out[1] = d_up;
             a.grad_out = device_rows(g->grad_out);
             ISO_TRY(add_projections<true>(a));
             a = ProductArgs{};
-            a.p[0] = device_rows(t.gate);
-            a.p[1] = device_rows(t.up);
+            a.p[0] = gate;
+            a.p[1] = up;
             a.q[0] = d_gate;
             a.q[1] = d_up;
             a.out[0] = device_rows(g->grad_x);
             a.np = t.channels;
+            a.p_units = units_end();
             a.nq = (int32_t)t.n;
             a.nk = t.hidden;
-            ISO_TRY(add_product(ProductKind::kGradX, product_func<ProductKind::kGradX>,
-                                wide(t.gate, t.channels, t.dtype) && wide(t.up, t.channels, t.dtype), a, partials));
+            ISO_TRY(add_product(ProductKind::kGradX, product_func<ProductKind::kGradX>, true, a, partials));
         }
         ProductArgs a{};
-        a.p[0] = device_rows(t.x);
+        a.p[0] = x;
         a.q[0] = d_gate;
         a.q[1] = d_up;
         a.out[0] = device_rows(g->grad_gate);
         a.out[1] = device_rows(g->grad_up);
         a.np = t.channels;
+        a.p_units = units_end();
         a.nq = t.hidden;
         a.nk = (int32_t)t.n;
-        return add_product(ProductKind::kGradWeights, product_func<ProductKind::kGradWeights>, wide(t.x, t.channels, t.dtype), a, partials);
+        return add_product(ProductKind::kGradWeights, product_func<ProductKind::kGradWeights>, true, a, partials);
     }
 
     BoundOperator &b;
     const iso_gated_t &t;
     const iso_gated_grads_t *g;
     GatedWorkspace work;
+    Rows x{}, gate{}, up{};                // as the products read them
 };
 
 }  // namespace iso

@@ -74,12 +74,12 @@ template <typename T> __device__ __forceinline__ void activate(int activation, f
 
 // An operand's tile for one step.  !DOWN: N rows of 128 bytes, the summed axis along the row.  DOWN: one row of N elements for
 // each of the step's places on the summed axis.  16-byte units of a row are permuted by the row (turn), so that lanes that read
-// together find different banks.
-template <typename T, int N, bool DOWN, int THREADS> struct Operand {
+// together find different banks.  PAIR: the rows are those of two tensors, half a tile each.
+template <typename T, int N, bool DOWN, bool PAIR, int THREADS> struct Operand {
     static constexpr int E = 16 / sizeof(T), kStep = kStepBytes / sizeof(T), kBytes = N * kStepBytes;
     static constexpr int kLoads = N * 8 / THREADS, kUnits = DOWN ? N / E : 8;       // loads of a lane, units of a row
-    static_assert(N * 8 % THREADS == 0);
-    const T *at[kLoads];
+    static constexpr int kThreads = THREADS, kTensors = PAIR ? 2 : 1, kRows = PAIR ? N / 2 : N;
+    static_assert(N * 8 % THREADS == 0 && (!PAIR || kLoads % 2 == 0));
 
     static __device__ __forceinline__ int turn(int row) {
         if (!DOWN) return row & 7;
@@ -88,59 +88,51 @@ template <typename T, int N, bool DOWN, int THREADS> struct Operand {
     }
     static __device__ __forceinline__ int row_of(int i) { return (threadIdx.x + THREADS * i) / kUnits; }
     static __device__ __forceinline__ int unit_of(int i) { return (threadIdx.x + THREADS * i) % kUnits ^ turn(row_of(i)); }
+    static constexpr __device__ int tensor_of(int i) { return PAIR && i >= kLoads / 2; }
 
-    // row_at(r): row r of the tile, clamped to one that is there.  Its summed axis begins at k.
-    template <typename F> __device__ __forceinline__ void begin_rows(int k, F &&row_at) {
+    const unsigned char *base[kTensors];   // of the tile's first row at the step, the same for all lanes
+    uint32_t offset[kLoads];               // of the lane's units from there: rows of fewer than 2^24 bytes
+
+    // Rows first, first + 1, ..., of which there are `rows` (the last stands for those behind it), the summed axis from k on.
+    __device__ __forceinline__ void begin_rows(const Rows *x, int k, int first, int rows) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) at[i] = (const T *)row_at(row_of(i)) + k + unit_of(i) * E;
+        for (int t = 0; t < kTensors; ++t) base[t] = (const unsigned char *)((const T *)x[t].data + first * x[t].stride + k);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            offset[i] = min(row_of(i) % kRows, rows - 1 - first) * (uint32_t)(x[tensor_of(i)].stride * sizeof(T)) + unit_of(i) * 16;
     }
     // Elements from `first` on of rows k, k + 1, ..., which hold `end`, a multiple of E.
     __device__ __forceinline__ void begin_down(const Rows &x, int k, int first, int end) {
+        base[0] = (const unsigned char *)((const T *)x.data + k * x.stride + first);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            at[i] = (const T *)x.data + (int64_t)(k + row_of(i)) * x.stride + min(first + unit_of(i) * E, end - E);
+            offset[i] = row_of(i) * (uint32_t)(x.stride * sizeof(T)) + min(unit_of(i) * E, end - E - first) * (uint32_t)sizeof(T);
     }
     __device__ __forceinline__ void advance(int64_t stride) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) at[i] += DOWN ? kStep * stride : kStep;
+        for (int t = 0; t < kTensors; ++t) base[t] += DOWN ? kStep * stride * (int64_t)sizeof(T) : kStepBytes;
     }
-    // places: how many of the step's places on the summed axis there are; the others become zeros.
+    // Straight into LDS, 16 bytes a lane, one lane's after the other's; waited for by wait_for_stage.  In assembly, as the compiler
+    // would wait for the whole stage before each transposing read of the other one.  places: how many of the step's places on the
+    // summed axis there are; the others become zeros.
     __device__ __forceinline__ void start(unsigned char *stage, int places) const {
+        const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)stage +
+                               __builtin_amdgcn_readfirstlane((threadIdx.x & ~63u) * 16);
+        uint32_t m0;
+        if (places >= kStep) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                             : "=&s"(m0) : "s"(first + THREADS * 16 * i), "v"(offset[i]), "s"(base[tensor_of(i)]) : "memory");
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const void *from = at[i];
-            if (places < kStep && (DOWN ? row_of(i) : unit_of(i) * E) >= places) from = &kZeroUnit;
-            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)stage +
-                                __builtin_amdgcn_readfirstlane((threadIdx.x & ~63u) * 16 + THREADS * 16 * i);
-            // straight into LDS, 16 bytes a lane, one lane's after the other's; waited for by wait_for_stage.  In assembly, as the
-            // compiler would wait for the whole stage before each transposing read of the other one.
-            uint32_t m0;
+            const void *from = base[tensor_of(i)] + offset[i];
+            if ((DOWN ? row_of(i) : unit_of(i) * E) >= places) from = &kZeroUnit;
             asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
-                         : "=&s"(m0) : "s"(to), "v"(from) : "memory");
+                         : "=&s"(m0) : "s"(first + THREADS * 16 * i), "v"(from) : "memory");
         }
-    }
-
-    // The same through registers, for rows at any alignment and of any length (!DOWN).
-    __device__ __forceinline__ void fetch(u4 (&held)[kLoads], int places) const {
-        typedef T vec_t __attribute__((ext_vector_type(E)));
-        typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int left = places - unit_of(i) * E;
-            vec_t v = {};
-            if (left >= E) {
-                v = *(const loose_t *)at[i];
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (e < left) v[e] = at[i][e];
-            }
-            held[i] = __builtin_bit_cast(u4, v);
-        }
-    }
-    __device__ __forceinline__ void keep(const u4 (&held)[kLoads], unsigned char *stage) const {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) *(u4 *)(stage + (threadIdx.x + THREADS * i) * 16) = held[i];
     }
 
     // Where a lane reads: row or element lane % 16 of a group of 16, a quarter of the step's places by lane / 16.
@@ -172,6 +164,47 @@ template <typename T, int N, bool DOWN, int THREADS> struct Operand {
             for (int i = 0; i < 4; ++i) v[i] = *(const uint32_t *)(from + i * N * 4);
             return v;
         }
+    }
+};
+
+// Rows at any alignment, of any length and any distance: through registers into the same places.
+template <typename Operand, typename T> struct LooseRows {
+    static constexpr int kLoads = Operand::kLoads;
+    const T *at[kLoads];
+    u4 held[kLoads];
+
+    __device__ __forceinline__ void begin_rows(const Rows *x, int k, int first, int rows) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const Rows &y = x[Operand::tensor_of(i)];
+            at[i] = (const T *)y.data + min(first + Operand::row_of(i) % Operand::kRows, rows - 1) * y.stride + k + Operand::unit_of(i) * Operand::E;
+        }
+    }
+    __device__ __forceinline__ void advance() {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) at[i] += Operand::kStep;
+    }
+    __device__ __forceinline__ void fetch(int places) {
+        constexpr int E = Operand::E;
+        typedef T vec_t __attribute__((ext_vector_type(E)));
+        typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int left = places - Operand::unit_of(i) * E;
+            vec_t v = {};
+            if (left >= E) {
+                v = *(const loose_t *)at[i];
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e < left) v[e] = at[i][e];
+            }
+            held[i] = __builtin_bit_cast(u4, v);
+        }
+    }
+    __device__ __forceinline__ void keep(unsigned char *stage) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) *(u4 *)(stage + (threadIdx.x + Operand::kThreads * i) * 16) = held[i];
     }
 };
 
@@ -289,8 +322,8 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
     constexpr bool kPair = KIND == ProductKind::kForward || KIND == ProductKind::kGates;
     static_assert(DIRECT || KIND == ProductKind::kForward);
     constexpr int GP = Tile::GP, GQ = Tile::GQ;
-    typedef Operand<T, Tile::P, !kPair, Tile::kThreads> OperandP;
-    typedef Operand<T, Tile::Q, KIND == ProductKind::kGradWeights, Tile::kThreads> OperandQ;
+    typedef Operand<T, Tile::P, !kPair, kPair, Tile::kThreads> OperandP;
+    typedef Operand<T, Tile::Q, KIND == ProductKind::kGradWeights, false, Tile::kThreads> OperandQ;
     constexpr int kStep = OperandP::kStep, kStage = OperandP::kBytes + OperandQ::kBytes;
     __shared__ __align__(256) unsigned char stages[Tile::kLds];
     const ProductWork work = product_work(a);
@@ -300,97 +333,107 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
     const int p0 = work.p * (kPair ? Tile::P / 2 : Tile::P), q0 = work.q * Tile::Q;
     const int first = work.split * a.split_steps, last = min(first + a.split_steps, a.steps);
     const int part_steps = KIND == ProductKind::kGradX ? a.steps / 2 : a.steps;      // kGradX goes through both halves
-
-    OperandP p;
-    OperandQ q;
-    const auto begin = [&](int step) {
-        const int part = KIND == ProductKind::kGradX && step >= part_steps, k = (step - part * part_steps) * kStep;
-        const int half = KIND == ProductKind::kGradX ? part : work.half;
-        if constexpr (kPair) {
-            p.begin_rows(k, [&](int r) {
-                const int h = min(p0 + r % (Tile::P / 2), a.np - 1);
-                const Rows &w = r < Tile::P / 2 ? a.p[0] : a.p[1];
-                return (const T *)w.data + h * w.stride;
-            });
-        } else {
-            const Rows &w = KIND == ProductKind::kGradX ? a.p[part] : a.p[0];
-            p.begin_down(w, k, p0, a.p_units);
-        }
-        const Rows &y = kPair ? a.q[0] : a.q[half];
-        if constexpr (KIND == ProductKind::kGradWeights)
-            q.begin_down(y, k, q0, (int)y.stride);
-        else
-            q.begin_rows(k, [&](int r) { return (const T *)y.data + (int64_t)min(q0 + r, a.nq - 1) * y.stride; });
-    };
-    const auto advance = [&](int step) {                   // to `step`
-        if (KIND == ProductKind::kGradX && step == part_steps) {
-            begin(step);
-            return;
-        }
-        p.advance(KIND == ProductKind::kGradX && step > part_steps ? a.p[1].stride : a.p[0].stride);
-        q.advance(a.q[0].stride);
-    };
     const auto places_of = [&](int step) {
         return a.nk - (KIND == ProductKind::kGradX && step >= part_steps ? step - part_steps : step) * kStep;
     };
 
     f4 acc[GP][GQ] = {};
     const uint32_t base_p = OperandP::lane_base(), base_q = OperandQ::lane_base();
-    const auto multiply = [&](const unsigned char *stage) {
+    // Half h of a step of P, and a half of its rows of Q, in registers.
+    u4 ps[2][GP], qs[2][GQ / 2];
+    const auto read_p = [&](u4 (&x)[GP], const unsigned char *stage, int h) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            u4 ps[GP], qs[GQ];
-#pragma unroll
-            for (int i = 0; i < GP; ++i) {
-                // a pair's wavefront takes the same units of either weight
-                const int g = kPair ? wp * (GP / 2) + i % (GP / 2) + i / (GP / 2) * (Tile::P / 32) : wp * GP + i;
-                ps[i] = OperandP::read(stage, base_p, g, h);
-            }
-#pragma unroll
-            for (int j = 0; j < GQ; ++j) qs[j] = OperandQ::read(stage + OperandP::kBytes, base_q, wq * GQ + j, h);
-#pragma unroll
-            for (int i = 0; i < GP; ++i)
-#pragma unroll
-                for (int j = 0; j < GQ; ++j) acc[i][j] = multiply_units<T>(ps[i], qs[j], acc[i][j]);
+        for (int i = 0; i < GP; ++i) {
+            // a pair's wavefront takes the same units of either weight
+            const int g = kPair ? wp * (GP / 2) + i % (GP / 2) + i / (GP / 2) * (Tile::P / 32) : wp * GP + i;
+            x[i] = OperandP::read(stage, base_p, g, h);
         }
     };
+    const auto read_q = [&](u4 (&x)[GQ / 2], const unsigned char *stage, int h, int part) {
+#pragma unroll
+        for (int j = 0; j < GQ / 2; ++j) x[j] = OperandQ::read(stage + OperandP::kBytes, base_q, wq * GQ + part * (GQ / 2) + j, h);
+    };
+    const auto multiply = [&](const u4 (&p)[GP], const u4 (&q)[GQ / 2], int part) {
+#pragma unroll
+        for (int i = 0; i < GP; ++i)
+#pragma unroll
+            for (int j = 0; j < GQ / 2; ++j) acc[i][part * (GQ / 2) + j] = multiply_units<T>(p[i], q[j], acc[i][part * (GQ / 2) + j]);
+    };
 
-    if (first < last) {
-        begin(first);
-        if constexpr (DIRECT) {
-            p.start(stages, places_of(first));
-            q.start(stages + OperandP::kBytes, places_of(first));
-            for (int step = first; step < last; ++step) {
-                const int stage = (step - first) & 1;
-                wait_for_stage();
-                if (step + 1 < last) {
-                    advance(step + 1);
-                    p.start(stages + (stage ^ 1) * kStage, places_of(step + 1));
-                    q.start(stages + (stage ^ 1) * kStage + OperandP::kBytes, places_of(step + 1));
-                }
-                multiply(stages + stage * kStage);
+    if constexpr (DIRECT) {
+        OperandP p;
+        OperandQ q;
+        const auto begin = [&](int step) {
+            const int part = KIND == ProductKind::kGradX && step >= part_steps, k = (step - part * part_steps) * kStep;
+            if constexpr (kPair) p.begin_rows(a.p, k, p0, a.np);
+            else p.begin_down(a.p[part], k, p0, a.p_units);
+            const Rows &y = a.q[KIND == ProductKind::kGradX ? part : work.half];
+            if constexpr (KIND == ProductKind::kGradWeights) q.begin_down(y, k, q0, (int)y.stride);
+            else q.begin_rows(&y, k, q0, a.nq);
+        };
+        const auto start = [&](int step) {                 // begin(step - 1) or start(step - 1) was before
+            if (KIND == ProductKind::kGradX && step == part_steps && step > first) {
+                begin(step);
+            } else if (step > first) {
+                p.advance(KIND == ProductKind::kGradX && step > part_steps ? a.p[1].stride : a.p[0].stride);
+                q.advance(a.q[0].stride);
             }
-        } else {
-            u4 held_p[OperandP::kLoads], held_q[OperandQ::kLoads];
-            const auto fetch = [&](int step) {
-                p.fetch(held_p, places_of(step));
-                q.fetch(held_q, places_of(step));
-            };
-            fetch(first);
-            p.keep(held_p, stages);
-            q.keep(held_q, stages + OperandP::kBytes);
+            unsigned char *stage = stages + ((step - first) & 1) * kStage;
+            p.start(stage, places_of(step));
+            q.start(stage + OperandP::kBytes, places_of(step));
+        };
+        // A quarter of a step is read while the one before is multiplied.  The barrier lies before the last quarter, all of whose
+        // operands are in registers by then, so that the next step's first reads have products to run under.
+        if (first < last) {
+            begin(first);
+            start(first);
+            wait_for_stage();
+            if (first + 1 < last) start(first + 1);
+            read_p(ps[0], stages, 0);
+            read_q(qs[0], stages, 0, 0);
             for (int step = first; step < last; ++step) {
-                const int stage = (step - first) & 1;
-                __syncthreads();
+                const unsigned char *now = stages + ((step - first) & 1) * kStage, *next = stages + ((step - first + 1) & 1) * kStage;
+                read_q(qs[1], now, 0, 1);
+                multiply(ps[0], qs[0], 0);
+                read_p(ps[1], now, 1);
+                read_q(qs[0], now, 1, 0);
+                multiply(ps[0], qs[1], 1);
+                read_q(qs[1], now, 1, 1);
+                multiply(ps[1], qs[0], 0);
                 if (step + 1 < last) {
-                    advance(step + 1);
-                    fetch(step + 1);
+                    wait_for_stage();
+                    if (step + 2 < last) start(step + 2);
+                    read_p(ps[0], next, 0);
+                    read_q(qs[0], next, 0, 0);
                 }
-                multiply(stages + stage * kStage);
-                if (step + 1 < last) {
-                    p.keep(held_p, stages + (stage ^ 1) * kStage);
-                    q.keep(held_q, stages + (stage ^ 1) * kStage + OperandP::kBytes);
-                }
+                multiply(ps[1], qs[1], 1);
+            }
+        }
+    } else {
+        LooseRows<OperandP, T> p;
+        LooseRows<OperandQ, T> q;
+        p.begin_rows(a.p, 0, p0, a.np);
+        q.begin_rows(a.q, 0, q0, a.nq);
+        p.fetch(places_of(0));
+        q.fetch(places_of(0));
+        for (int step = 0; step < last; ++step) {
+            unsigned char *stage = stages + (step & 1) * kStage;
+            p.keep(stage);
+            q.keep(stage + OperandP::kBytes);
+            __syncthreads();
+            if (step + 1 < last) {
+                p.advance();
+                q.advance();
+                p.fetch(places_of(step + 1));
+                q.fetch(places_of(step + 1));
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                read_p(ps[0], stage, h);
+                read_q(qs[0], stage, h, 0);
+                read_q(qs[1], stage, h, 1);
+                multiply(ps[0], qs[0], 0);
+                multiply(ps[0], qs[1], 1);
             }
         }
     }

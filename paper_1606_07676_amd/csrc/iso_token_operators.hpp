@@ -352,7 +352,10 @@ class GatedBinder {
         const int E = 16 / (int)dtype_size(t.dtype);
         return (t.channels + E - 1) / E * E;
     }
-    bool direct(const iso_rows_t &x) const { return wide(x, t.channels, t.dtype); }
+    // Rows that the products take straight from memory: on 16-byte boundaries, in whole units, fewer than 2^24 bytes apart.
+    bool direct(const iso_rows_t &x) const {
+        return wide(x, t.channels, t.dtype) && x.stride * (int64_t)dtype_size(t.dtype) < (1 << 24);
+    }
 
     // g and u of all tokens, up to out or to d_gate and d_up.
     template <bool BACKWARD> int add_projections(ProductArgs a) {

@@ -17,6 +17,8 @@
 #include "iso_attention_tiles.hpp"
 #include "iso_fastdiv.hpp"
 
+#include <type_traits>
+
 namespace iso {
 
 enum Activation { kSilu = ISO_ACTIVATION_SILU, kGelu = ISO_ACTIVATION_GELU };
@@ -55,7 +57,9 @@ static __device__ const u4 kZeroUnit = {0, 0, 0, 0};
 
 // ---- activations -------------------------------------------------------------
 
-// f(g) = g s and f'(g).  In 16 bits the exponential and the reciprocal are the hardware's, off by 2^-22 or so.
+// f(g) = g s and f'(g).  In 16 bits exponentials and reciprocals are the hardware's, off by 2^-22 or so, and the error function's
+// share is 0.5 erfc(|g| / sqrt 2) = t P(t) exp(-g^2 / 2), t = 1 / (1 + 0.26 |g|), P of degree 8 fitted to the smallest largest
+// relative error, 2.8e-8 for |g| < 14.5, beyond which it is 0 in 32 bits: the exponential serves the derivative as well.
 template <typename T> __device__ __forceinline__ void activate(int activation, float g, float &f, float &slope) {
     if (activation == kSilu) {
         float s;
@@ -64,9 +68,18 @@ template <typename T> __device__ __forceinline__ void activate(int activation, f
         f = g * s;
         slope = fmaf(f, 1.f - s, s);
     } else {
-        const float c = 0.5f * erfcf(-0.70710678118654752440f * g);
+        float c, e;
+        if constexpr (sizeof(T) == 4) {
+            c = 0.5f * erfcf(-0.70710678118654752440f * g);
+            e = expf(-0.5f * g * g);
+        } else {
+            const float t = __builtin_amdgcn_rcpf(fmaf(0.26f, fabsf(g), 1.f));
+            e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * (g * g));
+            const float rest = fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.0302301365f, -0.151493681f), 0.248731736f), -0.147787768f), 0.158757743f), 0.0519652266f), 0.102788585f), 0.103050987f), 0.103757021f) * t * e;
+            c = g < 0.f ? rest : 1.f - rest;
+        }
         f = g * c;
-        slope = fmaf(g * 0.39894228040143267794f, expf(-0.5f * g * g), c);
+        slope = fmaf(g * 0.39894228040143267794f, e, c);
     }
 }
 
@@ -74,15 +87,16 @@ template <typename T> __device__ __forceinline__ void activate(int activation, f
 
 // An operand's tile for one step.  !DOWN: N rows of 128 bytes, the summed axis along the row.  DOWN: one row of N elements for
 // each of the step's places on the summed axis.  16-byte units of a row are permuted by the row (turn), so that lanes that read
-// together find different banks.  PAIR: the rows are those of two tensors, half a tile each.
-template <typename T, int N, bool DOWN, bool PAIR, int THREADS> struct Operand {
+// together find different banks.  PAIR: the rows are those of two tensors, half a tile each.  RUN: of how many groups of 16 a
+// product's lanes take four rows each in turn, so that a lane's results are 4 RUN neighbours (!DOWN).
+template <typename T, int N, bool DOWN, bool PAIR, int RUN, int THREADS> struct Operand {
     static constexpr int E = 16 / sizeof(T), kStep = kStepBytes / sizeof(T), kBytes = N * kStepBytes;
     static constexpr int kLoads = N * 8 / THREADS, kUnits = DOWN ? N / E : 8;       // loads of a lane, units of a row
     static constexpr int kThreads = THREADS, kTensors = PAIR ? 2 : 1, kRows = PAIR ? N / 2 : N;
     static_assert(N * 8 % THREADS == 0 && (!PAIR || kLoads % 2 == 0));
 
     static __device__ __forceinline__ int turn(int row) {
-        if (!DOWN) return row & 7;
+        if (!DOWN) return RUN == 2 ? (row & 3) | (row >> 3 & 1) << 2 : row & 7;
         if (sizeof(T) == 2) return ((row & 3) << 1 | (row >> 3 & 1) << 3) & (kUnits - 1);
         return (row >> 2 & 3) << 2;
     }
@@ -138,17 +152,22 @@ template <typename T, int N, bool DOWN, bool PAIR, int THREADS> struct Operand {
     // Where a lane reads: row or element lane % 16 of a group of 16, a quarter of the step's places by lane / 16.
     static __device__ __forceinline__ uint32_t lane_base() {
         const int lane = threadIdx.x & 63, quarter = lane / 16, within = lane % 16;
-        if (!DOWN) return within * kStepBytes + (quarter ^ (within & 7)) * 16;
+        if (!DOWN) {
+            const int row = within / 4 * 4 * RUN + within % 4;
+            return row * kStepBytes + (quarter ^ turn(row)) * 16;
+        }
         if (sizeof(T) == 2) {
             const int row = 8 * quarter + within / 4;
             return row * N * 2 + (turn(row) ^ (within % 4 / 2)) * 16 + within % 2 * 8;
         }
         return 4 * quarter * N * 4 + ((quarter << 2) ^ (within / 4)) * 16 + within % 4 * 4;
     }
-    // Group g of 16 rows or elements, half `h` of the step: 8 elements of 16 bits, or 4 of 32, of the summed axis.
-    static __device__ __forceinline__ u4 read(const unsigned char *stage, uint32_t base, int g, int h) {
+    // The group of 16 rows or elements that begins at `first`, half `h` of the step: 8 elements of 16 bits, or 4 of 32, of the
+    // summed axis.
+    static __device__ __forceinline__ u4 read(const unsigned char *stage, uint32_t base, int first, int h) {
+        const int g = first / 16;
         if constexpr (!DOWN) {
-            return *(const u4 *)(stage + ((base + g * 16 * kStepBytes) ^ (h * 64)));
+            return *(const u4 *)(stage + ((base + first * kStepBytes) ^ (h * 64)));
         } else if constexpr (sizeof(T) == 2) {
             constexpr int kGroups = kUnits / 2 < 8 ? kUnits / 2 : 8;       // groups of 16 that the permutation mixes
             typedef short s4 __attribute__((ext_vector_type(4)));
@@ -256,64 +275,66 @@ __device__ __forceinline__ ProductWork product_work(const ProductArgs &a) {
 // What was started is in LDS, and all wavefronts have done with the stage before.
 __device__ __forceinline__ void wait_for_stage() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <typename T> struct Quad { typedef T type __attribute__((ext_vector_type(4))); };
-
-// Four consecutive elements of a row, of which `left` are there, at any alignment.
-template <typename T> __device__ __forceinline__ void store_four(T *to, f4 v, int left) {
-    typedef typename Quad<T>::type vec_t;
+// N consecutive elements of a row, of which `left` are there, at any alignment.
+template <typename T, int N> struct Run {
+    typedef T vec_t __attribute__((ext_vector_type(N)));
     typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
-    vec_t y;
+    vec_t v;
+
+    __device__ __forceinline__ void load(const T *from, int left) {
+        v = {};
+        if (left >= N) {
+            v = *(const loose_t *)from;
+        } else {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] = (T)v[r];
-    if (left >= 4) {
-        *(loose_t *)to = y;
-    } else {
-#pragma unroll
-        for (int r = 0; r < 3; ++r)
-            if (r < left) to[r] = y[r];
+            for (int r = 0; r < N - 1; ++r)
+                if (r < left) v[r] = from[r];
+        }
     }
-}
-template <typename T> __device__ __forceinline__ f4 load_four(const T *from, int left) {
-    typedef typename Quad<T>::type vec_t;
-    typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
-    vec_t y = {};
-    if (left >= 4) {
-        y = *(const loose_t *)from;
-    } else {
+    __device__ __forceinline__ void store(T *to, int left) const {
+        if (left >= N) {
+            *(loose_t *)to = v;
+        } else {
 #pragma unroll
-        for (int r = 0; r < 3; ++r)
-            if (r < left) y[r] = from[r];
+            for (int r = 0; r < N - 1; ++r)
+                if (r < left) to[r] = v[r];
+        }
     }
-    return f4{(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+};
+template <typename T> __device__ __forceinline__ void store_four(T *to, f4 x, int left) {
+    Run<T, 4> y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y.v[r] = (T)x[r];
+    y.store(to, left);
 }
 
-// What becomes of four neighbouring hidden units of a token, h to h + 3, from their g and u.
-template <typename T, bool BACKWARD>
-__device__ __forceinline__ void gated_epilogue(const ProductArgs &a, int token, int h, f4 g, f4 u) {
-    f4 first, second;
-    if constexpr (BACKWARD) {
-        // rows of the workspace are whole units of 16 bytes; what is behind the last hidden unit stays out of all sums
-        const f4 dy = load_four((const T *)a.grad_out.data + (int64_t)token * a.grad_out.stride + h, a.np - h);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float f, slope;
-            activate<T>(a.activation, g[r], f, slope);
-            first[r] = h + r < a.np ? dy[r] * u[r] * slope : 0.f;
-            second[r] = h + r < a.np ? dy[r] * f : 0.f;
-        }
-        const int left = (int)a.out[0].stride - h;
-        store_four((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h, first, left);
-        store_four((T *)a.out[1].data + (int64_t)token * a.out[1].stride + h, second, left);
-    } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float f, slope;
-            activate<T>(a.activation, g[r], f, slope);
-            first[r] = f * u[r];
-        }
-        store_four((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h, first, a.np - h);
+// What becomes of neighbouring hidden units of a token, from h on, from their g and u, N / 4 groups of four.
+template <typename T, bool BACKWARD, int N> struct GatedEnd {
+    Run<T, N> dy;
+
+    __device__ __forceinline__ void load(const ProductArgs &a, int token, int h, int left) {
+        if (BACKWARD) dy.load((const T *)a.grad_out.data + (int64_t)token * a.grad_out.stride + h, left);
     }
-}
+    // left: hidden units from h on
+    __device__ __forceinline__ void finish(const ProductArgs &a, int token, int h, int left, const f4 (&g)[N / 4], const f4 (&u)[N / 4]) const {
+        Run<T, N> first, second;
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            float f, slope;
+            activate<T>(a.activation, g[r / 4][r % 4], f, slope);
+            if constexpr (BACKWARD) {
+                // rows of the workspace are whole units of 16 bytes; what is behind the last hidden unit stays out of all sums
+                first.v[r] = (T)(r < left ? (float)dy.v[r] * u[r / 4][r % 4] * slope : 0.f);
+                second.v[r] = (T)(r < left ? (float)dy.v[r] * f : 0.f);
+            } else {
+                first.v[r] = (T)(f * u[r / 4][r % 4]);
+            }
+        }
+        if (BACKWARD) left += (int)a.out[0].stride - a.np;
+        first.store((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h, left);
+        if (BACKWARD) second.store((T *)a.out[1].data + (int64_t)token * a.out[1].stride + h, left);
+    }
+};
 
 // DIRECT: operands lie on 16-byte boundaries in whole units and go straight to LDS.  The backward pass sees to that, with copies
 // in its workspace where need be; the forward pass, which has none, takes other rows through registers.
@@ -322,8 +343,9 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
     constexpr bool kPair = KIND == ProductKind::kForward || KIND == ProductKind::kGates;
     static_assert(DIRECT || KIND == ProductKind::kForward);
     constexpr int GP = Tile::GP, GQ = Tile::GQ;
-    typedef Operand<T, Tile::P, !kPair, kPair, Tile::kThreads> OperandP;
-    typedef Operand<T, Tile::Q, KIND == ProductKind::kGradWeights, false, Tile::kThreads> OperandQ;
+    constexpr int kRun = kPair ? GP / 2 : 1;
+    typedef Operand<T, Tile::P, !kPair, kPair, kRun, Tile::kThreads> OperandP;
+    typedef Operand<T, Tile::Q, KIND == ProductKind::kGradWeights, false, 1, Tile::kThreads> OperandQ;
     constexpr int kStep = OperandP::kStep, kStage = OperandP::kBytes + OperandQ::kBytes;
     __shared__ __align__(256) unsigned char stages[Tile::kLds];
     const ProductWork work = product_work(a);
@@ -345,13 +367,13 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
 #pragma unroll
         for (int i = 0; i < GP; ++i) {
             // a pair's wavefront takes the same units of either weight
-            const int g = kPair ? wp * (GP / 2) + i % (GP / 2) + i / (GP / 2) * (Tile::P / 32) : wp * GP + i;
-            x[i] = OperandP::read(stage, base_p, g, h);
+            const int at = kPair ? wp * kRun * 16 + i % kRun * 4 + i / kRun * (Tile::P / 2) : (wp * GP + i) * 16;
+            x[i] = OperandP::read(stage, base_p, at, h);
         }
     };
     const auto read_q = [&](u4 (&x)[GQ / 2], const unsigned char *stage, int h, int part) {
 #pragma unroll
-        for (int j = 0; j < GQ / 2; ++j) x[j] = OperandQ::read(stage + OperandP::kBytes, base_q, wq * GQ + part * (GQ / 2) + j, h);
+        for (int j = 0; j < GQ / 2; ++j) x[j] = OperandQ::read(stage + OperandP::kBytes, base_q, (wq * GQ + part * (GQ / 2) + j) * 16, h);
     };
     const auto multiply = [&](const u4 (&p)[GP], const u4 (&q)[GQ / 2], int part) {
 #pragma unroll
@@ -438,23 +460,37 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
         }
     }
 
-    // lane: row lane % 16 and elements 4 (lane / 16) + 0..3 of each group
+    if constexpr (kPair) {
+        // lane: row lane % 16 and hidden units 4 kRun (lane / 16) + 0, 1, ... of what the wavefront has; whole tiles without branches,
+        // so that all of grad_out is on its way at once
+        constexpr bool kBackward = KIND == ProductKind::kGates;
+        const int h = p0 + wp * kRun * 16 + lane / 16 * 4 * kRun, row0 = q0 + wq * GQ * 16 + lane % 16;
+        const auto finish = [&](auto whole) {
+            constexpr bool kWhole = decltype(whole)::value;
+            const int left = kWhole ? 4 * kRun : a.np - h;
+            GatedEnd<T, kBackward, 4 * kRun> end[GQ];
 #pragma unroll
-    for (int j = 0; j < GQ; ++j) {
-        const int row = q0 + (wq * GQ + j) * 16 + lane % 16;
-        if (row >= a.nq) continue;
-        if constexpr (kPair) {
-            const int end = KIND == ProductKind::kGates ? (int)a.out[0].stride : a.np;
+            for (int j = 0; j < GQ; ++j)
+                if (kWhole || row0 + j * 16 < a.nq) end[j].load(a, row0 + j * 16, h, left);
 #pragma unroll
-            for (int i = 0; i < GP / 2; ++i) {
-                const int h = p0 + (wp * (GP / 2) + i) * 16 + lane / 16 * 4;
-                if (h < end) gated_epilogue<T, KIND == ProductKind::kGates>(a, row, h, acc[i][j], acc[i + GP / 2][j]);
+            for (int j = 0; j < GQ; ++j) {
+                f4 g[kRun], u[kRun];
+#pragma unroll
+                for (int i = 0; i < kRun; ++i) g[i] = acc[i][j], u[i] = acc[i + kRun][j];
+                if (kWhole || row0 + j * 16 < a.nq) end[j].finish(a, row0 + j * 16, h, left, g, u);
             }
-        } else {
+        };
+        if (p0 + Tile::P / 2 <= a.np && q0 + Tile::Q <= a.nq) finish(std::true_type{});
+        else finish(std::false_type{});
+    } else {
+        // lane: row lane % 16 and elements 4 (lane / 16) + 0..3 of each group
+#pragma unroll
+        for (int j = 0; j < GQ; ++j) {
+            const int row = q0 + (wq * GQ + j) * 16 + lane % 16;
+            if (row >= a.nq) continue;
 #pragma unroll
             for (int i = 0; i < GP; ++i) {
                 const int e = p0 + (wp * GP + i) * 16 + lane / 16 * 4;
-                if (e >= a.np) continue;
                 if (a.splits > 1) {
                     float *to = a.partials + (((uint64_t)work.split * a.halves + work.half) * a.nq + row) * a.np + e;
                     store_four(to, acc[i][j], a.np - e);
@@ -512,7 +548,11 @@ template <typename T> __global__ __launch_bounds__(256) void product_sum_kernel(
     if (slot >= a.slots) return;
     const int there = (int)min(a.slots - slot, (uint64_t)4);
     f4 sum = {};
-    for (uint32_t s = 0; s < a.splits; ++s) sum += load_four(a.partials + s * a.slots + slot, there);
+    for (uint32_t s = 0; s < a.splits; ++s) {
+        Run<float, 4> part;
+        part.load(a.partials + s * a.slots + slot, there);
+        sum += part.v;
+    }
     uint64_t row = slot / a.channels;
     uint32_t e = (uint32_t)(slot - row * a.channels);
     for (int i = 0; i < there; ++i) {
@@ -586,8 +626,11 @@ __global__ __launch_bounds__(512) void gated_few_kernel(const ProductArgs a) {
             gs += sums[((w * NT + t) * 2 + 0) * 64 + lane];
             us += sums[((w * NT + t) * 2 + 1) * 64 + lane];
         }
-        const int token = t * 16 + lane % 16, at = h0 + lane / 16 * 4, end = BACKWARD ? (int)a.out[0].stride : a.np;
-        if (token < a.nq && at < end) gated_epilogue<T, BACKWARD>(a, token, at, gs, us);
+        const int token = t * 16 + lane % 16, at = h0 + lane / 16 * 4;
+        if (token >= a.nq) continue;
+        GatedEnd<T, BACKWARD, 4> end;
+        end.load(a, token, at, a.np - at);
+        end.finish(a, token, at, a.np - at, {gs}, {us});
     }
 }
 

@@ -187,32 +187,52 @@ typedef ProductTile<2, 2, 2, 2> SmallTile;         // 64 x 64, 4
 // How a product is cut up.
 struct ProductPlan {
     int tile;                              // 0 large, 1 middle, 2 small
-    int size;                              // of the tile
     uint64_t p_tiles, q_tiles;
     int steps, splits, split_steps;
 };
 
+// Times in us, of a step of a tile that has its CU for itself, of one among as many as fit beside it, and of a tile's end.
+struct TileTimes {
+    double alone, among, end;
+    int beside;
+};
+
 // np: elements of a result's row (of a pair: hidden units of one weight), nq: its rows, nk: the summed axis.
+//
+// The tile and the parts of the summed axis by the time that they would take: a CU works on its share of the tiles, step by step
+// in the time of one alone or, side by side, of all; the sums of parts are written and read again at 5 TB/s.  Constants are those
+// of 16 and 32 bits on the GPU.  Weights' gradients of 32768 tokens, 1024 channels, 2816 hidden units, bfloat16: large tiles in 2
+// parts 370 and 11 us, in 5 389 together, in 1 715, middle ones in 1 524, small ones in 2 658 and 11; of 200000 tokens, 128
+// channels, 384 hidden units small ones in 1 2300, in 6 384 and 4; grad_x of 300 tokens, 1024 channels, 2816 hidden units large ones
+// in 1 117, small ones in 1 51, in 4 15 and 4.
 inline ProductPlan plan_product(ProductKind kind, int dtype, uint64_t np, uint64_t nq, uint64_t nk) {
-    static constexpr int kSize[3] = {256, 128, 64};
-    const bool pair = kind == ProductKind::kForward || kind == ProductKind::kGates;
+    static constexpr int kSize[3] = {LargeTile::P, MiddleTile::P, SmallTile::P};
+    static constexpr TileTimes kTimes[2][3] = {{{1.40, 1.50, 7.0, 1}, {0.85, 0.51, 2.2, 2}, {0.70, 0.27, 0.7, 5}},
+                                               {{0, 0, 0, 0}, {2.10, 1.88, 3.0, 2}, {0.74, 0.50, 1.0, 5}}};
+    const bool pair = kind == ProductKind::kForward || kind == ProductKind::kGates, single = dtype == ISO_DTYPE_F32;
     const uint64_t halves = kind == ProductKind::kGradWeights ? 2 : 1;
     const int step = kStepBytes / (int)dtype_size(dtype);
-    ProductPlan plan{};
-    for (plan.tile = dtype == ISO_DTYPE_F32 ? 1 : 0;; ++plan.tile) {
-        plan.size = kSize[plan.tile];
-        const uint64_t width = pair ? plan.size / 2 : plan.size;
-        plan.p_tiles = (np + width - 1) / width;
-        plan.q_tiles = (nq + plan.size - 1) / plan.size;
-        if (plan.tile == 2 || plan.p_tiles * plan.q_tiles * halves >= 192) break;
+    const int steps = (int)((nk + step - 1) / step) * (kind == ProductKind::kGradX ? 2 : 1);
+    ProductPlan best{};
+    double best_time = 0;
+    for (int tile = single ? 1 : 0; tile < 3; ++tile) {
+        const uint64_t width = pair ? kSize[tile] / 2 : kSize[tile];
+        ProductPlan plan{tile, (np + width - 1) / width, (nq + kSize[tile] - 1) / kSize[tile], steps, 1, steps};
+        const TileTimes &t = kTimes[single][tile];
+        for (int splits = 1; splits == 1 || (!pair && splits <= std::min(256, steps / 8)); splits += 1 + splits / 8) {
+            plan.split_steps = std::max(1, (steps + splits - 1) / splits);
+            plan.splits = std::max(1, (steps + plan.split_steps - 1) / plan.split_steps);
+            const uint64_t items = plan.p_tiles * plan.q_tiles * halves * plan.splits, share = (items + 255) / 256;
+            double time = plan.split_steps * std::max(t.alone * (double)((share + t.beside - 1) / t.beside), t.among * (double)share) +
+                          t.end * (double)share * (kind == ProductKind::kGates ? 2 : 1);
+            if (plan.splits > 1) time += 5 + 2 * 4e-6 / 5 * (double)plan.splits * (double)(halves * np * nq);
+            if (!best.p_tiles || time < best_time) {
+                best = plan;
+                best_time = time;
+            }
+        }
     }
-    plan.steps = (int)((nk + step - 1) / step) * (kind == ProductKind::kGradX ? 2 : 1);
-    plan.splits = 1;
-    const uint64_t tiles = plan.p_tiles * plan.q_tiles * halves;
-    if (!pair && tiles < 256) plan.splits = (int)std::clamp<uint64_t>(512 / std::max<uint64_t>(1, tiles), 1, std::max(1, plan.steps / 8));
-    plan.split_steps = std::max(1, (plan.steps + plan.splits - 1) / plan.splits);
-    plan.splits = std::max(1, (plan.steps + plan.split_steps - 1) / plan.split_steps);
-    return plan;
+    return best;
 }
 
 template <typename T, ProductKind KIND> const void *product_func(int tile, bool direct) {

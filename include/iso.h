@@ -589,7 +589,7 @@ int iso_layer_norm_backward_workspace_bytes(int64_t n, int heads, int channels, 
  * (rate = 1: residual everywhere).  What is dropped may hold anything.  Element e of [n][channels] in row-major order takes 16
  * bits, the (e % 8)th half word, low halves first, of the block of Philox4x32-10 with the counter (e / 8, seed[1]) and the key
  * seed[0], low words first.  out may be x or residual (same stride).
- * ISO_ERR_TOO_LARGE: n * channels of 2^35 or more. */
+ * ISO_ERR_TOO_LARGE: n * channels of 2^34 or more. */
 typedef struct {
     int32_t dtype, channels;
     int64_t n;

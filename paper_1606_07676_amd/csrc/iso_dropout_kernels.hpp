@@ -43,53 +43,77 @@ __device__ __forceinline__ uint4 philox_block(uint64_t counter, uint64_t more, u
 }
 
 // WIDE: blocks of 8 elements lie on 16-byte boundaries in all tensors, in dense tensors (the last one may not be whole) or in
-// rows of whole blocks.
-template <typename T, bool WIDE> __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a) {
+// rows of whole blocks.  A lane makes one block of numbers; two 16-byte units of float32 are those of a block, and the wavefront
+// hands the numbers round so that its loads and stores stay dense.
+//
+// The tensors' bytes bound it: 32768 x 1024 in bfloat16 with a residual 201 MB in 36 us, 5.5 TB/s, without 134 MB in 20.6; two or
+// four blocks a lane take 37 and 39.
+template <typename T, bool WIDE, bool RESIDUAL> __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a) {
+    constexpr int E = ElementTraits<T>::kPerLane, kUnits = 8 / E;
+    typedef T vec_t __attribute__((ext_vector_type(E)));
     const uint32_t block = (a.first_block + blockIdx.x) * 256u + threadIdx.x;
-    if (block >= a.blocks) return;
-    const uint64_t first = (uint64_t)block * 8;
     const uint64_t key = a.seed[0], more = a.seed[1];
     const T *x = (const T *)a.x, *residual = (const T *)a.residual;
     T *out = (T *)a.out;
-    typedef T vec_t __attribute__((ext_vector_type(8)));
-    typedef vec_t half_aligned_t __attribute__((aligned(16)));
-    const bool whole = WIDE && first + 8 <= a.elements;
-    uint64_t row = 0, at = first;
-    half_aligned_t v = {}, r = {};
-    if (whole) {
-        if (!a.flat) {
-            uint32_t q, rest;
-            fast_divmod(block, a.row_blocks, q, rest);
-            row = q;
-            at = rest * 8ull;
+    const auto dropped_or = [&](float value, uint32_t number) { return number >= a.threshold ? value * a.scale : 0.f; };
+    const uint32_t whole = (uint32_t)(a.elements / 8);
+    if constexpr (WIDE) {
+        // unit i of this lane: the same block, or of the wavefront's 128 units the lane's and the one 64 behind
+        vec_t v[kUnits], r[kUnits];
+        const uint32_t lane = threadIdx.x & 63, first = block - lane;
+        uint32_t row[kUnits];
+        int64_t at[kUnits];
+        bool there[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const uint32_t of = kUnits == 1 ? block : first + 32 * i + lane / 2;
+            uint32_t rest = of;
+            row[i] = 0;
+            if (!a.flat) fast_divmod(of, a.row_blocks, row[i], rest);
+            at[i] = rest * 8ll + (kUnits == 1 ? 0 : lane % 2 * 4);
+            there[i] = of < whole;
+            if (there[i]) {
+                v[i] = *(const vec_t *)(x + row[i] * a.x_stride + at[i]);
+                if (RESIDUAL) r[i] = *(const vec_t *)(residual + row[i] * a.residual_stride + at[i]);
+            }
         }
-        v = *(const half_aligned_t *)(x + row * a.x_stride + at);
-        if (residual) r = *(const half_aligned_t *)(residual + row * a.residual_stride + at);
+        const uint4 bits = philox_block(block, more, key);
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            uint32_t words[E / 2];
+            if constexpr (kUnits == 1) {
+                words[0] = bits.x, words[1] = bits.y, words[2] = bits.z, words[3] = bits.w;
+            } else {
+                const int from = 32 * i + lane / 2;
+                const uint32_t low[2] = {(uint32_t)__shfl(bits.x, from), (uint32_t)__shfl(bits.y, from)};
+                const uint32_t high[2] = {(uint32_t)__shfl(bits.z, from), (uint32_t)__shfl(bits.w, from)};
+                words[0] = lane % 2 ? high[0] : low[0];
+                words[1] = lane % 2 ? high[1] : low[1];
+            }
+            if (!there[i]) continue;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float y = dropped_or((float)v[i][e], e % 2 ? words[e / 2] >> 16 : words[e / 2] & 0xFFFF);
+                v[i][e] = (T)(RESIDUAL ? (float)r[i][e] + y : y);
+            }
+            *(vec_t *)(out + row[i] * a.out_stride + at[i]) = v[i];
+        }
+        if (block != whole) return;                        // what is left of a dense tensor
     }
+    if (block >= a.blocks) return;
     const uint4 bits = philox_block(block, more, key);
     const uint32_t words[4] = {bits.x, bits.y, bits.z, bits.w};
-    const auto kept = [&](float value, int e) {
-        const uint32_t number = e % 2 ? words[e / 2] >> 16 : words[e / 2] & 0xFFFF;
-        return number >= a.threshold ? value * a.scale : 0.f;
-    };
-    if (whole) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = kept((float)v[e], e);
-            v[e] = (T)(residual ? (float)r[e] + y : y);
-        }
-        *(half_aligned_t *)(out + row * a.out_stride + at) = v;
-        return;
-    }
+    const uint64_t begin = (uint64_t)block * 8;
+    uint64_t row = 0, at = begin;
     if (!a.flat) {
-        row = first / a.channels;
-        at = first - row * a.channels;
+        row = begin / a.channels;
+        at = begin - row * a.channels;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (first + e >= a.elements) return;
-        const float y = kept((float)x[row * a.x_stride + at], e);
-        out[row * a.out_stride + at] = (T)(residual ? (float)residual[row * a.residual_stride + at] + y : y);
+        if (begin + e >= a.elements) return;
+        const float y = dropped_or((float)x[row * a.x_stride + at], e % 2 ? words[e / 2] >> 16 : words[e / 2] & 0xFFFF);
+        out[row * a.out_stride + at] = (T)(RESIDUAL ? (float)residual[row * a.residual_stride + at] + y : y);
         if (++at == a.channels && !a.flat) {
             at = 0;
             ++row;

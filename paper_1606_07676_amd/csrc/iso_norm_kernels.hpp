@@ -23,10 +23,10 @@ struct NormArgs {
     const void *weight, *bias;             // [channels] or null
     float *mean, *rstd;                    // [n][heads]; may be null in the forward pass
     float *partials;                       // [workgroups][2][channels]: sums for the weight's and the bias's gradient
-    uint64_t rows;
+    uint64_t rows, step;                   // step: rows that all workgroups have at a time, a multiple of the heads
+    uint64_t token_step;                   // step / heads
     FastDiv heads;
     int32_t channels, units;               // units: of 16 bytes in a row, the last one perhaps not whole
-    int32_t lanes;                         // that share a row: a power of two
     float eps, inverse;                    // inverse: 1 / channels
     uint32_t first_block;
 };
@@ -44,23 +44,19 @@ __device__ __forceinline__ float add_other_32(float x) {
     const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
-// Sums over groups of `lanes` lanes, a power of two up to 64.
-template <int N> __device__ __forceinline__ void sum_over_lanes(float (&x)[N], int lanes) {
+// Sums over the lanes of a row, LANES of them; 0: all of the workgroup's.
+template <int LANES, int N> __device__ __forceinline__ void sum_over_row(float (&x)[N], float (*shared)[16]) {
     const auto all = [&](auto &&step) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = step(x[i]);
     };
-    if (lanes > 1) all([](float v) { return add_moved<0xB1>(v); });       // quads: 1 0 3 2
-    if (lanes > 2) all([](float v) { return add_moved<0x4E>(v); });       // quads: 2 3 0 1
-    if (lanes > 4) all([](float v) { return add_moved<0x141>(v); });      // 8 lanes mirrored
-    if (lanes > 8) all([](float v) { return add_moved<0x140>(v); });      // 16 lanes mirrored
-    if (lanes > 16) all(add_other_16);
-    if (lanes > 32) all(add_other_32);
-}
-// Sums over the lanes of a row.  WHOLE: the row has all of the workgroup's wavefronts.
-template <bool WHOLE, int N> __device__ __forceinline__ void sum_over_row(float (&x)[N], int lanes, float (*shared)[16]) {
-    sum_over_lanes(x, WHOLE ? 64 : lanes);
-    if constexpr (WHOLE) {
+    all([](float v) { return add_moved<0xB1>(v); });                      // quads: 1 0 3 2
+    all([](float v) { return add_moved<0x4E>(v); });                      // quads: 2 3 0 1
+    all([](float v) { return add_moved<0x141>(v); });                     // 8 lanes mirrored
+    if (!LANES || LANES > 8) all([](float v) { return add_moved<0x140>(v); });       // 16 lanes mirrored
+    if (!LANES || LANES > 16) all(add_other_16);
+    if (!LANES || LANES > 32) all(add_other_32);
+    if constexpr (!LANES) {
         const int waves = blockDim.x >> 6;
         __syncthreads();                                               // the sums before these have been read
         if ((threadIdx.x & 63) == 0)
@@ -75,146 +71,167 @@ template <bool WHOLE, int N> __device__ __forceinline__ void sum_over_row(float 
     }
 }
 
-// A lane's units of a row: units lane, lane + lanes, ...  WIDE: rows on 16-byte boundaries in whole units; otherwise units are
-// read and written at any alignment and the elements of the last one singly.
-template <typename T, bool WIDE, int U> struct NormRow {
+// The lane's place, the row that it begins with, and its units of a row: units place, place + lanes, ...  WIDE: rows on 16-byte
+// boundaries in whole units; otherwise units are read and written at any alignment and the elements of the last one singly.
+template <typename T, bool WIDE, int U, int LANES> struct NormLane {
     static constexpr int E = ElementTraits<T>::kPerLane;
     typedef T vec_t __attribute__((ext_vector_type(E)));
     typedef vec_t loose_t __attribute__((aligned(sizeof(T))));
-    vec_t v[U];
+    struct Units {
+        vec_t v[U];
+    };
+    int place, lanes, channels, units;
+    uint64_t row;
 
-    __device__ __forceinline__ void load(const T *row, int lane, const NormArgs &a) {
+    __device__ __forceinline__ explicit NormLane(const NormArgs &a) : channels(a.channels), units(a.units) {
+        lanes = LANES ? LANES : blockDim.x;
+        place = threadIdx.x % lanes;
+        row = (uint64_t)(a.first_block + blockIdx.x) * (LANES ? 256 / LANES : 1) + (LANES ? threadIdx.x / LANES : 0);
+    }
+    __device__ __forceinline__ T *first(const Heads &h, const NormArgs &a) const {
+        uint32_t token, head;
+        fast_divmod((uint32_t)row, a.heads, token, head);
+        return (T *)h.data + (int64_t)token * h.rank_stride + (int64_t)head * h.head_stride;
+    }
+    // f(u, e) for all elements that are there; !WIDE: also for those behind the row's end, which were loaded as zeros
+    template <typename F> __device__ __forceinline__ void each(F &&f) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (!WIDE || place + u * lanes < units) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) f(u, e);
+            }
+    }
+    __device__ __forceinline__ float if_there(int u, int e, float v) const {
+        return WIDE || (place + u * lanes) * E + e < channels ? v : 0.f;
+    }
+    __device__ __forceinline__ void load(Units &x, const T *from) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = lane + u * a.lanes, at = unit * E;
-            v[u] = {};
-            if (WIDE || at + E <= a.channels) {
-                if (unit < a.units) v[u] = WIDE ? *(const vec_t *)(row + at) : *(const loose_t *)(row + at);
-            } else {
+            const int unit = place + u * lanes, at = unit * E;
+            x.v[u] = {};
+            if (WIDE ? unit < units : at + E <= channels) {
+                x.v[u] = WIDE ? *(const vec_t *)(from + at) : *(const loose_t *)(from + at);
+            } else if (!WIDE) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (at + e < a.channels) v[u][e] = row[at + e];
+                    if (at + e < channels) x.v[u][e] = from[at + e];
             }
         }
     }
-    __device__ __forceinline__ void store(T *row, int lane, const NormArgs &a) const {
+    __device__ __forceinline__ void store(const Units &x, T *to) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = lane + u * a.lanes, at = unit * E;
-            if (WIDE || at + E <= a.channels) {
-                if (unit >= a.units) continue;
-                if (WIDE) *(vec_t *)(row + at) = v[u];
-                else *(loose_t *)(row + at) = v[u];
-            } else {
+            const int unit = place + u * lanes, at = unit * E;
+            if (WIDE ? unit < units : at + E <= channels) {
+                if (WIDE) *(vec_t *)(to + at) = x.v[u];
+                else *(loose_t *)(to + at) = x.v[u];
+            } else if (!WIDE) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (at + e < a.channels) row[at + e] = v[u][e];
+                    if (at + e < channels) to[at + e] = x.v[u][e];
             }
         }
     }
-    __device__ __forceinline__ bool there(int u, int e, int lane, const NormArgs &a) const {
-        const int unit = lane + u * a.lanes;
-        return WIDE ? unit < a.units : unit * E + e < a.channels;
+    // weight or bias, `otherwise` where there is none
+    __device__ __forceinline__ void load_or(Units &x, const void *from, float otherwise) const {
+        if (from) {
+            load(x, (const T *)from);
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) x.v[u][e] = (T)otherwise;
     }
 };
-
-template <typename T> __device__ __forceinline__ T *norm_row(const Heads &h, uint64_t row, const NormArgs &a) {
-    uint32_t token, head;
-    fast_divmod((uint32_t)row, a.heads, token, head);
-    return (T *)h.data + token * h.rank_stride + head * h.head_stride;
-}
-
-// Rows of this lane's group: first, first + step, ...
-struct NormRows {
-    int lane;
-    uint64_t first, step;
-};
-template <bool WHOLE> __device__ __forceinline__ NormRows norm_rows(const NormArgs &a) {
-    if (WHOLE) return {(int)threadIdx.x, a.first_block + blockIdx.x, gridDim.x};
-    const uint32_t groups = blockDim.x / a.lanes;
-    return {(int)(threadIdx.x & (a.lanes - 1)), (uint64_t)(a.first_block + blockIdx.x) * groups + threadIdx.x / a.lanes,
-            (uint64_t)gridDim.x * groups};
-}
 
 // The mean is made in two steps: the elements' distances from a first one give what that is off by, so that a row far from zero
 // loses nothing to the rounding of its sum; the variance is that of the distances.
-template <typename T, bool WIDE, int U, bool WHOLE>
-__global__ __launch_bounds__(WHOLE ? 1024 : 256) void layer_norm_kernel(const NormArgs a) {
-    typedef NormRow<T, WIDE, U> Row;
-    constexpr int E = Row::E;
+template <typename T, bool WIDE, int U, int LANES>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void layer_norm_kernel(const NormArgs a) {
+    typedef NormLane<T, WIDE, U, LANES> Lane;
     __shared__ float shared[2][16];
-    const NormRows rows = norm_rows<WHOLE>(a);
-    Row weight, bias, x, next;
-    if (a.weight) weight.load((const T *)a.weight, rows.lane, a);
-    if (a.bias) bias.load((const T *)a.bias, rows.lane, a);
-    if (rows.first < a.rows) next.load(norm_row<T>(a.x, rows.first, a), rows.lane, a);
-    for (uint64_t row = rows.first; row < a.rows; row += rows.step) {
+    const Lane lane(a);
+    typename Lane::Units weight, bias, x, next;
+    if (lane.row >= a.rows) return;                        // all lanes of the row
+    const T *in = lane.first(a.x, a);
+    T *out = lane.first(a.out, a);
+    lane.load_or(weight, a.weight, 1.f);
+    lane.load_or(bias, a.bias, 0.f);
+    lane.load(next, in);
+    for (uint64_t row = lane.row; row < a.rows; row += a.step) {
         x = next;
-        if (row + rows.step < a.rows) next.load(norm_row<T>(a.x, row + rows.step, a), rows.lane, a);
-        float sum[1] = {0.f};
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum[0] += (float)x.v[u][e];
-        sum_over_row<WHOLE>(sum, a.lanes, shared);
+        in += a.token_step * a.x.rank_stride;
+        if (row + a.step < a.rows) lane.load(next, in);
+        float sum[1] = {0.f}, moments[2] = {0.f, 0.f};
+        lane.each([&](int u, int e) { sum[0] += (float)x.v[u][e]; });
+        sum_over_row<LANES>(sum, shared);
         const float start = sum[0] * a.inverse;
-        float d[U][E], moments[2] = {0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                d[u][e] = x.there(u, e, rows.lane, a) ? (float)x.v[u][e] - start : 0.f;
-                moments[0] += d[u][e];
-                moments[1] = fmaf(d[u][e], d[u][e], moments[1]);
-            }
-        sum_over_row<WHOLE>(moments, a.lanes, shared);
+        lane.each([&](int u, int e) {
+            const float d = lane.if_there(u, e, (float)x.v[u][e] - start);
+            moments[0] += d;
+            moments[1] = fmaf(d, d, moments[1]);
+        });
+        sum_over_row<LANES>(moments, shared);
         const float off = moments[0] * a.inverse, var = fmaxf(fmaf(-off, off, moments[1] * a.inverse), 0.f);
         const float rstd = 1.f / sqrtf(var + a.eps);
-        if (rows.lane == 0) {
+        if (lane.place == 0) {
             if (a.mean) a.mean[row] = start + off;
             if (a.rstd) a.rstd[row] = rstd;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float y = (d[u][e] - off) * rstd;
-                if (a.weight) y *= (float)weight.v[u][e];
-                if (a.bias) y += (float)bias.v[u][e];
-                x.v[u][e] = (T)y;
-            }
-        x.store(norm_row<T>(a.out, row, a), rows.lane, a);
+            for (int e = 0; e < Lane::E; ++e)
+                x.v[u][e] = (T)fmaf(((float)x.v[u][e] - start - off) * rstd, (float)weight.v[u][e], (float)bias.v[u][e]);
+        lane.store(x, out);
+        out += a.token_step * a.out.rank_stride;
     }
 }
 
 // SUMS: the weight's and the bias's gradient are asked for.  mean is one rounding off the row's mean; what that is off by is
 // found again, from the same distances, so that rows far from zero give exact products.
-template <typename T, bool WIDE, int U, bool WHOLE, bool SUMS>
-__global__ __launch_bounds__(WHOLE ? 1024 : 256) void layer_norm_backward_kernel(const NormArgs a) {
-    typedef NormRow<T, WIDE, U> Row;
-    constexpr int E = Row::E;
+template <typename T, bool WIDE, int U, int LANES, bool SUMS>
+__global__ __launch_bounds__(LANES ? 256 : 1024, LANES ? 3 : 4) void layer_norm_backward_kernel(const NormArgs a) {
+    typedef NormLane<T, WIDE, U, LANES> Lane;
+    constexpr int E = Lane::E;
+    constexpr bool kAhead = LANES != 0;                                // 16 wavefronts have no registers for another row, nor for weights
     __shared__ float shared[3][16];
     extern __shared__ __align__(16) float wave_sums[];                 // [wavefronts][2][channels] where rows have less than a workgroup
-    const NormRows rows = norm_rows<WHOLE>(a);
-    Row weight, x, dy;
+    const Lane lane(a);
+    typename Lane::Units weight, x, dy, next_x, next_dy;
     float weight_sum[SUMS ? U : 1][SUMS ? E : 1] = {}, bias_sum[SUMS ? U : 1][SUMS ? E : 1] = {};
-    if (a.weight) weight.load((const T *)a.weight, rows.lane, a);
-    for (uint64_t row = rows.first; row < a.rows; row += rows.step) {
-        x.load(norm_row<T>(a.x, row, a), rows.lane, a);
-        dy.load(norm_row<T>(a.grad_out, row, a), rows.lane, a);
-        const float mean = a.mean[row], rstd = a.rstd[row];
+    if (kAhead) lane.load_or(weight, a.weight, 1.f);
+    const T *in = lane.first(a.x, a), *in_dy = lane.first(a.grad_out, a);
+    T *out = lane.first(a.out, a);
+    float next_mean = 0.f, next_rstd = 0.f;
+    const auto load_next = [&](uint64_t row) {
+        lane.load(next_x, in);
+        lane.load(next_dy, in_dy);
+        next_mean = a.mean[row];
+        next_rstd = a.rstd[row];
+    };
+    if (kAhead && lane.row < a.rows) load_next(lane.row);
+    for (uint64_t row = lane.row; row < a.rows; row += a.step) {
+        if (!kAhead) {
+            load_next(row);
+            lane.load_or(weight, a.weight, 1.f);
+        }
+        x = next_x;
+        dy = next_dy;
+        const float mean = next_mean, rstd = next_rstd;
+        in += a.token_step * a.x.rank_stride;
+        in_dy += a.token_step * a.grad_out.rank_stride;
+        if (kAhead && row + a.step < a.rows) load_next(row + a.step);
         float sums[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float d = x.there(u, e, rows.lane, a) ? (float)x.v[u][e] - mean : 0.f;
-                const float g = (float)dy.v[u][e] * (a.weight ? (float)weight.v[u][e] : 1.f);
-                sums[0] += d;
-                sums[1] += g;
-                sums[2] = fmaf(g, d, sums[2]);
-            }
-        sum_over_row<WHOLE>(sums, a.lanes, shared);
+        lane.each([&](int u, int e) {
+            const float d = lane.if_there(u, e, (float)x.v[u][e] - mean), g = (float)dy.v[u][e] * (float)weight.v[u][e];
+            sums[0] += d;
+            sums[1] += g;
+            sums[2] = fmaf(g, d, sums[2]);
+        });
+        sum_over_row<LANES>(sums, shared);
         const float off = sums[0] * a.inverse, mean_g = sums[1] * a.inverse;
         const float mean_gh = (sums[2] - off * sums[1]) * a.inverse * rstd;
 #pragma unroll
@@ -222,40 +239,40 @@ __global__ __launch_bounds__(WHOLE ? 1024 : 256) void layer_norm_backward_kernel
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const float h = ((float)x.v[u][e] - mean - off) * rstd;
-                const float g = (float)dy.v[u][e] * (a.weight ? (float)weight.v[u][e] : 1.f);
+                const float g = (float)dy.v[u][e] * (float)weight.v[u][e];
                 if constexpr (SUMS) {
                     weight_sum[u][e] = fmaf((float)dy.v[u][e], h, weight_sum[u][e]);
                     bias_sum[u][e] += (float)dy.v[u][e];
                 }
-                x.v[u][e] = (T)(rstd * (g - mean_g - h * mean_gh));
+                x.v[u][e] = (T)(rstd * (fmaf(-h, mean_gh, g) - mean_g));
             }
-        x.store(norm_row<T>(a.out, row, a), rows.lane, a);
+        lane.store(x, out);
+        out += a.token_step * a.out.rank_stride;
     }
     if constexpr (SUMS) {
         float *partial = a.partials + (uint64_t)(a.first_block + blockIdx.x) * 2 * a.channels;
         const auto put = [&](float *to) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x.there(u, e, rows.lane, a)) {
-                        const int at = (rows.lane + u * a.lanes) * E + e;
-                        to[at] = weight_sum[u][e];
-                        to[a.channels + at] = bias_sum[u][e];
-                    }
+            lane.each([&](int u, int e) {
+                const int at = (lane.place + u * lane.lanes) * E + e;
+                if (WIDE || at < a.channels) {
+                    to[at] = weight_sum[u][e];
+                    to[a.channels + at] = bias_sum[u][e];
+                }
+            });
         };
-        if constexpr (WHOLE) {
+        if constexpr (!LANES) {
             put(partial);
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    for (int m = a.lanes; m < 64; m *= 2) {            // the wavefront's rows
+#pragma unroll
+                    for (int m = LANES; m < 64; m *= 2) {              // the wavefront's rows
                         weight_sum[u][e] += __shfl_xor(weight_sum[u][e], m);
                         bias_sum[u][e] += __shfl_xor(bias_sum[u][e], m);
                     }
-            if ((int)(threadIdx.x & 63) < a.lanes) put(wave_sums + (threadIdx.x >> 6) * 2 * a.channels);
+            if ((threadIdx.x & 63) < LANES) put(wave_sums + (threadIdx.x >> 6) * 2 * a.channels);
             __syncthreads();
             for (int i = threadIdx.x; i < 2 * a.channels; i += 256) {
                 float s = 0.f;

@@ -48,6 +48,7 @@ struct ProductArgs {
     uint32_t halves;                       // results of a kind: 2 for kGradWeights
     uint32_t items, per_xcd, first_block;
     int32_t activation;
+    int32_t past_caches;                   // kForward: whole tiles of `out` are stored past the caches
 };
 
 constexpr int kBand = 8;
@@ -316,7 +317,7 @@ template <typename T, bool BACKWARD, int N> struct GatedEnd {
         if (BACKWARD) dy.load((const T *)a.grad_out.data + (int64_t)token * a.grad_out.stride + h, left);
     }
     // left: hidden units from h on
-    __device__ __forceinline__ void finish(const ProductArgs &a, int token, int h, int left, const f4 (&g)[N / 4], const f4 (&u)[N / 4]) const {
+    template <bool PAST_CACHES = false> __device__ __forceinline__ void finish(const ProductArgs &a, int token, int h, int left, const f4 (&g)[N / 4], const f4 (&u)[N / 4]) const {
         Run<T, N> first, second;
 #pragma unroll
         for (int r = 0; r < N; ++r) {
@@ -329,6 +330,10 @@ template <typename T, bool BACKWARD, int N> struct GatedEnd {
             } else {
                 first.v[r] = (T)(f * u[r / 4][r % 4]);
             }
+        }
+        if (!BACKWARD && PAST_CACHES) {
+            __builtin_nontemporal_store(first.v, (typename Run<T, N>::loose_t *)((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h));
+            return;
         }
         if (BACKWARD) left += (int)a.out[0].stride - a.np;
         first.store((T *)a.out[0].data + (int64_t)token * a.out[0].stride + h, left);
@@ -474,7 +479,7 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
         // so that all of grad_out is on its way at once
         constexpr bool kBackward = KIND == ProductKind::kGates;
         const int h = p0 + wp * kRun * 16 + lane / 16 * 4 * kRun, row0 = q0 + wq * GQ * 16 + lane % 16;
-        const auto finish = [&](auto whole) {
+        const auto finish = [&](auto whole, auto past_caches) {
             constexpr bool kWhole = decltype(whole)::value;
             const int left = kWhole ? 4 * kRun : a.np - h;
             GatedEnd<T, kBackward, 4 * kRun> end[GQ];
@@ -486,11 +491,12 @@ __global__ __launch_bounds__(Tile::kThreads) void product_kernel(const ProductAr
                 f4 g[kRun], u[kRun];
 #pragma unroll
                 for (int i = 0; i < kRun; ++i) g[i] = acc[i][j], u[i] = acc[i + kRun][j];
-                if (kWhole || row0 + j * 16 < a.nq) end[j].finish(a, row0 + j * 16, h, left, g, u);
+                if (kWhole || row0 + j * 16 < a.nq) end[j].template finish<decltype(past_caches)::value>(a, row0 + j * 16, h, left, g, u);
             }
         };
-        if (p0 + Tile::P / 2 <= a.np && q0 + Tile::Q <= a.nq) finish(std::true_type{});
-        else finish(std::false_type{});
+        if (p0 + Tile::P / 2 > a.np || q0 + Tile::Q > a.nq) finish(std::false_type{}, std::false_type{});
+        else if (!kBackward && a.past_caches) finish(std::true_type{}, std::true_type{});
+        else finish(std::true_type{}, std::false_type{});
     } else {
         // lane: row lane % 16 and elements 4 (lane / 16) + 0..3 of each group
 #pragma unroll

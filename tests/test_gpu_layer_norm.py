@@ -108,7 +108,7 @@ def test_heads_far_apart(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("shape", [(33, 2, 72), (11, 1, 2048)], ids=str)
+@pytest.mark.parametrize("shape", [(33, 2, 72), (11, 1, 2048), (900, 1, 483), (40, 3, 9), (50, 2, 3), (700, 1, 5001)], ids=str)
 def test_in_place(shape, dtype):
     t = tensors(shape, dtype, seed=3)
     out, mean, rstd = forward(t)

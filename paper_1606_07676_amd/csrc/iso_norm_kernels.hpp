@@ -196,8 +196,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void layer_norm_kernel(const No
             moments[1] = fmaf(d, d, moments[1]);
         });
         sum_over_row<LANES>(moments, shared);
-        const float off = moments[0] * a.inverse, var = fmaxf(fmaf(-off, off, moments[1] * a.inverse), 0.f);
-        const float rstd = 1.f / sqrtf(var + a.eps);
+        const float off = moments[0] * a.inverse, var = fmaf(-off, off, moments[1] * a.inverse);
+        const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + a.eps);       // NaN stays
         if (lane.place == 0) {
             if (a.mean) a.mean[row] = start + off;
             if (a.rstd) a.rstd[row] = rstd;

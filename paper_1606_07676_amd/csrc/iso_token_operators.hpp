@@ -50,9 +50,10 @@ inline uint64_t norm_workgroups(const NormShape &s, uint64_t rows, uint64_t head
     const uint64_t need = std::max<uint64_t>(1, (rows + groups - 1) / groups), limit = std::max<uint64_t>(1, most * 256 / s.threads());
     return need <= limit ? (need + unit - 1) / unit * unit : std::max<uint64_t>(1, limit / unit) * unit;
 }
-// Of 256 threads.  Norms with 768, 1536, 2048, 3072, us: 32768 x 1024 in bfloat16 23.1, 22.5, 22.7, 21.9; 70000 x 512 in float32 47.1,
-// 48.5, 47.6, 45.8; 262144 x 10 heads of 128 264, 254, 261, 251.  Gradients of 32768 x 1024 in bfloat16 with 512, 768, 1024 parts, us: 44.0, 45.8, 54.0 (a CU holds 3 workgroups);
-// 37271 x 483 in float16 39.7, 36.0, 44.8; 70000 x 512 in float32 85.8, 86.9, 88.4; 100000 x 16 heads of 64 115.9, 123.9, 127.0.
+// Of 256 threads.  Norms with 768, 1536, 2048, 3072, us: 32768 x 1024 in bfloat16 23.1, 22.5, 22.7, 21.9; 70000 x 512 in float32
+// 47.1, 48.5, 47.6, 45.8; 262144 x 10 heads of 128 264, 254, 261, 251.  Gradients with 512, 768, 1024 parts, before their stores went
+// past the caches, us: 32768 x 1024 in bfloat16 44.0, 45.8, 54.0 (a CU holds 3 workgroups); 37271 x 483 in float16 39.7, 36.0, 44.8;
+// 70000 x 512 in float32 85.8, 86.9, 88.4; 100000 x 16 heads of 64 115.9, 123.9, 127.0.
 constexpr uint64_t kNormWorkgroups = 3072, kNormParts = 512;
 
 inline int check_norm(int64_t n, int heads, int channels, int dtype) {
@@ -319,7 +320,7 @@ inline GatedWorkspace gated_workspace(int64_t n, int channels, int hidden, int d
 inline int check_gated(int64_t n, int channels, int hidden, int dtype) {
     ISO_TRY(check_dtype(dtype));
     if (n < 0 || channels < 1 || hidden < 1) return ISO_ERR_ARG;
-    if (channels > kGatedMaxWidth || hidden > kGatedMaxWidth || n > 0x7FFFFFFF) return ISO_ERR_TOO_LARGE;
+    if (channels > kGatedMaxWidth || hidden > kGatedMaxWidth || n >= 1 << 30) return ISO_ERR_TOO_LARGE;
     return ISO_SUCCESS;
 }
 

@@ -156,6 +156,22 @@ def test_no_tokens(dtype):
     assert not grads["gate"].any() and not grads["up"].any()
 
 
+def test_results_beyond_32_bits_of_bytes():
+    """The last tokens of many, against themselves alone."""
+    n, C, F = 70000, 8, 32776
+    g = torch.Generator(DEV).manual_seed(10)
+    normal = lambda *size: torch.randn(*size, device=DEV, generator=g).to(torch.bfloat16)  # noqa: E731
+    t = {"x": normal(n, C), "gate": normal(F, C), "up": normal(F, C), "dy": torch.empty(n, F, device=DEV, dtype=torch.bfloat16)}
+    out, alone = forward(t, "silu"), dict(t, x=t["x"][-40:], dy=t["dy"][-40:])
+    o = orc.Gated(*(host(alone[k]) for k in ("x", "gate", "up")), "silu", True)
+    within(host(out[-40:]), o.out, o.out_bound(U["bf16"]), "last rows")
+    t["dy"].normal_(generator=g)
+    grads, last = backward(t, "silu"), backward(dict(t, x=t["x"][-40:], dy=t["dy"][-40:]), "silu")
+    o.backward(host(t["dy"][-40:]), U["bf16"])
+    for got in (grads["x"][-40:], last["x"]):
+        near(got, o.grad_x, o.grad_x_error, U["bf16"], "grad_x")
+
+
 def test_another_stream():
     t = tensors(300, 128, 256, "bf16", seed=7)
     want, other = forward(t, "gelu"), torch.cuda.Stream()

@@ -139,6 +139,7 @@ def test_rows_that_are_constant_and_rows_that_are_not_numbers():
     part = {k: v[rows] if v.shape[0] == 12 else v for k, v in t.items()}
     check(part, "f32", out[rows], mean[rows], rstd[rows])
     assert torch.equal(out[3, 0], t["bias"]) and out[7].isnan().all() and out[9].isnan().all()
+    assert rstd[7].isnan().all() and rstd[9].isnan().all()
 
 
 def test_no_rows():
@@ -177,6 +178,17 @@ def test_two_dimensions_stand_for_one_head():
     two = {k: v[:, 0] if v.dim() == 3 else v for k, v in t.items()}
     out2, mean2, rstd2 = forward(two)
     assert torch.equal(out2, out[:, 0]) and mean2.shape == (31,) and torch.equal(mean2, mean[:, 0]) and torch.equal(rstd2, rstd[:, 0])
+
+
+def test_rows_beyond_32_bits_of_elements():
+    """One row repeated, and all rows of the result: the last of 2^32 and more elements."""
+    n, C = 2 ** 19 + 3, 8200
+    x = tensors((1, 1, C), "bf16", seed=13)["x"][0].expand(n, C)
+    out = torch.empty(n, C, device=DEV, dtype=torch.bfloat16)
+    iso.iso_start(iso.iso_layer_norm_init(x, out))
+    o = orc.LayerNorm(host(x[:1]))
+    within(host(out[-1:]), o.out, o.out_bound(U["bf16"]), "last row")
+    assert torch.equal(out[-1], out[0])
 
 
 def test_without_statistics():

@@ -68,7 +68,8 @@ inline uint64_t norm_workspace(int64_t n, int heads, int channels, int dtype) {
 
 template <typename T, bool WIDE, int U, int LANES> const void *norm_kernel(bool backward, bool sums) {
     if (!backward) return (const void *)(layer_norm_kernel<T, WIDE, U, LANES>);
-    return sums ? (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, true>) : (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, false>);
+    return sums ? (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, true>)
+                : (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, false>);
 }
 template <typename T, bool WIDE> const void *norm_kernel(const NormShape &s, bool backward, bool sums) {
     constexpr int kMost = kNormLaneElements * (int)sizeof(T) / 16;

@@ -6,14 +6,9 @@ import torch
 import paper_1606_07676_amd as iso
 from oracle import token_oracle as orc
 from token_rows import DEV, TYPES, U, host, inside_rows, untouched_around, within
+from token_shapes import FEW, LARGE, TILED
 
 pytestmark = pytest.mark.gpu
-
-# tokens, channels, hidden
-FEW = [(1, 1, 1), (1, 64, 16), (1, 136, 40), (5, 33, 17), (16, 256, 48), (17, 100, 31), (32, 512, 24), (37, 520, 90), (64, 1040, 33), (63, 72, 130)]
-TILED = [(65, 8, 8), (65, 1, 3), (70, 64, 64), (129, 130, 65), (100, 200, 300), (200, 72, 132), (333, 65, 127), (257, 264, 72), (65, 700, 513)]
-# enough tiles for the larger ones, with rows and elements left over
-LARGE = [(1500, 136, 1100), (2100, 72, 1928), (3333, 24, 1672)]
 
 
 def tensors(n, C, F, dtype, seed=0):

@@ -8,6 +8,8 @@ import sys
 import numpy as np
 import pytest
 
+from token_shapes import FEW, LARGE, NORMS, TILED
+
 N, C, F, H = 40, 24, 32, 3                # tokens, channels, hidden units, heads
 SIZE = {0: 4, 1: 2, 2: 2}
 
@@ -339,3 +341,66 @@ def test_binding_refuses(ops):
             bad()
     with pytest.raises(TypeError):
         iso.iso_dropout_init(x.double(), x.double(), torch.zeros(2, dtype=torch.int64), 0.1)
+
+
+def test_gpu_tests_take_every_kernel_of_the_projections(ops):
+    taken = set()
+    for shape in FEW + TILED + LARGE:
+        for dtype in (0, 1, 2):
+            o = Operands(ops.stub)
+            t, g, h = o.gated(*shape, dtype), o.gated_grads(*shape, dtype), ctypes.c_void_p()
+            need = o.bytes_of("iso_gated_backward_workspace_bytes", *shape, dtype)
+            work = o.alloc(need)
+            for call, args in (("iso_gated_init", (ctypes.byref(t),)), ("iso_gated_backward_init", (ctypes.byref(t), ctypes.byref(g), work, need))):
+                assert getattr(o.lib, call)(*args, ctypes.byref(h)) == 0
+                ops.stub.lib.stub_log_clear()
+                assert o.lib.iso_start(h, None) == 0
+                for i in range(ops.stub.lib.stub_log_size()):
+                    name = ops.stub.lib.stub_log_name(i).decode()
+                    m = re.search(r"\d(product|gated_few|align_rows|product_sum)_kernelI(f|DF16b|DF16_)", name)
+                    numbers = re.search(r"ProductKindE(\d)ENS_\d+ProductTileILi(\d)ELi\dELi(\d)ELi\dEEELb(\d)", name)
+                    few = re.search(r"Li(\d)ELb(\d)ELb(\d)", name)
+                    taken.add((m[1], m[2], *(numbers.groups() if m[1] == "product" else few.groups() if m[1] == "gated_few" else ())))
+                assert o.lib.iso_request_free(ctypes.byref(h)) == 0
+            o.free()
+    large, middle, small = ("4", "4"), ("2", "4"), ("2", "2")
+    want = set()
+    for dtype, tiles in (("f", (middle, small)), ("DF16b", (large, middle, small)), ("DF16_", (large, middle, small))):
+        want |= {("align_rows", dtype), ("product_sum", dtype)}
+        want |= {("product", dtype, kind, *tile, "1") for kind in "0123" for tile in tiles}
+        want |= {("product", dtype, "0", *tile, "0") for tile in tiles}
+        want |= {("gated_few", dtype, groups, backward, direct) for groups in "124" for backward in "01" for direct in "01"}
+    assert taken == want, (want - taken, taken - want)
+
+
+def test_gpu_tests_take_every_kernel_of_the_norm(ops):
+    taken = set()
+    for n, heads, channels in NORMS:
+        for dtype in (0, 1, 2):
+            o, h = Operands(ops.stub), ctypes.c_void_p()
+            rows = lambda: o.b.iso_heads_t(o.alloc(n * heads * channels * SIZE[dtype]), heads * channels, channels)       # noqa: E731
+            t = o.b.iso_layer_norm_t(dtype=dtype, heads=heads, channels=channels, n=n, eps=1e-5, x=rows(), out=rows())
+            t.weight, t.bias = o.alloc(channels * 4), o.alloc(channels * 4)
+            t.mean, t.rstd = o.alloc(n * heads * 4), o.alloc(n * heads * 4)
+            need = o.bytes_of("iso_layer_norm_backward_workspace_bytes", n, heads, channels, dtype)
+            g = [o.b.iso_layer_norm_grads_t(rows(), rows(), *sums) for sums in ((o.alloc(channels * 4), o.alloc(channels * 4)), (None, None))]
+            work = o.alloc(need)
+            for call, args in (("iso_layer_norm_init", (ctypes.byref(t),)),
+                               ("iso_layer_norm_backward_init", (ctypes.byref(t), ctypes.byref(g[0]), work, need)),
+                               ("iso_layer_norm_backward_init", (ctypes.byref(t), ctypes.byref(g[1]), None, 0))):
+                assert getattr(o.lib, call)(*args, ctypes.byref(h)) == 0
+                ops.stub.lib.stub_log_clear()
+                assert o.lib.iso_start(h, None) == 0
+                for i in range(ops.stub.lib.stub_log_size()):
+                    m = re.search(r"\d(layer_norm\w*?)_kernelI(f|DF16b|DF16_)(?:Lb(\d)ELi(\d)ELi(\d+)E(?:Lb(\d))?)?", ops.stub.lib.stub_log_name(i).decode())
+                    taken.add(tuple(v for v in m.groups() if v is not None))
+                assert o.lib.iso_request_free(ctypes.byref(h)) == 0
+            o.free()
+    want = set()
+    for dtype, most in (("f", "4"), ("DF16b", "2"), ("DF16_", "2")):
+        want.add(("layer_norm_sum", dtype))
+        for wide in "01":
+            for units, lanes in {("1", "8"), ("2", "8"), (most, "8"), (most, "16"), (most, "32"), (most, "64"), (most, "0")}:
+                want.add(("layer_norm", dtype, wide, units, lanes))
+                want |= {("layer_norm_backward", dtype, wide, units, lanes, sums) for sums in "01"}
+    assert taken == want, (want - taken, taken - want)

@@ -603,7 +603,8 @@ int iso_dropout_init(const iso_dropout_t *dropout, iso_request_t *req);
 /* The gated projections of a feed-forward block:
  *     out = f(x . gate) * (x . up)    f(g) = g / (1 + exp(-g))  or  g * (1 + erf(g / sqrt 2)) / 2
  * The backward pass makes x . gate and x . up again, and keeps the gradients of both, rounded to the tensors' type, in its
- * workspace: grad_x and the weights' gradients are products of those.
+ * workspace: grad_x and the weights' gradients are products of those.  In float16 it keeps those below 1/2 scaled as well, so that small
+ * ones lose no more to that rounding than others do; those of 65520 and more become infinite.
  * ISO_ERR_TOO_LARGE: channels or hidden > 2^20, n of 2^30 or more. */
 enum iso_activation {
     ISO_ACTIVATION_SILU = 0,

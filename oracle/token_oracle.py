@@ -9,9 +9,10 @@ EPS = 2.0 ** -24
 TINY = {2.0 ** -24: 2.0 ** -126, 2.0 ** -9: 2.0 ** -126, 2.0 ** -8: 2.0 ** -126, 2.0 ** -11: 2.0 ** -25}
 
 
-def rounded(value, error, u):
-    """Bound after rounding value +- error to elements with unit roundoff u; f16 rounds what is below 2^-14 by up to 2^-25."""
-    return error + u * (np.abs(value) + error) + TINY[u]
+def rounded(value, error, u, tiny=None):
+    """Bound after rounding value +- error to elements with unit roundoff u; f16 rounds what is below 2^-14 by up to 2^-25.
+    tiny: by how much instead, for elements that are kept scaled."""
+    return error + u * (np.abs(value) + error) + (TINY[u] if tiny is None else tiny)
 
 
 class LayerNorm:
@@ -103,11 +104,11 @@ class Gated:
     def out_bound(self, u):
         return rounded(self.out, self.f_error * (np.abs(self.u) + self.u_error) + np.abs(self.f) * self.u_error + 2 * EPS * np.abs(self.out), u)
 
-    def backward(self, dy, u):
-        """u: of the tensors' type, to which the gradients of g and u are rounded on the way."""
+    def backward(self, dy, u, tiny=None):
+        """u: of the tensors' type, to which the gradients of g and u are rounded on the way; tiny: as for rounded."""
         self.d_gate, self.d_up = dy * self.u * self.slope, dy * self.f
-        e_gate = rounded(self.d_gate, np.abs(dy) * (self.u_error * (np.abs(self.slope) + self.slope_error) + np.abs(self.u) * self.slope_error) + 2 * EPS * np.abs(self.d_gate), u)
-        e_up = rounded(self.d_up, np.abs(dy) * self.f_error + EPS * np.abs(self.d_up), u)
+        e_gate = rounded(self.d_gate, np.abs(dy) * (self.u_error * (np.abs(self.slope) + self.slope_error) + np.abs(self.u) * self.slope_error) + 2 * EPS * np.abs(self.d_gate), u, tiny)
+        e_up = rounded(self.d_up, np.abs(dy) * self.f_error + EPS * np.abs(self.d_up), u, tiny)
         a, b = np.abs(self.d_gate) + e_gate, np.abs(self.d_up) + e_up
         sums = lambda n: EPS * (n + 18)  # noqa: E731  terms, and the splits of a sum
         F, n = self.gate.shape[0], self.x.shape[0]

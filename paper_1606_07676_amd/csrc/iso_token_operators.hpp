@@ -294,11 +294,12 @@ template <bool BACKWARD> const void *few_func(int dtype, int groups, bool direct
 
 inline int64_t whole_units(int elements) { return (elements + 7) / 8 * 8; }
 
-// Offsets, each a multiple of 256 bytes: d_gate and d_up of all tokens, copies of x, gate and up with aligned rows where theirs are
-// not, the sums of splits.
+// Offsets, each a multiple of 256 bytes: d_gate and d_up of all tokens, in float16 each row followed by its scaled copy, and the marks
+// of which to take; copies of x, gate and up with aligned rows where theirs are not, the sums of splits.
 struct GatedWorkspace {
-    uint64_t d_gate = 0, d_up = 0, copies[3] = {}, partials = 0, bytes = 0;
+    uint64_t d_gate = 0, d_up = 0, marks = 0, copies[3] = {}, partials = 0, bytes = 0;
 };
+constexpr int kMarkUnits = 16;             // hidden units of a mark at least
 inline GatedWorkspace gated_workspace(int64_t n, int channels, int hidden, int dtype) {
     GatedWorkspace w;
     const auto take = [&](uint64_t rows, int width) {
@@ -306,8 +307,11 @@ inline GatedWorkspace gated_workspace(int64_t n, int channels, int hidden, int d
         w.bytes += (rows * whole_units(width) * dtype_size(dtype) + 255) / 256 * 256;
         return at;
     };
-    w.d_gate = take(n, hidden);
-    w.d_up = take(n, hidden);
+    const uint64_t kept = dtype == ISO_DTYPE_F16 ? 2 : 1;
+    w.d_gate = take(kept * n, hidden);
+    w.d_up = take(kept * n, hidden);
+    w.marks = w.bytes;
+    if (dtype == ISO_DTYPE_F16) w.bytes += ((uint64_t)(n + 15) / 16 * ((hidden + kMarkUnits - 1) / kMarkUnits) * 4 + 255) / 256 * 256;
     w.copies[0] = take(n, channels);
     w.copies[1] = take(n ? hidden : 0, channels);
     w.copies[2] = take(n ? hidden : 0, channels);
@@ -463,17 +467,23 @@ class GatedBinder {
     }
 
     int backward(char *workspace) {
-        const int64_t padded = whole_units(t.hidden);
-        const Rows d_gate{workspace + work.d_gate, padded}, d_up{workspace + work.d_up, padded};
+        const int64_t padded = whole_units(t.hidden), stride = t.dtype == ISO_DTYPE_F16 ? 2 * padded : padded;
+        const Rows d_gate{workspace + work.d_gate, stride}, d_up{workspace + work.d_up, stride};
         void *partials = workspace + work.partials;
+        ProductArgs kept{};
+        kept.d_width = (int32_t)padded;
+        kept.marks = (uint32_t *)(workspace + work.marks);
+        // the hidden units that a wavefront of the kernel up to d_gate and d_up has, one set of 16 or two
+        kept.marks_block = t.n <= kFewTokens || plan_product(ProductKind::kGates, t.dtype, t.hidden, t.n, t.channels).tile == 2 ? 16 : 32;
+        kept.marks_row = (t.hidden + kept.marks_block - 1) / kept.marks_block;
         if (t.n) {
             ISO_TRY(align_rows(workspace));
-            ProductArgs a{};
+            ProductArgs a = kept;
             a.out[0] = d_gate;
             a.out[1] = d_up;
             a.grad_out = device_rows(g->grad_out);
             ISO_TRY(add_projections<true>(a));
-            a = ProductArgs{};
+            a = kept;
             a.p[0] = gate;
             a.p[1] = up;
             a.q[0] = d_gate;
@@ -485,7 +495,7 @@ class GatedBinder {
             a.nk = t.hidden;
             ISO_TRY(add_product(ProductKind::kGradX, product_func<ProductKind::kGradX>, true, a, partials));
         }
-        ProductArgs a{};
+        ProductArgs a = kept;
         a.p[0] = x;
         a.q[0] = d_gate;
         a.q[1] = d_up;

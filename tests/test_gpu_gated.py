@@ -185,3 +185,76 @@ def test_gradient_against_differences(n):
                                            "gelu", False).out * dy).sum())
         change = (value(1e-6) - value(-1e-6)) / 2e-6
         assert abs(change - float((host(grads[name]) * direction).sum())) < 1e-5 * np.abs(host(grads[name]) * direction).sum() + 1e-6, name
+
+
+# Gradients of x . gate and x . up that float16 holds with fewer bits, or not at all, unscaled.  Of those below 1/2 the products
+# take copies times 2^16, which are rounded by at most 2^-25 / 2^16.
+SCALED = 2.0 ** -41
+SMALL = [(1, 64, 40), (30, 64, 48), (61, 72, 130), (65, 8, 8), (333, 65, 127), (2048, 64, 64), (1320, 120, 343), (5000, 200, 1500), (4096, 2040, 100),
+         (12000, 1048, 264)]
+
+
+def rms(x, axis=None):
+    return np.sqrt(np.mean(x ** 2, axis))
+
+
+def small_bound(want, axis=None):
+    """Of a gradient's error, together: the roundings of the result and of what it is a sum of as in `near`, and the result's own
+    absolute rounding, at most 2^-25 an element."""
+    return (3 * U["f16"] * (2 / 3) ** 0.5 + 64 * orc.EPS) * rms(want, axis) + 2.0 ** -25
+
+
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+@pytest.mark.parametrize("scale", [1e-3, 1e-5, 1e-6])
+@pytest.mark.parametrize("shape", SMALL, ids=str)
+def test_small_gradients_in_float16(shape, scale, activation):
+    t = tensors(*shape, "f16", seed=11)
+    t["dy"] = (t["dy"].float() * scale).to(torch.float16)
+    o = orc.Gated(*(host(t[k]) for k in ("x", "gate", "up")), activation, True)
+    o.backward(host(t["dy"]), U["f16"], SCALED)
+    assert max(np.abs(o.d_gate).max(), np.abs(o.d_up).max()) < 0.49
+    grads = backward(t, activation)
+    for got, want, error, what in ((grads["x"], o.grad_x, o.grad_x_error, "grad_x"), (grads["gate"], o.grad_gate, o.grad_gate_error, "grad_gate"),
+                                   (grads["up"], o.grad_up, o.grad_up_error, "grad_up")):
+        within(host(got), want, orc.rounded(want, error, U["f16"]), what)
+        assert rms(host(got) - want) <= small_bound(want), what
+
+
+@pytest.mark.parametrize("shape", [(48, 16, 1024), (700, 16, 1024), (3000, 72, 2048)], ids=str)
+def test_tokens_with_small_gradients_beside_others_in_float16(shape):
+    """A token's grad_x is as exact as its own gradients allow, whatever the tokens beside it hold."""
+    t = tensors(*shape, "f16", seed=12)
+    t["gate"], t["up"] = t["gate"] * 4, t["up"] * 4
+    small = torch.arange(shape[0], device=DEV) % 3 != 0
+    t["dy"][small] = (t["dy"][small].float() * 1e-6).to(torch.float16)
+    o = orc.Gated(*(host(t[k]) for k in ("x", "gate", "up")), "silu", True)
+    o.backward(host(t["dy"]), U["f16"], SCALED)
+    small = small.cpu().numpy()
+    assert max(np.abs(o.d_gate[small]).max(), np.abs(o.d_up[small]).max()) < 0.49 < np.abs(o.d_gate[~small]).max()
+    grads = backward(t, "silu")
+    got, error = host(grads["x"]), orc.rounded(o.grad_x, o.grad_x_error, U["f16"])
+    within(got[small], o.grad_x[small], error[small], "small tokens")
+    assert rms(got[small] - o.grad_x[small]) <= small_bound(o.grad_x[small])
+    # the others, and the sums over all tokens, with whole numbers' rounding below 2^-14
+    o.backward(host(t["dy"]), U["f16"])
+    check(t, "f16", "silu", forward(t, "silu"), grads)
+
+
+@pytest.mark.parametrize("shape", [(48, 64, 96), (700, 64, 192), (5000, 200, 1024)], ids=str)
+def test_hidden_units_with_small_gradients_beside_others_in_float16(shape):
+    """Rows of grad_gate are as exact as their own block of hidden units allows, whatever other blocks hold; grad_up likewise."""
+    t = tensors(*shape, "f16", seed=13)
+    F = shape[2]
+    t["up"][:F // 3] *= 1e-4                               # small d_gate
+    t["gate"][2 * F // 3:] *= 1e-4                         # small d_up
+    t["dy"] = (t["dy"].float() * 0.01).to(torch.float16)
+    t["dy"][0] *= 1000                                     # one token whose gradients are not
+    o = orc.Gated(*(host(t[k]) for k in ("x", "gate", "up")), "gelu", True)
+    o.backward(host(t["dy"]), U["f16"], SCALED)
+    grads = backward(t, "gelu")
+    a, b = F // 96 * 32, (2 * F // 3 + 31) // 32 * 32      # whole blocks of 32
+    assert np.abs(o.d_gate[:, :a]).max() < 0.49 < np.abs(o.d_gate[:, a:]).max() and np.abs(o.d_up[:, b:]).max() < 0.49 < np.abs(o.d_up[:, :b]).max()
+    for got, want, error, rows in ((grads["gate"], o.grad_gate, o.grad_gate_error, slice(0, a)), (grads["up"], o.grad_up, o.grad_up_error, slice(b, F))):
+        within(host(got)[rows], want[rows], orc.rounded(want, error, U["f16"])[rows], "small rows")
+        assert rms(host(got)[rows] - want[rows]) <= small_bound(want[rows])
+    check(t, "f16", "gelu", forward(t, "gelu"), grads)

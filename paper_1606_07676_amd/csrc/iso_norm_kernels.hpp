@@ -27,7 +27,7 @@ struct NormArgs {
     const void *weight, *bias;             // [channels] or null
     float *mean, *rstd;                    // [n][heads]; may be null in the forward pass
     float *partials;                       // [workgroups][2][channels]: sums for the weight's and the bias's gradient
-    uint64_t rows, step;                   // step: rows that all workgroups have at a time, a multiple of the heads
+    uint64_t rows, step;                   // step: rows that all workgroups have at a time, a multiple of the heads but where noted
     uint64_t token_step;                   // step / heads
     FastDiv heads;
     int32_t channels, units;               // units: of 16 bytes in a row, the last one perhaps not whole
@@ -93,7 +93,8 @@ template <typename T, bool WIDE, int U, int LANES> struct NormLane {
         place = threadIdx.x % lanes;
         row = (uint64_t)(a.first_block + blockIdx.x) * (LANES ? 256 / LANES : 1) + (LANES ? threadIdx.x / LANES : 0);
     }
-    __device__ __forceinline__ T *first(const Heads &h, const NormArgs &a) const {
+    __device__ __forceinline__ T *first(const Heads &h, const NormArgs &a) const { return at_row(h, a, row); }
+    static __device__ __forceinline__ T *at_row(const Heads &h, const NormArgs &a, uint64_t row) {
         uint32_t token, head;
         fast_divmod((uint32_t)row, a.heads, token, head);
         return (T *)h.data + (int64_t)token * h.rank_stride + (int64_t)head * h.head_stride;
@@ -213,9 +214,11 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void layer_norm_kernel(const No
 }
 
 // SUMS: the weight's and the bias's gradient are asked for.  mean is one rounding off the row's mean; what that is off by is
-// found again, from the same distances, so that rows far from zero give exact products.
-template <typename T, bool WIDE, int U, int LANES, bool SUMS>
-__global__ __launch_bounds__(LANES ? 256 : 1024, LANES ? 3 : 4) void layer_norm_backward_kernel(const NormArgs a) {
+// found again, from the same distances, so that rows far from zero give exact products.  MOVES: the step is no multiple of the
+// heads, so that lanes come to other heads from row to row (at the price of registers; each workgroup leaves a partial sum, of which
+// there should be no more for more heads).
+template <typename T, bool WIDE, int U, int LANES, bool SUMS, bool MOVES>
+__global__ __launch_bounds__(LANES ? 256 : 1024, LANES ? MOVES ? 2 : 3 : 4) void layer_norm_backward_kernel(const NormArgs a) {
     typedef NormLane<T, WIDE, U, LANES> Lane;
     constexpr int E = Lane::E;
     constexpr bool kAhead = LANES != 0;                                // 16 wavefronts have no registers for another row, nor for weights
@@ -228,6 +231,10 @@ __global__ __launch_bounds__(LANES ? 256 : 1024, LANES ? 3 : 4) void layer_norm_
     const T *in = lane.first(a.x, a), *in_dy = lane.first(a.grad_out, a);
     T *out = lane.first(a.out, a);
     float next_mean = 0.f, next_rstd = 0.f;
+    const auto advance = [&](auto *&now, const Heads &h, uint64_t row) {       // to `row`, which may be behind the last one
+        if (MOVES) now = Lane::at_row(h, a, row);
+        else now += a.token_step * h.rank_stride;
+    };
     const auto load_next = [&](uint64_t row) {
         lane.load(next_x, in);
         lane.load(next_dy, in_dy);
@@ -243,8 +250,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024, LANES ? 3 : 4) void layer_norm_
         x = next_x;
         dy = next_dy;
         const float mean = next_mean, rstd = next_rstd;
-        in += a.token_step * a.x.rank_stride;
-        in_dy += a.token_step * a.grad_out.rank_stride;
+        advance(in, a.x, row + a.step);
+        advance(in_dy, a.grad_out, row + a.step);
         if (kAhead && row + a.step < a.rows) load_next(row + a.step);
         float sums[3] = {0.f, 0.f, 0.f};
         lane.each([&](int u, int e) {
@@ -270,7 +277,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024, LANES ? 3 : 4) void layer_norm_
                 x.v[u][e] = (T)(rstd * (fmaf(-h, mean_gh, g) - mean_g));
             }
         lane.store(x, out, a.past_caches);
-        out += a.token_step * a.out.rank_stride;
+        advance(out, a.out, row + a.step);
     }
     if constexpr (SUMS) {
         float *partial = a.partials + (uint64_t)(a.first_block + blockIdx.x) * 2 * a.channels;

@@ -44,17 +44,26 @@ inline NormShape norm_shape(int channels, int dtype) {
     s.whole = s.lanes > 64;
     return s;
 }
-// Workgroups of 256 threads at most `most`; all of them together take whole tokens' rows at a time, so that a lane keeps its head.
+// Workgroups that together take whole tokens' rows at a time, so that a lane keeps its head: as many as have the threads of `most`
+// of 256 at most, but those of one token's rows at least.
+inline uint64_t norm_unit(const NormShape &s, uint64_t heads) { return heads / std::gcd(heads, s.groups()); }
+inline uint64_t norm_need(const NormShape &s, uint64_t rows) { return std::max<uint64_t>(1, (rows + s.groups() - 1) / s.groups()); }
+inline uint64_t norm_limit(const NormShape &s, uint64_t most) { return std::max<uint64_t>(1, most * 256 / s.threads()); }
 inline uint64_t norm_workgroups(const NormShape &s, uint64_t rows, uint64_t heads, uint64_t most) {
-    const uint64_t groups = s.groups(), unit = heads / std::gcd(heads, groups);
-    const uint64_t need = std::max<uint64_t>(1, (rows + groups - 1) / groups), limit = std::max<uint64_t>(1, most * 256 / s.threads());
-    return need <= limit ? (need + unit - 1) / unit * unit : std::max<uint64_t>(1, limit / unit) * unit;
+    const uint64_t unit = norm_unit(s, heads);
+    return std::min((norm_need(s, rows) + unit - 1) / unit, std::max<uint64_t>(1, norm_limit(s, most) / unit)) * unit;
 }
 // Of 256 threads.  Norms with 768, 1536, 2048, 3072, us: 32768 x 1024 in bfloat16 23.1, 22.5, 22.7, 21.9; 70000 x 512 in float32
 // 47.1, 48.5, 47.6, 45.8; 262144 x 10 heads of 128 264, 254, 261, 251.  Gradients with 512, 768, 1024 parts, before their stores went
 // past the caches, us: 32768 x 1024 in bfloat16 44.0, 45.8, 54.0 (a CU holds 3 workgroups); 37271 x 483 in float16 39.7, 36.0, 44.8;
 // 70000 x 512 in float32 85.8, 86.9, 88.4; 100000 x 16 heads of 64 115.9, 123.9, 127.0.
 constexpr uint64_t kNormWorkgroups = 3072, kNormParts = 512;
+// Workgroups of a gradient that sums over rows, each of which leaves a part of the sums.  Where one token's rows take more than the
+// limit, lanes move from head to head instead: 64 x 4099 heads of 128 in bfloat16 39.0 us with 512 parts, with 4099 59.7.
+inline bool norm_moves(const NormShape &s, uint64_t heads) { return norm_unit(s, heads) > norm_limit(s, kNormParts); }
+inline uint64_t norm_parts(const NormShape &s, uint64_t rows, uint64_t heads) {
+    return norm_moves(s, heads) ? std::min(norm_need(s, rows), norm_limit(s, kNormParts)) : norm_workgroups(s, rows, heads, kNormParts);
+}
 
 inline int check_norm(int64_t n, int heads, int channels, int dtype) {
     ISO_TRY(check_dtype(dtype));
@@ -63,32 +72,36 @@ inline int check_norm(int64_t n, int heads, int channels, int dtype) {
     return ISO_SUCCESS;
 }
 inline uint64_t norm_workspace(int64_t n, int heads, int channels, int dtype) {
-    return norm_workgroups(norm_shape(channels, dtype), (uint64_t)n * heads, heads, kNormParts) * 2 * channels * 4;
+    return norm_parts(norm_shape(channels, dtype), (uint64_t)n * heads, heads) * 2 * channels * 4;
 }
 
-template <typename T, bool WIDE, int U, int LANES> const void *norm_kernel(bool backward, bool sums) {
-    if (!backward) return (const void *)(layer_norm_kernel<T, WIDE, U, LANES>);
-    return sums ? (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, true>)
-                : (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, false>);
-}
-template <typename T, bool WIDE> const void *norm_kernel(const NormShape &s, bool backward, bool sums) {
-    constexpr int kMost = kNormLaneElements * (int)sizeof(T) / 16;
-    if (s.whole) return norm_kernel<T, WIDE, kMost, 0>(backward, sums);
-    switch (s.lanes) {
-        case 64: return norm_kernel<T, WIDE, kMost, 64>(backward, sums);
-        case 32: return norm_kernel<T, WIDE, kMost, 32>(backward, sums);
-        case 16: return norm_kernel<T, WIDE, kMost, 16>(backward, sums);
+enum class NormPass { kForward, kBackward, kSums, kMovingSums };
+template <typename T, bool WIDE, int U, int LANES> const void *norm_kernel(NormPass pass) {
+    switch (pass) {
+        case NormPass::kForward: return (const void *)(layer_norm_kernel<T, WIDE, U, LANES>);
+        case NormPass::kBackward: return (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, false, false>);
+        case NormPass::kSums: return (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, true, false>);
+        default: return (const void *)(layer_norm_backward_kernel<T, WIDE, U, LANES, true, true>);
     }
-    if (s.per_lane == 1) return norm_kernel<T, WIDE, 1, 8>(backward, sums);
-    if constexpr (kMost == 4)
-        if (s.per_lane == 4) return norm_kernel<T, WIDE, 4, 8>(backward, sums);
-    return norm_kernel<T, WIDE, 2, 8>(backward, sums);
 }
-inline const void *norm_kernel(int dtype, bool is_wide, const NormShape &s, bool backward, bool sums) {
+template <typename T, bool WIDE> const void *norm_kernel(const NormShape &s, NormPass pass) {
+    constexpr int kMost = kNormLaneElements * (int)sizeof(T) / 16;
+    if (s.whole) return norm_kernel<T, WIDE, kMost, 0>(pass);
+    switch (s.lanes) {
+        case 64: return norm_kernel<T, WIDE, kMost, 64>(pass);
+        case 32: return norm_kernel<T, WIDE, kMost, 32>(pass);
+        case 16: return norm_kernel<T, WIDE, kMost, 16>(pass);
+    }
+    if (s.per_lane == 1) return norm_kernel<T, WIDE, 1, 8>(pass);
+    if constexpr (kMost == 4)
+        if (s.per_lane == 4) return norm_kernel<T, WIDE, 4, 8>(pass);
+    return norm_kernel<T, WIDE, 2, 8>(pass);
+}
+inline const void *norm_kernel(int dtype, bool is_wide, const NormShape &s, NormPass pass) {
     switch (dtype) {
-        case ISO_DTYPE_F32: return is_wide ? norm_kernel<float, true>(s, backward, sums) : norm_kernel<float, false>(s, backward, sums);
-        case ISO_DTYPE_BF16: return is_wide ? norm_kernel<__bf16, true>(s, backward, sums) : norm_kernel<__bf16, false>(s, backward, sums);
-        default: return is_wide ? norm_kernel<_Float16, true>(s, backward, sums) : norm_kernel<_Float16, false>(s, backward, sums);
+        case ISO_DTYPE_F32: return is_wide ? norm_kernel<float, true>(s, pass) : norm_kernel<float, false>(s, pass);
+        case ISO_DTYPE_BF16: return is_wide ? norm_kernel<__bf16, true>(s, pass) : norm_kernel<__bf16, false>(s, pass);
+        default: return is_wide ? norm_kernel<_Float16, true>(s, pass) : norm_kernel<_Float16, false>(s, pass);
     }
 }
 
@@ -139,8 +152,9 @@ inline int bind_layer_norm(BoundOperator &b, const iso_layer_norm_t &t, const is
     const bool is_wide = wide(t.x, t.channels, t.dtype) && wide(out, t.channels, t.dtype) && wide(in, t.channels, t.dtype) && at_16(t.weight) &&
                          (g || at_16(t.bias));
     a.past_caches = whole_lines(out, t.channels, t.dtype);
-    const void *func = norm_kernel(t.dtype, is_wide, s, g != nullptr, sums);
-    const uint64_t workgroups = norm_workgroups(s, rows, t.heads, sums ? kNormParts : kNormWorkgroups);
+    const NormPass pass = !g ? NormPass::kForward : !sums ? NormPass::kBackward : norm_moves(s, t.heads) ? NormPass::kMovingSums : NormPass::kSums;
+    const void *func = norm_kernel(t.dtype, is_wide, s, pass);
+    const uint64_t workgroups = sums ? norm_parts(s, rows, t.heads) : norm_workgroups(s, rows, t.heads, kNormWorkgroups);
     a.step = workgroups * s.groups();
     a.token_step = a.step / t.heads;
     ISO_TRY(add_launch(b, func, workgroups, s.threads(), a, sums && !s.whole ? 4 * 2 * (size_t)t.channels * 4 : 0));

@@ -6,7 +6,7 @@ import torch
 import paper_1606_07676_amd as iso
 from oracle import token_oracle as orc
 from token_rows import DEV, TYPES, U, host, inside_rows, untouched_around, within
-from token_shapes import NORMS
+from token_shapes import MANY_HEADS, NORMS
 
 pytestmark = pytest.mark.gpu
 
@@ -215,3 +215,19 @@ def test_gradient_against_differences():
                                                b + (s * direction if name == "bias" else 0)).out * dy).sum())
         change = (value(1e-6) - value(-1e-6)) / 2e-6
         assert abs(change - float((host(grads[name]) * direction).sum())) < 1e-5 * np.abs(host(grads[name]) * direction).sum() + 1e-6, name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", MANY_HEADS, ids=str)
+def test_many_heads_with_no_common_factor(shape, dtype):
+    """More heads than workgroups that sum: a lane comes to other heads from row to row."""
+    t = tensors(shape, dtype, seed=14)
+    out, mean, rstd = forward(t)
+    grads = backward(t, mean, rstd)
+    check(t, dtype, out, mean, rstd, grads)
+    dy, again = t["dy"].clone(), t["x"].clone()
+    assert torch.equal(backward(t, mean, rstd, into=dy, dy=dy)["x"], grads["x"])
+    assert torch.equal(forward(dict(t, x=again), again)[0], out)
+    rows = inside_rows(shape, t["x"].dtype, 5, 1)
+    assert torch.equal(forward(t, rows)[0], out)
+    untouched_around(rows)

@@ -8,7 +8,7 @@ import sys
 import numpy as np
 import pytest
 
-from token_shapes import FEW, LARGE, NORMS, TILED
+from token_shapes import FEW, LARGE, MANY_HEADS, NORMS, TILED
 
 N, C, F, H = 40, 24, 32, 3                # tokens, channels, hidden units, heads
 SIZE = {0: 4, 1: 2, 2: 2}
@@ -301,6 +301,16 @@ def test_workspaces(ops):
         assert ops.lib.iso_gated_backward_workspace_bytes(*bad, ctypes.byref(size)) == iso.ISO_ERR_ARG
 
 
+@pytest.mark.parametrize("heads", [1, 3, 31, 300, 509, 4099, 4100, 65521, 65536])
+def test_workspaces_of_norms_do_not_grow_with_the_heads(ops, heads):
+    """One part of the sums for every 256 threads at most, 512 of them, or 1024 of 128."""
+    for dtype in (0, 1, 2):
+        for channels in (1, 24, 128, 1000, 1500, 3000, 16384):
+            for n in (0, 1, 2, 50, 60000):
+                need = ops.bytes_of("iso_layer_norm_backward_workspace_bytes", n, heads, channels, dtype)
+                assert need <= 1024 * 2 * channels * 4, (dtype, channels, n, need)
+
+
 @pytest.mark.parametrize("dtype", [0, 1, 2])
 def test_kernels_of_projections(ops, dtype):
     few = ops.gated(n=64, dtype=dtype)
@@ -403,4 +413,28 @@ def test_gpu_tests_take_every_kernel_of_the_norm(ops):
             for units, lanes in {("1", "8"), ("2", "8"), (most, "8"), (most, "16"), (most, "32"), (most, "64"), (most, "0")}:
                 want.add(("layer_norm", dtype, wide, units, lanes))
                 want |= {("layer_norm_backward", dtype, wide, units, lanes, sums) for sums in "01"}
+    assert taken == want, (want - taken, taken - want)
+
+
+def test_gpu_tests_take_every_kernel_of_the_norm_that_moves_from_head_to_head(ops):
+    taken = set()
+    for n, heads, channels in MANY_HEADS:
+        for dtype in (0, 1, 2):
+            o, h = Operands(ops.stub), ctypes.c_void_p()
+            rows = lambda: o.b.iso_heads_t(o.alloc(n * heads * channels * SIZE[dtype]), heads * channels, channels)       # noqa: E731
+            t = o.b.iso_layer_norm_t(dtype=dtype, heads=heads, channels=channels, n=n, x=rows(), weight=o.alloc(channels * 4))
+            t.mean, t.rstd = o.alloc(n * heads * 4), o.alloc(n * heads * 4)
+            g = o.b.iso_layer_norm_grads_t(rows(), rows(), o.alloc(channels * 4), o.alloc(channels * 4))
+            need = o.bytes_of("iso_layer_norm_backward_workspace_bytes", n, heads, channels, dtype)
+            assert o.lib.iso_layer_norm_backward_init(ctypes.byref(t), ctypes.byref(g), o.alloc(need), need, ctypes.byref(h)) == 0
+            ops.stub.lib.stub_log_clear()
+            assert o.lib.iso_start(h, None) == 0
+            name = ops.stub.lib.stub_log_name(0).decode()
+            m = re.search(r"layer_norm_backward_kernelI(f|DF16b|DF16_)Lb(\d)ELi(\d)ELi(\d+)ELb1ELb1E", name)
+            assert m, name
+            taken.add(m.groups())
+            assert o.lib.iso_request_free(ctypes.byref(h)) == 0
+            o.free()
+    want = {(dtype, wide, *of) for dtype, most in (("f", "4"), ("DF16b", "2"), ("DF16_", "2")) for wide in "01"
+            for of in {("1", "8"), ("2", "8"), (most, "8"), (most, "16"), (most, "32"), (most, "64"), (most, "0")}}
     assert taken == want, (want - taken, taken - want)

@@ -273,6 +273,53 @@ def test_overlaps_and_what_may_be_in_place(ops):
     assert ops.project(t) == 0
 
 
+def test_partial_overlaps(ops):
+    """Inside one buffer that holds both, so that nothing but the overlap is wrong."""
+    meet, rows, heads = ops.iso.ISO_ERR_OVERLAP, ops.b.iso_rows_t, ops.b.iso_heads_t
+    size = N * H * C * 4
+    for on, want in ((4, meet), (C * 4, meet), (H * C * 4, meet), (size - 4, meet), (size, 0)):
+        both = ops.alloc(2 * size)
+        for x, out in ((both, both + on), (both + on, both)):
+            assert ops.forward(ops.norm(x=heads(x, H * C, C), out=heads(out, H * C, C))) == want, on
+            assert ops.backward(ops.norm(x=heads(x, H * C, C)), ops.norm_grads(grad_x=heads(out, H * C, C))) == want, on
+            assert ops.backward(ops.norm(), ops.norm_grads(grad_out=heads(x, H * C, C), grad_x=heads(out, H * C, C))) == want, on
+    size = N * C * 4
+    for on, want in ((4, meet), (C * 4, meet), (size - 4, meet), (size, 0)):
+        both = ops.alloc(2 * size)
+        for name in ("x", "residual"):
+            for x, out in ((both, both + on), (both + on, both)):
+                assert ops.drop(ops.dropout(**{name: rows(x, C), "out": rows(out, C)})) == want, (name, on)
+    length = {"x": N * C * 4, "gate": F * C * 4, "up": F * C * 4, "out": N * F * 4, "grad_out": N * F * 4, "grad_x": N * C * 4,
+              "grad_gate": F * C * 4, "grad_up": F * C * 4}
+    width = {"out": F, "grad_out": F}
+    for name in ("x", "gate", "up"):
+        for on, want in ((-4, meet), (4 - length["out"], meet), (-length["out"], 0), (4, meet), (length[name] - 4, meet), (length[name], 0)):
+            at = ops.alloc(3 * length["out"]) + length["out"]
+            assert ops.project(ops.gated(**{name: rows(at, C), "out": rows(at + on, F)})) == want, (name, on)
+    # a gradient over an operand, or over another gradient
+    for name in ("grad_x", "grad_gate", "grad_up"):
+        for other in ("x", "gate", "up", "grad_out", "grad_x", "grad_gate", "grad_up"):
+            if other == name:
+                continue
+            for on, want in ((4, meet), (length[other] - 4, meet), (length[other], 0)):
+                at = ops.alloc(length[other] + length[name])
+                t, g = ops.gated(), ops.gated_grads()
+                setattr(g if other.startswith("grad") else t, other, rows(at, width.get(other, C)))
+                setattr(g, name, rows(at + on, C))
+                assert ops.project_back(t, g) == want, (name, other, on)
+    # a workspace over an operand's end, and behind it
+    need = ops.bytes_of("iso_gated_backward_workspace_bytes", N, C, F, 0)
+    for name in ("x", "gate", "up", "grad_out", "grad_x", "grad_gate", "grad_up"):
+        at, t, g = ops.alloc(length[name] + need), ops.gated(), ops.gated_grads()
+        setattr(g if name.startswith("grad") else t, name, rows(at, width.get(name, C)))
+        assert ops.project_back(t, g, work=at + length[name] - 16) == meet and ops.project_back(t, g, work=at + length[name]) == 0, name
+    need, size = ops.bytes_of("iso_layer_norm_backward_workspace_bytes", N, H, C, 0), N * H * C * 4
+    for name in ("x", "grad_out", "grad_x"):
+        at, t, g = ops.alloc(size + need), ops.norm(), ops.norm_grads()
+        setattr(g if name.startswith("grad") else t, name, heads(at, H * C, C))
+        assert ops.backward(t, g, work=at + size - 4) == meet and ops.backward(t, g, work=at + size) == 0, name
+
+
 def test_slices_of_one_buffer(ops):
     """Weights and their gradients side by side in rows of one buffer."""
     both, grads = ops.alloc(F * 2 * C * 4), ops.alloc(F * 2 * C * 4)

@@ -258,3 +258,40 @@ def test_hidden_units_with_small_gradients_beside_others_in_float16(shape):
         within(host(got)[rows], want[rows], orc.rounded(want, error, U["f16"])[rows], "small rows")
         assert rms(host(got)[rows] - want[rows]) <= small_bound(want[rows])
     check(t, "f16", "gelu", forward(t, "gelu"), grads)
+
+
+def test_weights_gradients_beyond_32_bits_of_bytes():
+    """Rows of grad_gate and grad_up that sum over all of 70000 tokens, the last of which lie behind 2^32 bytes of grad_out, d_gate and
+    d_up: the oracle's, for the first and the last hidden units."""
+    n, C, F, some = 70000, 8, 32776, 24
+    g = torch.Generator(DEV).manual_seed(15)
+    normal = lambda *size: torch.randn(*size, device=DEV, generator=g).to(torch.bfloat16)  # noqa: E731
+    t = {"x": normal(n, C), "gate": normal(F, C), "up": normal(F, C), "dy": torch.empty(n, F, device=DEV, dtype=torch.bfloat16)}
+    t["dy"].normal_(generator=g)
+    t["dy"][-40:] *= 100                                   # the last tokens weigh as much as a tenth of all others
+    grads = backward(t, "silu")
+    for rows in (slice(0, some), slice(F - some, F)):
+        o = orc.Gated(host(t["x"]), host(t["gate"][rows]), host(t["up"][rows]), "silu", True)
+        o.backward(host(t["dy"][:, rows]), U["bf16"])
+        near(grads["gate"][rows], o.grad_gate, o.grad_gate_error, U["bf16"], "grad_gate")
+        near(grads["up"][rows], o.grad_up, o.grad_up_error, U["bf16"], "grad_up")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+def test_many_tiles_of_gelu(shape, dtype):
+    """The larger tiles' ends, whole and cut off, with the other activation."""
+    t = tensors(*shape, dtype, seed=16)
+    check(t, dtype, "gelu", forward(t, "gelu"), backward(t, "gelu"))
+
+
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(2048, 72, 2048), (1024, 136, 512), (1100, 136, 1100)], ids=str)
+def test_far_ends_of_the_activations_in_larger_tiles(shape, dtype, activation):
+    n, C, F = shape
+    t = tensors(n, C, F, dtype, seed=17)
+    t["x"][:, 0] = 1
+    t["gate"][:, 1:] = 0
+    t["gate"][:, 0] = torch.linspace(-300, 300, F, device=DEV).to(TYPES[dtype])
+    check(t, dtype, activation, forward(t, activation), backward(t, activation))

@@ -1,8 +1,13 @@
 """The 64-bit definitions of layer norm, gated projections and dropout: their gradients against differences, and the generator
 against the known answers that its authors published."""
+import os
+import re
+
 import numpy as np
 import pytest
+from scipy.special import erfcx
 
+from conftest import ROOT
 from oracle import token_oracle as orc
 
 
@@ -54,3 +59,30 @@ def test_kept_elements():
     assert keep.reshape(-1).tolist() == [n >= 16384 for n in numbers] and factor == 4 / 3
     assert orc.kept(40, 50, (-1, 2), 0.0)[0].all() and not orc.kept(40, 50, (1, -2), 1.0)[0].any()
     assert abs(orc.kept(400, 500, (5, 6), 0.1)[0].mean() - 0.9) < 5 * (0.09 / 2e5) ** 0.5
+
+
+def test_the_fit_of_the_error_function():
+    """0.5 erfc(|g| / sqrt 2) = t P(t) exp(-g^2 / 2) with the kernel's own constants: in exact arithmetic as near as its comment says;
+    in 32 bits off by the argument's three roundings, together 1.5 g^2 units of 2^-24, one unit each for the exponential and the
+    last two products, 1.4 for the fit, and what is left of 8 for t and the terms."""
+    text = open(os.path.join(ROOT, "paper_1606_07676_amd", "csrc", "iso_gated_kernels.hpp")).read()
+    terms = np.array([float(x.rstrip("f")) for x in re.search(r"kTerms\[9\] = \{([^}]*)\}", text)[1].replace("\n", " ").split(",")], dtype=np.float32)
+    assert len(terms) == 9 and "fmaf(0.26f, fabsf(g), 1.f)" in text
+    f32, wide = np.float32, np.longdouble
+    g = np.linspace(0, 14.5, 200001).astype(f32)
+    scaled = 0.5 * erfcx(g.astype(float) / np.sqrt(2))                   # without the exponential
+    t = 1 / (1 + wide(f32(0.26)) * g.astype(wide))
+    rest = np.full(g.shape, terms[8], dtype=wide)
+    for term in terms[7::-1]:
+        rest = wide(term) + t * rest
+    assert float(np.abs(rest * t / scaled - 1).max()) < 7.9e-8
+    fma = lambda a, b, c: (a.astype(float) * b.astype(float) + c.astype(float)).astype(f32)       # noqa: E731
+    t = (1 / fma(f32(0.26), g, f32(1)).astype(float)).astype(f32)
+    e = np.exp2((f32(-0.5 * 1.44269504088896340736) * (g * g)).astype(float)).astype(f32)
+    rest = np.full(g.shape, terms[8])
+    for term in terms[7::-1]:
+        rest = fma(t, rest, term)
+    rest = rest * (t * e)
+    there = g < 12.5                                                    # above, 32 bits hold the share with fewer bits
+    want = scaled * np.exp(-0.5 * g.astype(float) ** 2)
+    assert np.all(np.abs(rest / want - 1)[there] < 2.0 ** -24 * (8 + 2 * g[there].astype(float) ** 2))

@@ -46,8 +46,9 @@ __device__ __forceinline__ uint4 philox_block(uint64_t counter, uint64_t more, u
 // rows of whole blocks.  A lane makes one block of numbers; two 16-byte units of float32 are those of a block, and the wavefront
 // hands the numbers round so that its loads and stores stay dense.
 //
-// The tensors' bytes bound it: 32768 x 1024 in bfloat16 with a residual 201 MB in 28.6 us, 7.0 TB/s, without 134 MB in 19.9.  Two or
-// four blocks a lane are slower by 2 and 8 %; stores that stay in the caches take 36.4 us, loads that do not 32.4.
+// The tensors' bytes bound it: 32768 x 1024 in bfloat16 with a residual 201 MB in 34.5 us, 5.8 TB/s, without 134 MB in 23.2, inputs
+// from memory (1.6 GB of them take turns).  Stores that stay in the caches take 36.3 and 24.2 us, loads past them as well 33.1 and
+// 22.8.  Tensors that are not WIDE go element by element: 65535 rows of 333 inside rows of 336 in bfloat16 50 us, dense rows of 336 15.8.
 template <typename T, bool WIDE, bool RESIDUAL> __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a) {
     constexpr int E = ElementTraits<T>::kPerLane, kUnits = 8 / E;
     typedef T vec_t __attribute__((ext_vector_type(E)));

@@ -20,9 +20,9 @@
 // whose summed axis is its rows' (DOWN below) is read back transposed, so none is ever laid out anew in memory.
 //
 // The matrix units bound it for large products, up to the tiles' ends and what loads take from them: 32768 tokens, 1024 channels,
-// 4096 hidden units, bfloat16, 450 us forward, 1.22 PFLOP/s (a library product of these sizes 1.26); 8192 of each 1.33.  The
-// gradients at 2816 hidden units 1.1 ms: 382, 311 and 360 us for the three products, 21 for the sums of the last one's parts.
-// float32 reaches 135 TFLOP/s of a library product's 153.
+// 4096 hidden units, bfloat16, 468 us forward with inputs from memory, 1.17 PFLOP/s (a library product of these sizes 1.26); 8192 of
+// each 1.41.  The gradients at 2816 hidden units 1.09 ms: 404, 311 and 362 us for the three products, 25 for the sums of the last
+// one's parts.  float32 reaches 135 TFLOP/s of a library product's 153.
 #pragma once
 
 #include "iso_attention_kernels.hpp"
@@ -728,8 +728,8 @@ template <typename T> __global__ __launch_bounds__(256) void product_sum_kernel(
 
 // 16 hidden units of both weights to a workgroup, for up to 16 NT tokens: the weights' bytes bound it, so they go from memory to
 // the matrix units' registers once, with no stage between, and the wavefronts share the channels and join their sums in LDS.
-// 1 token, 2048 channels, 5632 hidden units, bfloat16: 46 MB in 13 us with the launch, 5 TB/s without; 4 or 16 wavefronts, and twice
-// as many products at once, change that by less than 5 %.
+// 1 token, 2048 channels, 5632 hidden units: 46 MB in bfloat16 in 15.6 us from memory, in 14.0 where the last-level cache holds them, 92 MB
+// in float32 in 28.1; 4 or 16 wavefronts, and twice as many products at once, change that by less than 5 %.
 template <typename T, int NT, bool BACKWARD, bool DIRECT>
 __global__ __launch_bounds__(512) void gated_few_kernel(const ProductArgs a) {
     constexpr int E = 16 / sizeof(T), kStep = 4 * E;       // channels of one product: 32 of 16 bits, 16 of 32

@@ -8,9 +8,10 @@
 // of a workgroup.  So each tensor is gone through once, and its bytes bound the kernels.  Lanes keep their places in the row, and
 // their head, from row to row, the next row is under way while one is worked on, weights stay in registers, and so do the sums
 // over rows of the weight's and the bias's gradient.  Rows of whole 128-byte lines are stored past the caches, which then hold
-// more of what is read: 32768 x 1024 in bfloat16 134 MB in 22.5 us (23.3 otherwise), 70000 x 512 in float32 287 MB in 47.2 (55.3),
-// gradients of the former 201 MB in 39.3 (44.1); queries and keys of 64 x 64 x 64 ranks, 10 heads of 128 in bfloat16, 1.34 GB in
-// 260 (272), where vector arithmetic takes part.  Loads past the caches: 27.2, 52.0, 42.6 and 253.
+// more of what is read: 32768 x 1024 in bfloat16 134 MB in 25.6 us (26.2 otherwise), 70000 x 512 in float32 287 MB in 49.9 (52.6),
+// gradients of the former 201 MB in 43.5 (44.2); queries and keys of 64 x 64 x 64 ranks, 10 heads of 128 in bfloat16, 1.34 GB in
+// 251 (263), where vector arithmetic takes part.  Loads past the caches as well: 27.6, 49.9, 42.3 and 243.  Times here and below are
+// of passes whose inputs take turns, 1.6 GB of them, so that they come from memory.
 #pragma once
 
 #include "iso_attention_kernels.hpp"
@@ -102,7 +103,7 @@ template <typename T, bool WIDE, int U, int LANES> struct NormLane {
     __device__ __forceinline__ bool unit_there(int u) const { return place + u * lanes < units; }
     // Where unit u of this lane begins in the row.  A last unit that is not whole ends with the row and begins inside the one before:
     // both hold, and store, the same values there, and sums take them once.  No load waits for the elements of a broken unit then
-    // (gradients of 37271 x 483 in float16 26.3 us, with single elements 37.4).
+    // (gradients of 37271 x 483 in float16 30.6 us, with single elements 47.7).
     __device__ __forceinline__ int begin(int u) const {
         const int at = (place + u * lanes) * E;
         return WIDE ? at : max(0, min(at, channels - E));

@@ -21,7 +21,7 @@ inline bool same_rows(const iso_rows_t &a, const iso_rows_t &b) { return a.data 
 inline iso_heads_t one_head(const iso_rows_t &t) { return iso_heads_t{t.data, t.stride, 0}; }
 inline bool wide(const iso_rows_t &t, int elements, int dtype) { return wide(one_head(t), elements, dtype); }
 // Rows of whole 128-byte lines: they may be stored past the caches, where others would be written to memory in pieces (norm of
-// 100000 x 232 in bfloat16, 16 us in place of 18; 100000 x 3 heads of 72, 17 and 20).
+// 100000 x 3 heads of 72 in bfloat16, 22.9 us in place of 21.2; 100000 x 232 21.1 and 20.9).
 inline bool whole_lines(const iso_heads_t &t, int elements, int dtype) {
     const uint64_t size = dtype_size(dtype);
     return (((uintptr_t)t.data | (uint64_t)t.rank_stride * size | (uint64_t)t.head_stride * size | (uint64_t)elements * size) & 127) == 0;
@@ -53,11 +53,11 @@ inline uint64_t norm_workgroups(const NormShape &s, uint64_t rows, uint64_t head
     const uint64_t unit = norm_unit(s, heads);
     return std::min((norm_need(s, rows) + unit - 1) / unit, std::max<uint64_t>(1, norm_limit(s, most) / unit)) * unit;
 }
-// Of 256 threads.  Norms with 768, 1536, 2048, 3072, us: 32768 x 1024 in bfloat16 23.1, 22.5, 22.7, 21.9; 70000 x 512 in float32
-// 47.1, 48.5, 47.6, 45.8; 262144 x 10 heads of 128 264, 254, 261, 251.  Gradients with 512, 768, 1024 parts, before their stores went
-// past the caches, us: 32768 x 1024 in bfloat16 44.0, 45.8, 54.0 (a CU holds 3 workgroups); 37271 x 483 in float16 39.7, 36.0, 44.8;
-// 70000 x 512 in float32 85.8, 86.9, 88.4; 100000 x 16 heads of 64 115.9, 123.9, 127.0.
-constexpr uint64_t kNormWorkgroups = 3072, kNormParts = 512;
+// Of 256 threads.  Norms with 3, 6, 8 and 12 for each CU, inputs from memory, us: 32768 x 1024 in bfloat16 26.1, 25.9, 25.8, 25.6;
+// 70000 x 512 in float32 50.8, 51.0, 51.3, 49.9; 262144 x 10 heads of 128 265, 254, 261, 251.  Gradients with 256, 512, 768, 1024 parts:
+// 32768 x 1024 in bfloat16 42.7, 43.5, 44.6, 50.3 (a CU holds 3 workgroups); 37271 x 483 in float16 31.7, 30.6, 31.0, 36.3; 70000 x 512
+// in float32 78.7, 81.6, 83.1, 83.5; 100000 x 16 heads of 64 160, 113, 118, 122.
+constexpr uint64_t kNormWorkgroups = 12 * 256, kNormParts = 512;
 // Workgroups of a gradient that sums over rows, each of which leaves a part of the sums.  Where one token's rows take more than the
 // limit, lanes move from head to head instead: 64 x 4099 heads of 128 in bfloat16 39.0 us with 512 parts, with 4099 59.7.
 inline bool norm_moves(const NormShape &s, uint64_t heads) { return norm_unit(s, heads) > norm_limit(s, kNormParts); }
@@ -449,14 +449,15 @@ class GatedBinder {
         gate = device_rows(t.gate);
         up = device_rows(t.up);
         a.out[0] = device_rows(t.out);
-        // What is stored past the caches leaves them to the operands: 32768 tokens, 1024 channels, 4096 hidden units, bfloat16, 450 us
-        // in place of 490.  Not where a wavefront's 64 bytes of a row are parts of more: 133 became 166 us for 232 channels.
+        // What is stored past the caches leaves them to the operands: 32768 tokens, 1024 channels, 4096 hidden units, bfloat16, 468 us
+        // in place of 492.  Not where a wavefront's 64 bytes of a row are parts of more lines: 117 became 122 us for 232 channels and
+        // 2044 hidden units, though 499 became 488 for 1024 and 4092.
         a.past_caches = (((uintptr_t)t.out.data | (uint64_t)t.out.stride * dtype_size(t.dtype)) & 63) == 0;
         return add_projections<false>(a);
     }
 
     // The backward pass's products need rows on 16-byte boundaries in whole units: others are copied first.  2000 tokens, 2685
-    // channels, 8192 hidden units, bfloat16: 0.65 ms in place of 2.2 with products that take such rows through registers.
+    // channels, 8192 hidden units, bfloat16: 0.60 ms in place of 2.2 with products that take such rows through registers.
     int align_rows(char *workspace) {
         AlignArgs a{};
         a.channels = t.channels;

@@ -295,3 +295,46 @@ def test_far_ends_of_the_activations_in_larger_tiles(shape, dtype, activation):
     t["gate"][:, 1:] = 0
     t["gate"][:, 0] = torch.linspace(-300, 300, F, device=DEV).to(TYPES[dtype])
     check(t, dtype, activation, forward(t, activation), backward(t, activation))
+
+
+@pytest.mark.parametrize("shape", [(40, 72, 130), (700, 72, 130), (2100, 136, 1100)], ids=str)
+def test_which_gradients_are_small_is_found_at_every_start(shape):
+    """One request, started eagerly and replayed, over gradients of changing size, in a workspace that holds what was before."""
+    (n, C, F), half = shape, torch.float16
+    t = tensors(*shape, "f16", seed=18)
+    sizes = [t["dy"].clone(), (t["dy"].float() * 1e-5).to(half), torch.zeros_like(t["dy"]), t["dy"].clone(), (t["dy"].float() * 1e-6).to(half)]
+    sizes[3][::3] *= 1e-5
+    wants = [{k: v.clone() for k, v in backward(dict(t, dy=dy), "silu").items()} for dy in sizes]
+    grads = {k: torch.empty_like(t[k]) for k in ("x", "gate", "up")}
+    work = torch.empty(iso.iso_gated_backward_workspace_bytes(n, C, F, half), dtype=torch.uint8, device=DEV)
+    req = iso.iso_gated_backward_init(t["x"], t["gate"], t["up"], t["dy"], grads["x"], grads["gate"], grads["up"], work)
+    iso.iso_start(req)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        iso.iso_start(req)
+    for turn in range(2):
+        for i, dy in enumerate(sizes):
+            for start in (lambda: iso.iso_start(req), graph.replay):
+                t["dy"].copy_(dy)
+                for v in grads.values():
+                    v.fill_(7)
+                start()
+                torch.cuda.synchronize()
+                for name, want in wants[i].items():
+                    assert torch.equal(grads[name], want), (turn, i, name)
+
+
+@pytest.mark.parametrize("n", [30, 300])
+def test_gradients_that_are_not_numbers_stay_by_themselves_in_float16(n):
+    """Beside small ones, which stay as exact as they were."""
+    t = tensors(n, 72, 70, "f16", seed=19)
+    t["dy"] = (t["dy"].float() * 1e-5).to(torch.float16)
+    clean = backward(t, "silu")
+    t["dy"][3, 5], t["dy"][n - 1, 69], t["dy"][17, 33] = float("nan"), float("inf"), float("-inf")
+    grads = backward(t, "silu")
+    good, rows = torch.ones(n, dtype=torch.bool, device=DEV), torch.ones(70, dtype=torch.bool, device=DEV)
+    good[[3, 17, n - 1]], rows[[5, 33, 69]] = False, False
+    assert torch.equal(grads["x"][good], clean["x"][good]) and not grads["x"][~good].isfinite().any()
+    for name in ("gate", "up"):
+        assert torch.equal(grads[name][rows], clean[name][rows]) and not grads[name][~rows].isfinite().any()
